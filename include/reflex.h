@@ -328,6 +328,117 @@ typedef struct {
 /* a  fp32 [B][T][A], updated in place;  cond [B][Cd];  k, K as in reflex_flow_step. Errors as the single calls. */
 int reflex_expert_step(reflex_cache_t *cache, const reflex_expert *expert, float *a, const void *cond, int k, int K, void *stream);
 
+/* ---- Sec. 3.1 "Incremental Prefill" (only the newest frame is encoded): the paged prefix of the vision-language backbone ----
+ * The action expert's static prefix is what the backbone computes; these calls hold it while it grows. Per layer of the backbone and
+ * chunk of new tokens: queries and keys are rotated by their positions (reflex_rotary_axes), keys and values go into pages
+ * (reflex_pages_write, which rotates the keys itself where asked to), the chunk attends to everything the pages hold
+ * (reflex_pages_attention); the finished prefix, or its newest tokens, are read back (reflex_pages_read) as reflex_cache_init_static,
+ * reflex_cache_stage_static and reflex_cache_append_sliding take them.
+ *
+ * Sequences share a pool of pages of `page` tokens. Token p of sequence b lies in page table[b][p / page], slot p % page. A row is the
+ * d elements of one (token, KV head), held
+ *   REFLEX_PAGE_SAME   in dtype;
+ *   REFLEX_PAGE_INT8   as q[i] * 2^(e - 127): q whole numbers in [-127, 127], one exponent byte e for the row;
+ *   REFLEX_PAGE_E4M3   the same with q in e4m3 (finite codes only).
+ * e - 127 is the smallest exponent under which the row's largest magnitude fits (127 or 448), at least -100. Elements are rounded to the
+ * nearest q, ties to the even one; magnitudes above 2^127 are held as 2^127. Scaling by a power of two is exact, so that rounding is
+ * the only one, and what a row stands for is exact in bf16 and in fp32. A row with an infinity or a NaN gets e = 255 and reads as NaN
+ * throughout. */
+#define REFLEX_PAGE_SAME 0
+#define REFLEX_PAGE_E4M3 1
+#define REFLEX_PAGE_INT8 2
+
+typedef struct reflex_pages reflex_pages_t; /* opaque, host-side */
+typedef struct {
+    int32_t L, n_pages; /* layers, pages of a layer                                                     */
+    int32_t page;       /* tokens of a page: 16, 32, 64 or 128                                           */
+    int32_t Hq, Hkv, d; /* as in reflex_cache_desc                                                       */
+    int32_t dtype;      /* REFLEX_DTYPE_* of the rows that are written, read and attended with           */
+    int32_t format;     /* REFLEX_PAGE_*                                                                 */
+    int32_t max_seqs;   /* most sequences of a call, at most 1024                                        */
+    int32_t max_rows;   /* most rows of q of a call of reflex_pages_attention                            */
+} reflex_pages_desc;
+
+/* The sequences of a call: device arrays, so that a captured graph sees each replay's. Rows of packed tensors (k, v, q, out) are
+ * tokens: sequence b's new tokens are rows [cu[b], cu[b + 1]), the last ones of its len[b] tokens (positions len[b] - n .. len[b] - 1).
+ * Rows behind cu[B] are padding: read or written by nothing. cu starts at 0 and does not decrease. Sequences may have no new token, or
+ * no token at all. Sequences may share pages that nobody writes; a call that writes one (page, slot) twice leaves either row there, or
+ * parts of both.
+ * The kernels check what they follow: a table entry outside [0, n_pages) or a position outside [0, max_pages * page) is never
+ * dereferenced. What such a token would have written is left out, what would have been read through it (the row read back; every row of
+ * the sequence's attention that sees it) is NaN, and reflex_pages_check_status names the sequence. */
+typedef struct {
+    const int32_t *table; /* device [B][max_pages]                          */
+    const int32_t *cu;    /* device [B + 1] (reflex_pages_read: may be NULL) */
+    const int32_t *len;   /* device [B]                                     */
+    int32_t B, max_pages;
+} reflex_page_batch;
+
+/* Rotary positions with several axes (time, height, width of images and video; one axis: text). Pair i of a row turns by the angle
+ * pos[axis[i]][token] * freq[i] (radians; freq 0: not at all). Pairs are elements (i, i + R / 2), or (2i, 2i + 1) where adjacent;
+ * elements from R on are left as they are. */
+typedef struct {
+    const float *freq;   /* device [R / 2]                                              */
+    const uint8_t *axis; /* device [R / 2]; an axis >= axes does not turn its pair       */
+    int32_t R;           /* a multiple of 16, at most d                                 */
+    int32_t axes;        /* 1 .. 8                                                      */
+    int32_t adjacent;
+} reflex_rotary;
+
+/* y = x rotated (inverse: by the opposite angles, which is also the gradient with respect to x of a loss whose gradient with respect
+ * to y is given as x, and takes a row back to where it came from). Angles are reduced exactly in 64-bit integers, so positions
+ * of any size lose nothing; the products are fp32, rounded to dtype once.
+ *   x, y   device [n][H][d] dtype, tokens ldx / ldy elements apart (heads of a packed projection: ldx > H d); y may be x itself
+ *          (same ld) but must not overlap it otherwise
+ *   pos    device int32 [axes][n]
+ * Requirements: d % 16 == 0, d <= 1024; ldx, ldy multiples of 8, at least H d; n >= 0 (0: nothing to do); pointers 16-byte aligned
+ * (axis, freq, pos: to their elements). */
+int reflex_rotary_axes(const void *x, int64_t ldx, void *y, int64_t ldy, const int32_t *pos, const reflex_rotary *rot, int n, int H, int d,
+                       int inverse, int dtype, void *stream);
+
+/* Bytes of ONE pool (K or V): [L][n_pages][Hkv][page][d] elements; of ONE array of exponent bytes [L][n_pages][Hkv][page] (0 for
+ * REFLEX_PAGE_SAME); of the workspace (status word, partial results of split sequences and, for 8-bit formats, one layer's pages in bf16). 0 for
+ * an invalid descriptor. */
+size_t reflex_pages_pool_bytes(const reflex_pages_desc *desc);
+size_t reflex_pages_exp_bytes(const reflex_pages_desc *desc);
+size_t reflex_pages_workspace_bytes(const reflex_pages_desc *desc);
+
+/* A handle over caller-owned device memory (pools and exponents 16-byte aligned, contents kept as found; workspace 256-byte aligned, its
+ * status part is cleared on `stream`). k_exp, v_exp: NULL for REFLEX_PAGE_SAME. The memory must outlive the handle. The handle
+ * belongs to the device that is current; calls with another current device are refused (REFLEX_ERR_STATE).
+ * Calls of reflex_pages_attention on one handle must be ordered (one stream, or events): they share the workspace. Handles with
+ * workspaces of their own may share pools. */
+int reflex_pages_create(const reflex_pages_desc *desc, void *k_pool, void *v_pool, void *k_exp, void *v_exp, void *workspace, void *stream,
+                        reflex_pages_t **out);
+int reflex_pages_destroy(reflex_pages_t *pages);
+/* REFLEX_OK, REFLEX_ERR_TIMEOUT (a bounded device-side wait ran out) or REFLEX_ERR_STATE (a sequence's table entry or position was outside the
+ * pool or the table); synchronises `stream`. The word keeps the first event until the handle is created again. */
+int reflex_pages_check_status(reflex_pages_t *pages, void *stream);
+
+/* The new tokens' keys and values into their pages of one layer.
+ *   k, v   device [n_rows][Hkv][d] dtype, tokens ldk / ldv elements apart (multiples of 8)
+ *   rot    NULL: keys as they are; else keys are rotated first (in fp32, with no rounding before that of the page's format)
+ *   pos    device int32 [axes][n_rows], or NULL with rot == NULL */
+int reflex_pages_write(reflex_pages_t *pages, int layer, const reflex_page_batch *batch, const void *k, int64_t ldk, const void *v, int64_t ldv,
+                       int n_rows, const reflex_rotary *rot, const int32_t *pos, void *stream);
+
+/* Tokens [start[b], len[b]) of every sequence (start NULL: 0; a negative start counts as 0) and of layers [layer, layer + n_layers) back as dense rows.
+ *   k_out, v_out   device [B][n_layers][S_out][Hkv][d] dtype: token p to row p - start[b]; rows past a sequence's last token are left
+ *                  as they were, tokens past S_out rows are left out */
+int reflex_pages_read(reflex_pages_t *pages, int layer, int n_layers, const reflex_page_batch *batch, const int32_t *start, void *k_out, void *v_out,
+                      int S_out, void *stream);
+
+/* The new tokens' attention over the pages of one layer (their own keys and values included: write them first):
+ *   out = softmax(scale * q K^T + mask) V,   KV head of query head h: h / (Hq / Hkv)
+ *   q, out   device [n_rows][Hq][d] dtype
+ *   scale    <= 0 selects 1/sqrt(d)
+ *   causal   0: every new token sees all len[b] tokens; 1: the token at position p sees positions <= p
+ *   window   > 0: only positions > p - window; 0: no limit
+ * A row that sees nothing is 0. Softmax and sums are fp32; on the tensor cores the weights are rounded to bf16 before they meet V.
+ * Requirements: n_rows <= max_rows; d as for reflex_cache_create. */
+int reflex_pages_attention(reflex_pages_t *pages, int layer, const reflex_page_batch *batch, const void *q, void *out, int n_rows, float scale,
+                           int causal, int window, void *stream);
+
 /* ---- Sec. 3.4 "Stream Throughput: Asynchronous Pipeline", Algorithm 1 (future-conditional overlap scheduling), Eq. 3 ----
  * Host logic only; no device work. A control loop calls reflex_overlap_tick once per control period:
  *   - the event names the action to execute (chunk index, position in the chunk; Algorithm 1 line 5);

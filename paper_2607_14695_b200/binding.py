@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libreflex_b200.so")
 DTYPE_BF16 = 0
 DTYPE_F32 = 1
 ATTN_AUTO, ATTN_SIMT, ATTN_TC, ATTN_TC2 = 0, 1, 2, 3
+PAGE_SAME, PAGE_E4M3, PAGE_INT8 = 0, 1, 2
 
 OK = 0
 ERR_INVALID_ARG, ERR_SHAPE, ERR_ALIGN, ERR_STATE, ERR_CUDA, ERR_TIMEOUT, ERR_NOT_IMPLEMENTED = -1, -2, -3, -4, -5, -6, -7
@@ -30,6 +31,8 @@ EXPORTS = [
     "reflex_adarmsnorm", "reflex_adarmsnorm_gate", "reflex_adarmsnorm_noalloc", "reflex_adarmsnorm_qkv", "reflex_adarmsnorm_swiglu", "reflex_linear_residual", "reflex_partitioned_attention",
     "reflex_flow_step", "reflex_expert_step", "reflex_overlap_create", "reflex_overlap_destroy", "reflex_overlap_tick", "reflex_overlap_inference_done",
     "reflex_overlap_simulate",
+    "reflex_rotary_axes", "reflex_pages_pool_bytes", "reflex_pages_exp_bytes", "reflex_pages_workspace_bytes", "reflex_pages_create", "reflex_pages_destroy",
+    "reflex_pages_check_status", "reflex_pages_write", "reflex_pages_read", "reflex_pages_attention",
 ]
 
 
@@ -52,6 +55,20 @@ class OverlapStats(ctypes.Structure):
 
 class CacheDesc(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("L", "B", "Hq", "Hkv", "d", "S_max", "N", "T_max", "dtype", "static_banks")]
+
+
+class PagesDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("L", "n_pages", "page", "Hq", "Hkv", "d", "dtype", "format", "max_seqs", "max_rows")]
+
+
+class PageBatchDesc(ctypes.Structure):
+    """struct reflex_page_batch."""
+    _fields_ = [("table", ctypes.c_void_p), ("cu", ctypes.c_void_p), ("len", ctypes.c_void_p), ("B", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class RotaryDesc(ctypes.Structure):
+    """struct reflex_rotary."""
+    _fields_ = [("freq", ctypes.c_void_p), ("axis", ctypes.c_void_p), ("R", ctypes.c_int32), ("axes", ctypes.c_int32), ("adjacent", ctypes.c_int32)]
 
 
 class ReflexError(RuntimeError):
@@ -106,6 +123,16 @@ def load():
     lib.reflex_overlap_tick.argtypes = [vp, ctypes.POINTER(OverlapEvent)]
     lib.reflex_overlap_inference_done.argtypes = [vp, dbl]
     lib.reflex_overlap_simulate.argtypes = [i, dbl, dbl, ctypes.POINTER(dbl), i, i, i, ctypes.POINTER(OverlapStats)]
+    pp, bp, rp, i64 = ctypes.POINTER(PagesDesc), ctypes.POINTER(PageBatchDesc), ctypes.POINTER(RotaryDesc), ctypes.c_int64
+    lib.reflex_rotary_axes.argtypes = [vp, i64, vp, i64, vp, rp, i, i, i, i, i, vp]
+    for fn in (lib.reflex_pages_pool_bytes, lib.reflex_pages_exp_bytes, lib.reflex_pages_workspace_bytes):
+        fn.argtypes = [pp]; fn.restype = ctypes.c_size_t
+    lib.reflex_pages_create.argtypes = [pp, vp, vp, vp, vp, vp, vp, ctypes.POINTER(vp)]
+    lib.reflex_pages_destroy.argtypes = [vp]
+    lib.reflex_pages_check_status.argtypes = [vp, vp]
+    lib.reflex_pages_write.argtypes = [vp, i, bp, vp, i64, vp, i64, i, rp, vp, vp]
+    lib.reflex_pages_read.argtypes = [vp, i, i, bp, vp, vp, vp, i, vp]
+    lib.reflex_pages_attention.argtypes = [vp, i, bp, vp, vp, i, f, i, i, vp]
     for name in EXPORTS:
         getattr(lib, name)  # every declared symbol must resolve
     _lib = lib
@@ -412,6 +439,113 @@ def prepare_flow_step(x, v, x_lowp, k, K):
     B, T, A = x.shape
     args = (_ptr(x), _ptr(v), _ptr(x_lowp), B, T, A, int(k), int(K), dtype_code(v))
     return _prepared(load().reflex_flow_step, args)
+
+
+# ---- the paged prefix: rotary positions, page writes and reads, attention of new tokens over pages ----
+
+class Rotary:
+    """Rotary positions with several axes: pair i turns by pos[axis[i]] * freq[i]. freq: device fp32 [R / 2]; axis: device uint8 [R / 2];
+    pairs are (i, i + R / 2), or (2i, 2i + 1) where adjacent."""
+
+    def __init__(self, freq: torch.Tensor, axis: torch.Tensor, adjacent: bool = False):
+        self.freq, self.axis, self.adjacent = freq, axis, int(bool(adjacent))
+
+
+class PageBatch:
+    """The sequences of a call, device int32: table [B][max_pages]; cu [B + 1] (new tokens of sequence b: rows [cu[b], cu[b + 1]); None for
+    reads); length [B] (tokens with the new ones)."""
+
+    def __init__(self, table: torch.Tensor, cu: Optional[torch.Tensor], length: torch.Tensor):
+        self.table, self.cu, self.length = table, cu, length
+
+
+class Pages:
+    """Pools of pages (allocated through torch unless lent as k_pool, v_pool, k_exp, v_exp), their workspace and the opaque handle.
+    k_pool, v_pool [L][n_pages][Hkv][page][d] in dtype, int8 or float8_e4m3fn; k_exp, v_exp uint8 [L][n_pages][Hkv][page] (8-bit formats)."""
+
+    def __init__(self, L, n_pages, page, Hq, Hkv, d, dtype, format=PAGE_SAME, max_seqs=64, max_rows=4096, k_pool=None, v_pool=None, k_exp=None, v_exp=None,
+                 device=None, stream=None):
+        lib = load()
+        self.desc = PagesDesc(L, n_pages, page, Hq, Hkv, d, dtype, format, max_seqs, max_rows)
+        wsb = int(lib.reflex_pages_workspace_bytes(ctypes.byref(self.desc)))
+        if wsb == 0:
+            raise ReflexError(ERR_SHAPE, "invalid pages descriptor")
+        self.device = torch.device(device if device is not None else k_pool.device if k_pool is not None else "cuda:0")
+        kind = {PAGE_SAME: torch_dtype(dtype), PAGE_E4M3: torch.float8_e4m3fn, PAGE_INT8: torch.int8}[format]
+        shape = (L, n_pages, Hkv, page, d)
+
+        def lent(t, shape, kind, name):
+            if t is None:
+                return torch.zeros(shape, dtype=kind, device=self.device)
+            if tuple(t.shape) != tuple(shape) or t.dtype != kind or not t.is_contiguous() or t.device.type != self.device.type or t.device.index not in (None, self.device.index or 0):
+                raise ValueError(f"{name} must be dense {kind} {tuple(shape)} on {self.device}")
+            return t
+        self.k_pool, self.v_pool = lent(k_pool, shape, kind, "k_pool"), lent(v_pool, shape, kind, "v_pool")
+        if format == PAGE_SAME:
+            if k_exp is not None or v_exp is not None:
+                raise ValueError("pages in dtype have no exponents")
+            self.k_exp = self.v_exp = None
+        else:
+            self.k_exp, self.v_exp = lent(k_exp, shape[:-1], torch.uint8, "k_exp"), lent(v_exp, shape[:-1], torch.uint8, "v_exp")
+        self.workspace = torch.empty((wsb,), dtype=torch.uint8, device=self.device)
+        self.handle = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            _check(lib.reflex_pages_create(ctypes.byref(self.desc), _ptr(self.k_pool), _ptr(self.v_pool), _ptr(self.k_exp), _ptr(self.v_exp), _ptr(self.workspace),
+                                           _stream(stream), ctypes.byref(self.handle)))
+
+    def close(self):
+        if getattr(self, "handle", None) is not None and self.handle:
+            load().reflex_pages_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def reflex_pages_check_status(pages: Pages, stream=None):
+    with torch.cuda.device(pages.device):
+        _check(load().reflex_pages_check_status(pages.handle, _stream(stream)))
+
+
+def reflex_rotary_axes(x, y, pos, rotary: Rotary, inverse=False, stream=None):
+    """y <- x rotated; x, y [tokens][H][d] (tokens may lie further apart than their heads; y may be x), pos int32 [axes][tokens]. inverse: by
+    the opposite angles, which is the gradient."""
+    rc = _native().rotary_axes(x, y, pos, rotary.freq, rotary.axis, rotary.adjacent, int(inverse), stream)
+    if rc:
+        _check(rc)
+    return y
+
+
+def reflex_pages_write(pages: Pages, layer, batch: PageBatch, k, v, rotary: Optional[Rotary] = None, pos=None, stream=None):
+    """Keys and values of the new tokens, [tokens][Hkv][d] (tokens may lie further apart than their heads), into the pages; keys are rotated
+    first where a rotation is given."""
+    d = pages.desc
+    r = (None, None, 0) if rotary is None else (rotary.freq, rotary.axis, rotary.adjacent)
+    rc = _native().pages_write(_handle(pages), layer, batch.table, batch.cu, batch.length, k, v, *r, pos, stream, d.dtype, d.Hkv, d.d)
+    if rc:
+        _check(rc)
+
+
+def reflex_pages_read(pages: Pages, layer, batch: PageBatch, k_out, v_out, start=None, stream=None):
+    """Tokens [start[b], length[b]) of every sequence into k_out, v_out [B][layers][S_out][Hkv][d]: as many layers from `layer` on as the
+    outputs have. Rows behind a sequence's last token are left as they were."""
+    d = pages.desc
+    rc = _native().pages_read(_handle(pages), layer, batch.table, batch.length, start, k_out, v_out, stream, d.dtype, d.Hkv, d.d)
+    if rc:
+        _check(rc)
+    return k_out, v_out
+
+
+def reflex_pages_attention(pages: Pages, layer, batch: PageBatch, q, out, scale=0.0, causal=False, window=0, stream=None):
+    """q, out [tokens][Hq][d]: every new token's attention over its sequence's pages. Rows behind the last sequence are left as they were."""
+    d = pages.desc
+    rc = _native().pages_attention(_handle(pages), layer, batch.table, batch.cu, batch.length, q, out, scale, int(causal), window, stream, d.dtype, d.Hq, d.d)
+    if rc:
+        _check(rc)
+    return out
 
 
 # ---- Algorithm 1: overlap scheduling (host logic) ----

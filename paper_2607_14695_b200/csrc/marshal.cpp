@@ -2,6 +2,7 @@
 // the C ABI out (include/reflex.h). What bounds a small direct call is the host: the launch itself is some 3.3 us, and pulling
 // pointers, sizes and the stream out of the tensors in Python and through ctypes took another 2 to 3. No arithmetic, no state.
 #include <Python.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -291,9 +292,170 @@ PyObject *append_sliding(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- the paged prefix ----
+
+reflex_pages_t *pages(PyObject *o)
+{
+    if (o == Py_None) return nullptr;
+    void *p = PyLong_AsVoidPtr(o);
+    if (!p && PyErr_Occurred()) throw Bad();
+    return (reflex_pages_t *)p;
+}
+
+void want(bool ok, const char *what)
+{
+    if (ok) return;
+    PyErr_SetString(PyExc_ValueError, what);
+    throw Bad();
+}
+
+// The calls of the paged prefix run on the device of their tensors, whichever is current, and on that device's current stream unless one is
+// named. All tensors have to lie there.
+struct On {
+    c10::Device dev;
+    c10::OptionalDeviceGuard guard;
+    explicit On(PyObject *first) : dev(tensor(first).device())
+    {
+        want(dev.is_cuda(), "expected tensors on a CUDA device");
+        guard.reset_device(dev);
+    }
+    const at::Tensor &at_home(PyObject *o, const char *what) const
+    {
+        const at::Tensor &t = tensor(o);
+        if (t.device() != dev) {
+            PyErr_Format(PyExc_ValueError, "%s lies on another device than the call's first tensor", what);
+            throw Bad();
+        }
+        return t;
+    }
+    const int32_t *i32(PyObject *o, const char *what) const
+    {
+        if (o == Py_None) return nullptr;
+        const at::Tensor &t = at_home(o, what);
+        if (t.scalar_type() != at::kInt || !t.is_contiguous()) {
+            PyErr_Format(PyExc_ValueError, "%s must be contiguous int32", what);
+            throw Bad();
+        }
+        return t.const_data_ptr<int32_t>();
+    }
+    // rows [n][H][d] whose heads are dense: the distance of two tokens in elements
+    int64_t rows(PyObject *o, const char *what) const
+    {
+        const at::Tensor &t = at_home(o, what);
+        if (t.dim() != 3 || (t.size(2) > 1 && t.stride(2) != 1) || (t.size(1) > 1 && t.stride(1) != t.size(2))) {
+            PyErr_Format(PyExc_ValueError, "%s must be [tokens][heads][d] with dense heads", what);
+            throw Bad();
+        }
+        return t.size(0) > 1 ? t.stride(0) : t.size(1) * t.size(2);
+    }
+};
+
+int narrow(int64_t v) { want(v >= 0 && v <= 0x7fffffff, "a size above 2^31 - 1"); return (int)v; }
+
+reflex_page_batch batch(const On &on, PyObject *table, PyObject *cu, PyObject *len)
+{
+    reflex_page_batch q;
+    q.table = on.i32(table, "table"); q.cu = on.i32(cu, "cu"); q.len = on.i32(len, "length");
+    const at::Tensor &t = tensor(table);
+    want(t.dim() == 2, "table must be [B][max_pages]");
+    q.B = narrow(t.size(0)); q.max_pages = narrow(t.size(1));
+    want(tensor(len).dim() == 1 && tensor(len).size(0) == q.B, "length must be [B]");
+    want(cu == Py_None || (tensor(cu).dim() == 1 && tensor(cu).size(0) == (int64_t)q.B + 1), "cu must be [B + 1]");
+    return q;
+}
+
+// freq, axis, adjacent, pos of n tokens
+reflex_rotary rotation(const On &on, PyObject *freq, PyObject *axis, PyObject *adjacent, PyObject *pos, int64_t n)
+{
+    reflex_rotary r;
+    const at::Tensor &f = on.at_home(freq, "freq"), &a = on.at_home(axis, "axis"), &p = on.at_home(pos, "pos");
+    want(f.scalar_type() == at::kFloat && f.dim() == 1 && f.is_contiguous(), "freq must be a dense fp32 vector");
+    want(a.scalar_type() == at::kByte && a.dim() == 1 && a.is_contiguous() && a.size(0) == f.size(0), "axis must be a dense uint8 vector as long as freq");
+    want(p.dim() == 2 && p.size(1) == n, "pos must be [axes][tokens]");
+    on.i32(pos, "pos");
+    r.freq = f.const_data_ptr<float>(); r.axis = a.const_data_ptr<uint8_t>();
+    r.R = narrow(2 * f.size(0)); r.axes = narrow(p.size(0)); r.adjacent = integer(adjacent);
+    return r;
+}
+
+// x, y, pos, freq, axis, adjacent, inverse, stream
+PyObject *rotary_axes(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 8, [&]() -> PyObject * {
+        const On on(a[0]);
+        const int64_t ldx = on.rows(a[0], "x"), ldy = on.rows(a[1], "y");
+        const at::Tensor &x = tensor(a[0]), &y = tensor(a[1]);
+        want(x.sizes() == y.sizes() && x.scalar_type() == y.scalar_type(), "x and y must have one shape and type");
+        const int dt = dtype(a[0]), rows = narrow(x.size(0)), H = narrow(x.size(1)), d = narrow(x.size(2)), inv = integer(a[6]);
+        const reflex_rotary r = rotation(on, a[3], a[4], a[5], a[2], x.size(0));
+        const int32_t *pos = on.i32(a[2], "pos");
+        void *px = x.data_ptr(), *py = y.data_ptr(), *st = stream(a[7]);
+        return PyLong_FromLong(unlocked([&] { return reflex_rotary_axes(px, ldx, py, ldy, pos, &r, rows, H, d, inv, dt, st); }));
+    });
+}
+
+// handle, layer, table, cu, length, k, v, (freq, axis, adjacent, pos) or four None, stream, dtype, Hkv, d of the handle
+PyObject *pages_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 15, [&]() -> PyObject * {
+        const On on(a[5]);
+        reflex_pages_t *p = pages(a[0]);
+        const int layer = integer(a[1]);
+        const reflex_page_batch q = batch(on, a[2], a[3], a[4]);
+        const int64_t ldk = on.rows(a[5], "k"), ldv = on.rows(a[6], "v");
+        const at::Tensor &k = tensor(a[5]), &v = tensor(a[6]);
+        want(k.sizes() == v.sizes() && dtype(a[5]) == integer(a[12]) && dtype(a[6]) == integer(a[12]) && k.size(1) == integer(a[13]) && k.size(2) == integer(a[14]),
+             "k and v must be [tokens][Hkv][d] in the pages' dtype");
+        const int rows = narrow(k.size(0));
+        reflex_rotary r;
+        const bool rot = a[7] != Py_None;
+        if (rot) r = rotation(on, a[7], a[8], a[9], a[10], k.size(0));
+        const int32_t *pos = on.i32(a[10], "pos");
+        void *pk = k.data_ptr(), *pv = v.data_ptr(), *st = stream(a[11]);
+        return PyLong_FromLong(unlocked([&] { return reflex_pages_write(p, layer, &q, pk, ldk, pv, ldv, rows, rot ? &r : nullptr, pos, st); }));
+    });
+}
+
+// handle, layer, table, length, start or None, k_out, v_out, stream, dtype, Hkv, d of the handle
+PyObject *pages_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 11, [&]() -> PyObject * {
+        const On on(a[5]);
+        reflex_pages_t *p = pages(a[0]);
+        const int layer = integer(a[1]);
+        const reflex_page_batch q = batch(on, a[2], Py_None, a[3]);
+        const int32_t *start = on.i32(a[4], "start");
+        const at::Tensor &k = tensor(a[5]), &v = on.at_home(a[6], "v_out");
+        want(a[4] == Py_None || (tensor(a[4]).dim() == 1 && tensor(a[4]).size(0) == q.B), "start must be [B]");
+        want(k.dim() == 5 && k.sizes() == v.sizes() && k.is_contiguous() && v.is_contiguous() && k.size(0) == q.B && k.size(3) == integer(a[9]) && k.size(4) == integer(a[10]) &&
+             dtype(a[5]) == integer(a[8]) && dtype(a[6]) == integer(a[8]), "k_out and v_out must be dense [B][layers][S_out][Hkv][d] in the pages' dtype");
+        const int layers = narrow(k.size(1)), S = narrow(k.size(2));
+        void *pk = k.data_ptr(), *pv = v.data_ptr(), *st = stream(a[7]);
+        return PyLong_FromLong(unlocked([&] { return reflex_pages_read(p, layer, layers, &q, start, pk, pv, S, st); }));
+    });
+}
+
+// handle, layer, table, cu, length, q, out, scale, causal, window, stream, dtype, Hq, d of the handle
+PyObject *pages_attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return entry(n, 14, [&]() -> PyObject * {
+        const On on(a[5]);
+        reflex_pages_t *p = pages(a[0]);
+        const int layer = integer(a[1]);
+        const reflex_page_batch b = batch(on, a[2], a[3], a[4]);
+        const at::Tensor &q = tensor(a[5]), &o = on.at_home(a[6], "out");
+        want(q.dim() == 3 && q.sizes() == o.sizes() && q.is_contiguous() && o.is_contiguous() && q.size(1) == integer(a[12]) && q.size(2) == integer(a[13]) &&
+             dtype(a[5]) == integer(a[11]) && dtype(a[6]) == integer(a[11]), "q and out must be dense [tokens][Hq][d] in the pages' dtype");
+        const float scale = real(a[7]);
+        const int rows = narrow(q.size(0)), causal = integer(a[8]), window = integer(a[9]);
+        void *pq = q.data_ptr(), *po = o.data_ptr(), *st = stream(a[10]);
+        return PyLong_FromLong(unlocked([&] { return reflex_pages_attention(p, layer, &b, pq, po, rows, scale, causal, window, st); }));
+    });
+}
+
 #define M(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {M(adarmsnorm), M(adarmsnorm_gate), M(adarmsnorm_qkv), M(adarmsnorm_swiglu), M(linear_residual), M(partitioned_attention), M(flow_step),
-                         M(write_static), M(commit_static), M(append_sliding), {nullptr, nullptr, 0, nullptr}};
+                         M(write_static), M(commit_static), M(append_sliding), M(rotary_axes), M(pages_write), M(pages_read), M(pages_attention), {nullptr, nullptr, 0, nullptr}};
 #undef M
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

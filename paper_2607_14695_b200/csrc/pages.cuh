@@ -1,0 +1,197 @@
+// Shared by the kernels of the paged prefix (reflex_pages_*, reflex_rotary_axes): geometry, page lookup, 8-bit rows, rotation angles.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "reflex_internal.cuh"
+
+namespace reflex {
+
+// Pools and geometry of a handle, of one layer where a kernel works on one (the pointers then are the layer's).
+struct PageGeom {
+    void *k, *v;              // [L][n_pages][Hkv][P][d] in the pages' format
+    uint8_t *ke, *ve;         // [L][n_pages][Hkv][P], NULL for REFLEX_PAGE_SAME
+    uint32_t *status;
+    int n_pages, P, log_p, Hq, Hkv, d;
+};
+
+constexpr int kMaxSeqs = 1024;         // sequences of a call: cu fits the shared memory of the kernels that search it
+constexpr uint32_t kStatusBadPage = 0x40000000u;
+
+// What a page lookup of sequence b could not follow is reported once (the low bits name the sequence).
+__device__ __forceinline__ void report_bad_page(uint32_t *status, int b) { atomicCAS(status, 0u, kStatusBadPage | (uint32_t)b); }
+
+// page of positions [idx * P, (idx + 1) * P) of sequence b, -1 where the table does not give one of the pool's
+__device__ __forceinline__ int page_at(const reflex_page_batch &q, int n_pages, int b, int idx)
+{
+    if ((unsigned)idx >= (unsigned)q.max_pages) return -1;
+    const int id = q.table[(size_t)b * q.max_pages + idx];
+    return (unsigned)id < (unsigned)n_pages ? id : -1;
+}
+
+// first row of a (page, head) block of a layer, in rows of d elements
+__device__ __forceinline__ size_t page_row(const PageGeom &g, int page, int h) { return ((size_t)page * g.Hkv + h) << g.log_p; }
+
+// cu into shared memory (all threads of the block), the search of a row in it: the last b with cu[b] <= row, so that empty sequences
+// before it are passed over. Any contents give a b in [0, B).
+__device__ __forceinline__ void load_cu(const reflex_page_batch &q, int *cu_s)
+{
+    for (int i = threadIdx.x; i <= q.B; i += blockDim.x) cu_s[i] = q.cu[i];
+}
+__device__ __forceinline__ int find_seq(const int *cu_s, int B, int row)
+{
+    int lo = 0, hi = B;      // cu[lo] <= row < cu[hi], as far as cu is in order
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (cu_s[mid] <= row) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// ---- 8-bit rows ----
+
+template <int FMT> struct PageFormat;
+template <> struct PageFormat<REFLEX_PAGE_INT8> { static constexpr int exponent = 6; static constexpr uint32_t mantissa = 0x7E0000u; };   // 127 = 1.984375 * 2^6
+template <> struct PageFormat<REFLEX_PAGE_E4M3> { static constexpr int exponent = 8; static constexpr uint32_t mantissa = 0x600000u; };   // 448 = 1.75 * 2^8
+constexpr int kPageMinExponent = -100;
+
+// Exponent byte of a row whose largest magnitude has these bits (a pattern above infinity's is a NaN's): 255 unless finite.
+template <int FMT>
+__device__ __forceinline__ int row_exponent(uint32_t largest)
+{
+    if (largest >= 0x7f800000u) return 255;
+    largest = min(largest, 0x7f000000u);        // 2^127
+    const int e = (int)(largest >> 23) - 127 - PageFormat<FMT>::exponent + ((largest & 0x7fffffu) > PageFormat<FMT>::mantissa ? 1 : 0);
+    return max(e, kPageMinExponent) + 127;
+}
+
+// four numbers of a row as bytes, given 2^-e (exact: a power of two)
+template <int FMT>
+__device__ __forceinline__ uint32_t quantise4(const float *x, float inv)
+{
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = fminf(fmaxf(x[i], -0x1p127f), 0x1p127f) * inv;
+    if constexpr (FMT == REFLEX_PAGE_E4M3) {
+        const uint32_t a = __nv_cvt_float2_to_fp8x2(make_float2(f[0], f[1]), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t b = __nv_cvt_float2_to_fp8x2(make_float2(f[2], f[3]), __NV_SATFINITE, __NV_E4M3);
+        return a | (b << 16);
+    } else {
+        uint32_t w = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w |= ((uint32_t)__float2int_rn(f[i]) & 0xffu) << (8 * i);
+        return w;
+    }
+}
+
+__device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t bf16x2_sub(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+
+// Two bytes of an 8-bit row (byte I of w0 and byte J of w1) as the two bf16 of a register, unscaled and exact.
+//   int8: with the sign bit s and the seven bits u below it the byte is u - 128 s. 0x4300 | u is 128 + u in bf16 and 0x4300 | (byte & 0x80) is
+//   128 (1 + s): their difference is the byte.
+//   e4m3: sign, four bits of exponent and three of mantissa moved to where bf16 has them give the number times 2^(7 - 127), whether it is
+//   normal or not; the product with 2^120 is exact.
+template <int FMT, int I, int J>
+__device__ __forceinline__ uint32_t bytes_to_bf16x2(uint32_t w0, uint32_t w1)
+{
+    if constexpr (FMT == REFLEX_PAGE_INT8) {
+        const uint32_t x = __byte_perm(w0, w1, I | (I << 4) | ((J + 4) << 8) | ((J + 4) << 12));
+        return bf16x2_sub((x & 0x007f007fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u);
+    } else {
+        const uint32_t x = __byte_perm(w0, w1, (I << 4) | ((J + 4) << 12) | I | ((J + 4) << 8)) & 0xff00ff00u;
+        return bf16x2_mul((x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), 0x7b807b80u);
+    }
+}
+// 2^(e - 127) of an exponent byte: as a pair of bf16, and in fp32 (255: NaN)
+__device__ __forceinline__ uint32_t exponent_bf16x2(int e)
+{
+    const uint32_t one = e == 255 ? 0x7fc0u : e == 0 ? 0x0040u : (uint32_t)e << 7;
+    return one | (one << 16);
+}
+__device__ __forceinline__ float exponent_f32(int e) { return e == 255 ? __int_as_float(0x7fc00000) : e == 0 ? 0x1p-127f : __int_as_float(e << 23); }
+
+// ---- rotation angles ----
+// A pair's frequency in revolutions per position, modulo 1, as a 64-bit fraction: position times fraction, modulo 2^64, is the fraction of a
+// revolution that the position turns by, for any 32-bit position and with no rounding. Its upper 32 bits are a quarter of fp32's spacing near 1.
+struct TurnRate { uint32_t lo, hi; };
+__device__ __forceinline__ TurnRate turn_rate(float freq)
+{
+    // 1 / (2 pi) to twice the precision of a double
+    const double c0 = 0x1.45f306dc9c883p-3, c1 = -0x1.6b01ec5417056p-57;
+    const double f = (double)freq, r0 = f * c0, r1 = fma(f, c0, -r0) + f * c1;
+    const double whole = floor(r0), frac = r0 - whole;                     // exact
+    const unsigned long long u = __double2ull_rd(frac * 0x1p64) + (unsigned long long)__double2ll_rn(r1 * 0x1p64);
+    TurnRate t;
+    t.lo = (uint32_t)u;
+    t.hi = (uint32_t)(u >> 32);
+    return t;
+}
+__device__ __forceinline__ void turn(TurnRate t, int pos, float &sin_a, float &cos_a)
+{
+    const uint32_t p = (uint32_t)pos;
+    const uint32_t frac = __umulhi(p, t.lo) + p * t.hi - (pos < 0 ? t.lo : 0u);
+    sincospif((float)(int32_t)frac * 0x1p-31f, &sin_a, &cos_a);
+}
+
+// ---- 8 consecutive elements as fp32 ----
+__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *f)
+{
+    const uint4 u = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void load8(const float *p, float *f)
+{
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+        const float4 v = *reinterpret_cast<const float4 *>(p + i);
+        f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
+    }
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16 *p, const float *f)
+{
+    *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+}
+__device__ __forceinline__ void store8(float *p, const float *f)
+{
+    *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    *reinterpret_cast<float4 *>(p + 4) = make_float4(f[4], f[5], f[6], f[7]);
+}
+
+// ---- launchers ----
+struct PageRotation { reflex_rotary rot; const int32_t *pos; int inverse; };      // rot.R == 0: none
+
+cudaError_t launch_rotary_axes(const void *x, int64_t ldx, void *y, int64_t ldy, const PageRotation &r, int n, int H, int d, int dtype, cudaStream_t st);
+cudaError_t launch_page_write(const PageGeom &g, const reflex_page_batch &q, const void *k, int64_t ldk, const void *v, int64_t ldv, int n_rows,
+                              const PageRotation &r, int dtype, int format, cudaStream_t st);
+cudaError_t launch_page_read(const PageGeom &g, const reflex_page_batch &q, const int32_t *start, void *k_out, void *v_out, int n_layers, int S_out, int dtype,
+                             int format, cudaStream_t st);
+
+struct PageAttention {
+    PageGeom g;
+    reflex_page_batch q;
+    const void *qry;
+    void *out;
+    int n_rows, causal, window;
+    float scale;
+};
+cudaError_t launch_page_plain(const PageAttention &a, int dtype, int format, cudaStream_t st);
+
+}  // namespace reflex

@@ -1,0 +1,476 @@
+"""The paged prefix against its definitions in 64 bits: rotary positions with several axes, rows into 8-bit pages and back, attention of new
+tokens over pages."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2607_14695_b200 import binding as rb  # noqa: E402
+from paper_2607_14695_b200 import build as rbuild  # noqa: E402
+
+if torch.cuda.is_available():
+    rbuild.build()
+import pages_util as U  # noqa: E402
+from pages_util import DEV, HALF, Paged  # noqa: E402
+
+BF16, F32 = torch.bfloat16, torch.float32
+FORMATS = [rb.PAGE_SAME, rb.PAGE_E4M3, rb.PAGE_INT8]
+
+
+def _rot(R, axes, adjacent=False, base=10000.0):
+    i = torch.arange(R // 2)
+    return rb.Rotary((base ** (-2.0 * i / R)).float().to(DEV), (i % axes).to(torch.uint8).to(DEV), adjacent)
+
+
+# ---- rotary ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,H,d,R,axes,adjacent,inverse,spare", [
+    (1, 1, 32, 32, 1, False, False, 0), (1, 9, 256, 256, 3, False, False, 1), (7, 5, 128, 96, 3, True, True, 0), (301, 3, 64, 32, 2, False, True, 2),
+    (33, 10, 128, 128, 4, True, False, 1), (1000, 24, 64, 64, 8, False, False, 0), (5, 2, 1024, 1008, 3, False, False, 0), (129, 4, 48, 16, 3, True, False, 3)])
+def test_rotary(dtype, n, H, d, R, axes, adjacent, inverse, spare):
+    g = torch.Generator().manual_seed(n + d)
+    x = torch.randn(n, H + spare, d, generator=g).to(dtype)
+    pos = torch.randint(-4096, 1 << 20, (axes, n), generator=g, dtype=torch.int32)
+    pos[:, 0] = torch.tensor([2 ** 31 - 1, -2 ** 31, 0, 1, -1, 12345678, 7, 2])[:axes]
+    rot = _rot(R, axes, adjacent)
+    y = torch.full((n, H + spare, d), math.nan, dtype=dtype, device=DEV)
+    out = rb.reflex_rotary_axes(x.to(DEV)[:, :H], y[:, :H], pos.to(DEV), rot, inverse=inverse)
+    want = U.rotated(x[:, :H], pos, rot.freq.cpu(), rot.axis.cpu(), adjacent, inverse)
+    # sine and cosine to 2^-22 (two units in the last place of fp32 and the fraction's 2^-32 revolutions) and far positions' angles as exact here
+    # as 64 bits have them (2^31 * 2^-53), two products and a sum, one rounding at the end
+    size = torch.maximum(x[:, :H].double().abs().amax(-1, keepdim=True), want.abs())
+    assert ((out.cpu().double() - want).abs() <= HALF[dtype] * want.abs() + size * 2 * (2.0 ** -22 + 2 * 2.0 ** -24 + 2.0 ** -21)).all()
+    assert torch.isnan(y[:, H:]).all()
+
+
+def test_rotary_in_place_and_back():
+    x = torch.randn(77, 6, 128, device=DEV)
+    pos = torch.randint(0, 5000, (3, 77), dtype=torch.int32, device=DEV)
+    rot = _rot(128, 3)
+    apart = rb.reflex_rotary_axes(x, torch.empty_like(x), pos, rot)
+    y = x.clone()
+    assert rb.reflex_rotary_axes(y, y, pos, rot) is y and torch.equal(y, apart)
+    rb.reflex_rotary_axes(y, y, pos, rot, inverse=True)
+    assert (y - x).abs().max() <= 8 * 2.0 ** -22 * x.abs().max()
+
+
+def test_rotary_gradient():
+    """Inverse = the gradient, against differences in 64 bits of the definition."""
+    g = torch.Generator().manual_seed(3)
+    x, dy = torch.randn(4, 2, 32, generator=g), torch.randn(4, 2, 32, generator=g)
+    pos = torch.randint(0, 900, (3, 4), generator=g, dtype=torch.int32)
+    for adjacent in (False, True):
+        rot = _rot(16, 3, adjacent)
+        grad = rb.reflex_rotary_axes(dy.to(DEV), torch.empty(4, 2, 32, device=DEV), pos.to(DEV), rot, inverse=True).cpu().double()
+        loss = lambda t: (U.rotated(t, pos, rot.freq.cpu(), rot.axis.cpu(), adjacent) * dy.double()).sum()      # noqa: E731
+        for at in [(0, 0, 0), (1, 1, 9), (2, 0, 15), (3, 1, 31), (2, 1, 1)]:
+            h = torch.zeros(4, 2, 32, dtype=torch.float64)
+            h[at] = 0.5
+            assert abs(float(loss(x.double() + h) - loss(x.double() - h)) - float(grad[at])) <= 8 * 2.0 ** -22 * dy.abs().max()
+
+
+def test_rotary_nothing_and_unknown_axes():
+    rot = _rot(32, 5)
+    x = torch.randn(3, 2, 32, device=DEV)
+    pos = torch.randint(1, 99, (2, 3), dtype=torch.int32, device=DEV)       # axes 2, 3, 4 have no positions: those pairs stay
+    y = rb.reflex_rotary_axes(x, torch.empty_like(x), pos, rot)
+    stay = (rot.axis >= 2).repeat(2).cpu()
+    assert torch.equal(y.cpu()[..., stay], x.cpu()[..., stay]) and not torch.equal(y, x)
+    rb.reflex_rotary_axes(x[:0], x[:0], pos[:, :0].contiguous(), rot)
+
+
+# ---- rows into pages and back --------------------------------------------------------------------------------------------
+
+def _read(c, layers=1, layer=0, S=None, start=None):
+    S = max(1, max(c.lens)) if S is None else S
+    out = [torch.full((len(c.lens), layers, S, c.Hkv, c.d), -7.0, dtype=c.dtype, device=DEV) for _ in range(2)]
+    rb.reflex_pages_read(c.pages, layer, c.batch, out[0], out[1], start=None if start is None else torch.tensor(start, dtype=torch.int32, device=DEV))
+    return [o.cpu() for o in out]
+
+
+def _same(a, b):
+    return torch.equal(torch.isnan(a), torch.isnan(b)) and torch.equal(torch.nan_to_num(a.double()), torch.nan_to_num(b.double()))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("lens,page,Hkv,d", [([1], 16, 1, 32), ([17, 0, 64, 5], 16, 2, 64), ([130, 1, 127], 64, 1, 256), ([33, 200], 128, 3, 128), ([70] * 5, 32, 4, 256)])
+def test_write_and_read(fmt, dtype, lens, page, Hkv, d):
+    c = Paged(lens, lens, page, Hkv, Hkv, d, dtype, fmt, L=2)
+    c.poison()
+    before = [t.clone() for t in (c.pages.k_pool, c.pages.v_pool)]
+    c.write_all(layer=1)
+    assert torch.equal(before[0].view(torch.uint8)[0], c.pages.k_pool.view(torch.uint8)[0])            # the other layer is untouched
+    used = set(c.table[c.table >= 0].tolist())
+    free = [p for p in range(c.n_pages) if p not in used]
+    assert torch.equal(before[1].view(torch.uint8)[1, free], c.pages.v_pool.view(torch.uint8)[1, free])
+    for got, want in zip(_read(c, layer=1), (c.k[1], c.v[1])):
+        for b, n in enumerate(lens):
+            assert _same(got[b, 0, :n], want[b].to(dtype))                          # exact: one rounding, into the page
+            assert (got[b, 0, n:] == -7.0).all()
+    rb.reflex_pages_check_status(c.pages)
+
+
+@pytest.mark.parametrize("fmt", [rb.PAGE_E4M3, rb.PAGE_INT8])
+def test_rows_of_every_size(fmt):
+    """Zeros, the smallest and largest numbers, rows on the edge of an exponent, ties, infinities and NaN."""
+    top = U.TOP[fmt]
+    rows = [torch.zeros(32), torch.full((32,), 1e-44), torch.full((32,), 3.3e38), torch.linspace(-1, 1, 32) * 2.0 ** 127, torch.linspace(-top, top, 32),
+            torch.linspace(-top, top, 32) * 1.0001, torch.linspace(-1, 1, 32) * 2.0 ** -95, torch.arange(32) + 0.5, (torch.arange(32) + 0.5) * 4.0, torch.randn(32) * 1e30,
+            torch.full((32,), -0.0), torch.tensor([math.inf] + [1.0] * 31), torch.tensor([1.0] * 31 + [-math.inf]), torch.tensor([2.0] * 30 + [math.nan, 1.0])]
+    x = torch.stack(rows)[:, None].float()
+    c = Paged([len(rows)], [len(rows)], 16, 1, 1, 32, F32, fmt)
+    c.write_all(k=x, v=x.flip(0).contiguous())
+    k, v = _read(c)
+    want, exps = U.held(x, fmt)
+    assert _same(k[0, 0], want.float()) and _same(v[0, 0], want.flip(0).float())
+    table = c.table[0].tolist()
+    assert c.pages.k_exp[0, table[0], 0, :len(rows)].cpu().tolist() == exps[:, 0].tolist()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_write_rotates_keys(fmt, adjacent):
+    """New tokens behind old ones, uneven, some sequences idle, rows of a packed projection, padding behind the last row."""
+    lens, news, d, Hkv = [40, 16, 9, 70], [7, 0, 9, 33], 128, 2
+    c = Paged(lens, news, 32, Hkv, Hkv, d, BF16, fmt, spare_rows=5)
+    packed = c.normal(c.rows, 3 * Hkv, d)
+    pos = torch.randint(0, 3000, (3, c.rows), generator=c.g, dtype=torch.int32)
+    rot = _rot(96, 3, adjacent)
+    dev = packed.to(DEV)
+    c.poison()
+    rb.reflex_pages_write(c.pages, 0, c.batch, dev[:, :Hkv], dev[:, Hkv:2 * Hkv], rotary=rot, pos=pos.to(DEV))
+    start = [a - n for a, n in zip(lens, news)]
+    k, v = _read(c, S=max(news), start=start)
+    turned = U.rotated(packed[:, :Hkv], pos, rot.freq.cpu(), rot.axis.cpu(), adjacent)
+    for b, n in enumerate(news):
+        r = slice(int(c.cu[b]), int(c.cu[b]) + n)
+        assert _same(v[b, 0, :n], U.held(packed[r, Hkv:2 * Hkv], fmt)[0].to(BF16))
+        want = turned[r]
+        size = packed[r, :Hkv].double().abs().amax(-1, keepdim=True) * 1.5
+        # the rotation's own error, then one rounding: to bf16, to the row's integers (half a step: half of 2^e) or to e4m3 (2^-4, or half of 2^(e - 9))
+        if n == 0:
+            continue
+        slack = 2.0 ** -20 * size
+        if fmt == rb.PAGE_SAME:
+            lim = HALF[BF16] * want.abs() + slack
+        else:
+            step = torch.exp2(U.held(want, fmt)[1].double() - 127)[..., None]
+            lim = (0.5 * step if fmt == rb.PAGE_INT8 else torch.maximum(2.0 ** -4 * want.abs(), 2.0 ** -10 * step)) + slack
+        assert ((k[b, 0, :n].double() - want).abs() <= lim * 1.001).all()
+        assert (k[b, 0, n:] == -7.0).all()
+    rb.reflex_pages_check_status(c.pages)
+
+
+def test_read_layers_and_windows():
+    c = Paged([50, 3, 0, 64], [0] * 4, 16, 2, 2, 64, BF16, rb.PAGE_INT8, L=4)
+    for layer in range(4):
+        c.write_all(layer=layer)
+    k, v = _read(c, layers=3, layer=1, S=20, start=[37, -5, 0, 60])
+    for i, l in enumerate((1, 2, 3)):
+        for b, (lo, hi) in enumerate([(37, 50), (0, 3), (0, 0), (60, 64)]):
+            assert _same(k[b, i, :hi - lo], c.k[l][b][lo:hi].to(BF16)) and _same(v[b, i, :hi - lo], c.v[l][b][lo:hi].to(BF16))
+            assert (k[b, i, hi - lo:] == -7.0).all()
+    short = _read(c, layers=1, layer=3, S=10)                                      # tokens past S_out rows are left out
+    assert _same(short[0][3, 0], c.k[3][3][:10].to(BF16))
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------
+
+CASES = [
+    # lens, news, page, Hq, Hkv, d, causal, window
+    ([1], [1], 16, 1, 1, 64, True, 0),
+    ([37], [1], 16, 8, 1, 256, False, 0),
+    ([817, 64, 129], [1, 1, 1], 64, 8, 1, 256, True, 0),
+    ([300, 5, 0, 128, 77], [1, 1, 0, 0, 3], 32, 8, 2, 128, True, 0),
+    ([257, 200], [2, 9], 128, 14, 2, 128, True, 0),
+    ([100, 90], [5, 90], 16, 4, 4, 64, True, 0),
+    ([130, 260], [130, 100], 64, 4, 2, 128, True, 0),
+    ([400], [90], 64, 8, 1, 256, False, 0),
+    ([513, 30, 200], [140, 30, 1], 32, 8, 1, 256, True, 0),
+    ([300, 260], [70, 64], 128, 7, 1, 128, True, 100),
+    ([300, 260], [70, 64], 16, 8, 2, 64, False, 77),
+    ([600], [1], 64, 8, 1, 128, True, 33),
+    ([64, 64], [64, 64], 32, 16, 2, 256, True, 1),
+    ([3, 2], [5, 4], 16, 8, 1, 256, True, 0),             # more new tokens than tokens: the first ones see nothing
+    ([150], [40], 16, 2, 1, 32, True, 0),
+    ([140], [3], 16, 24, 1, 64, False, 0),
+]
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0]}-{c[1]}-p{c[2]}-{c[3]}x{c[4]}x{c[5]}-{'c' if c[6] else 'f'}{c[7]}".replace(" ", ""))
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention(case, fmt, dtype):
+    lens, news, page, Hq, Hkv, d, causal, window = case
+    if dtype == F32 and sum(news) * Hq * max(lens) > 400000:
+        pytest.skip("the plain kernel has smaller cases")
+    c = Paged(lens, news, page, Hq, Hkv, d, dtype, fmt, spare_rows=3, seed=len(lens) + d)
+    c.poison()
+    c.write_all()
+    q = c.normal(c.rows, Hq, d)
+    out = torch.full((c.rows, Hq, d), -7.0, dtype=dtype, device=DEV)
+    for _ in range(2):           # (a second call finds what the first has left in the workspace)
+        rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), out, causal=causal, window=window)
+        rb.reflex_pages_check_status(c.pages)
+        c.check(out, c.attend(q, causal=causal, window=window), str(case))
+        assert (out[int(c.cu[-1]):] == -7.0).all()           # rows behind the last sequence
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("news", [[1, 1], [40, 70]])
+def test_attention_logits_of_any_size(fmt, news):
+    """Wide logits (one key takes all), a scale of its own, and none at all (the mean of the values)."""
+    c = Paged([180, 97], news, 64, 8, 1, 128, BF16, fmt, seed=5)
+    c.write_all()
+    q = c.normal(c.rows, 8, 128, std=12.0)
+    out = torch.empty((c.rows, 8, 128), dtype=BF16, device=DEV)
+    for x, scale in ((q, 0.0), (q, 1.0), (q, 1e-3), (torch.zeros_like(q), 0.0)):
+        rb.reflex_pages_attention(c.pages, 0, c.batch, x.to(DEV), out, scale=scale, causal=True)
+        c.check(out, c.attend(x, causal=True, scale=scale or None), f"scale {scale}")
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("news", [[1, 1], [33, 60]])
+def test_attention_of_masked_and_unmasked_nan(fmt, news):
+    """A row that is not finite reaches the tokens that see it, and those only."""
+    lens, Hq, d = [200, 150], 8, 128
+    c = Paged(lens, news, 32, Hq, 1, d, BF16, fmt, seed=11)
+    k, v = c.normal(sum(lens), 1, d), c.normal(sum(lens), 1, d)
+    k[190, 0, 3] = math.nan                  # sequence 0, position 190
+    v[200 + 20, 0, 7] = math.inf             # sequence 1, position 20
+    c.write_all(k=k, v=v)
+    q = c.normal(c.rows, Hq, d)
+    out = torch.empty((c.rows, Hq, d), dtype=BF16, device=DEV)
+    rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), out, causal=True, window=100)
+    got = out.cpu()
+    sees = [[p - 100 < at <= p for p in range(n - m, n)] for n, m, at in zip(lens, news, (190, 20))]
+    for b in range(2):
+        for i, s in enumerate(sees[b]):
+            row = got[int(c.cu[b]) + i]
+            if b == 0:
+                assert torch.isfinite(row).all() == (not s), (b, i)
+            elif fmt != rb.PAGE_SAME:
+                assert torch.isfinite(row).all() == (not s), (b, i)
+
+
+@pytest.mark.parametrize("fmt", [rb.PAGE_SAME, rb.PAGE_INT8])
+@pytest.mark.parametrize("news", [[1, 1, 1], [30, 1, 80]])
+def test_pages_outside_the_pool(fmt, news):
+    """A bad table entry, or a length past the table: nothing is followed, the sequence reads NaN and is named; the others are right."""
+    lens = [100, 90, 200]
+    c = Paged(lens, news, 32, 8, 1, 128, BF16, fmt, seed=2)
+    c.write_all()
+    rb.reflex_pages_check_status(c.pages)
+    bad = c.table.clone()
+    bad[1, 1] = c.n_pages
+    batch = rb.PageBatch(bad.to(DEV), c.batch.cu, c.batch.length)
+    q = c.normal(c.rows, 8, 128)
+    out = torch.zeros((c.rows, 8, 128), dtype=BF16, device=DEV)
+    rb.reflex_pages_attention(c.pages, 0, batch, q.to(DEV), out)
+    r = slice(int(c.cu[1]), int(c.cu[2]))
+    assert torch.isnan(out[r]).all()
+    want = c.attend(q)
+    out[r] = want[0][r].to(DEV).to(BF16)
+    c.check(out, want)
+    with pytest.raises(rb.ReflexError) as e:
+        rb.reflex_pages_check_status(c.pages)
+    assert e.value.code == rb.ERR_STATE and "sequence 1" in str(e.value)
+
+
+def test_lengths_past_the_table():
+    c = Paged([64, 40], [2, 2], 32, 4, 4, 64, BF16, rb.PAGE_E4M3, seed=2)
+    c.write_all()
+    batch = rb.PageBatch(c.batch.table, c.batch.cu, torch.tensor([64, 70], dtype=torch.int32, device=DEV))
+    before = c.pages.k_pool.view(torch.uint8).clone()
+    rows = c.normal(4, 4, 64).to(DEV)
+    rb.reflex_pages_write(c.pages, 0, batch, rows, rows)
+    changed = (before != c.pages.k_pool.view(torch.uint8)).any(-1).nonzero()
+    assert set(changed[:, 1].tolist()) == {int(c.table[0, 1])}       # sequence 0's new tokens alone
+    out = torch.zeros((4, 4, 64), dtype=BF16, device=DEV)
+    rb.reflex_pages_attention(c.pages, 0, batch, rows, out)
+    assert torch.isnan(out[2:]).all() and torch.isfinite(out[:2]).all()
+    with pytest.raises(rb.ReflexError):
+        rb.reflex_pages_check_status(c.pages)
+
+
+def test_the_path_together():
+    """Four ticks of an incremental prefill, each frame rotated, written and attended to; the prefix goes to the action expert's static region and the
+    newest frame to its ring, and the expert's attention over them is what the pages stand for."""
+    L, B, Hq, Hkv, d, page, frame = 2, 2, 8, 1, 256, 32, 24
+    N, T, ticks = 48, 8, 4
+    seq = [[frame * (t + 1) - 3 * b * (t + 1) for t in range(ticks)] for b in range(B)]        # lengths after every tick
+    most = -(-frame * ticks // page)
+    pages = rb.Pages(L, B * most + 1, page, Hq, Hkv, d, rb.DTYPE_BF16, rb.PAGE_INT8, max_seqs=B, max_rows=B * frame)
+    table = torch.randperm(B * most + 1)[:B * most].to(torch.int32).view(B, most).to(DEV)
+    rot = _rot(d, 3)
+    g = torch.Generator().manual_seed(8)
+    keys = [[torch.zeros(0, Hkv, d, dtype=torch.float64) for _ in range(B)] for _ in range(L)]
+    for t in range(ticks):
+        new = [seq[b][t] - (seq[b][t - 1] if t else 0) for b in range(B)]
+        cu = torch.tensor([0] + torch.tensor(new).cumsum(0).tolist(), dtype=torch.int32, device=DEV)
+        batch = rb.PageBatch(table, cu, torch.tensor([s[t] for s in seq], dtype=torch.int32, device=DEV))
+        n = sum(new)
+        pos = torch.randint(0, 500, (3, n), generator=g, dtype=torch.int32)
+        for l in range(L):
+            qkv = torch.randn(n, Hq + 2 * Hkv, d, generator=g).to(BF16).to(DEV)
+            rb.reflex_pages_write(pages, l, batch, qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], rotary=rot, pos=pos.to(DEV))
+            q = rb.reflex_rotary_axes(qkv[:, :Hq], torch.empty((n, Hq, d), dtype=BF16, device=DEV), pos.to(DEV), rot)
+            out = rb.reflex_pages_attention(pages, l, batch, q, torch.empty_like(q), causal=False)
+            kv = [torch.zeros((B, 1, frame * ticks, Hkv, d), dtype=BF16, device=DEV) for _ in range(2)]
+            rb.reflex_pages_read(pages, l, batch, kv[0], kv[1])
+            for b in range(B):
+                k, v = [x[b, 0, :seq[b][t], 0].double().cpu() for x in kv]
+                r = slice(int(cu[b]), int(cu[b + 1]))
+                w = torch.softmax(torch.einsum("nhd,kd->nhk", q[r].double().cpu(), k) / 16, -1)
+                want, mass = torch.einsum("nhk,kd->nhd", w, v), torch.einsum("nhk,kd->nhd", w, v.abs())
+                assert ((out[r].double().cpu() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 1e-3) * 1.01 * mass).all()
+    rb.reflex_pages_check_status(pages)
+    S = [s[-2] for s in seq]
+    cache = rb.Cache(L, B, Hq, Hkv, d, frame * ticks, N, T, rb.DTYPE_BF16)
+    older = rb.PageBatch(table, None, torch.tensor(S, dtype=torch.int32, device=DEV))
+    ks, vs = [torch.zeros((B, L, max(S), Hkv, d), dtype=BF16, device=DEV) for _ in range(2)]
+    rb.reflex_pages_read(pages, 0, older, ks, vs)
+    rb.reflex_cache_init_static(cache, [0, 1], ks, vs, S=S)
+    m = min(new)
+    newest = rb.PageBatch(table, None, torch.tensor([s[-1] for s in seq], dtype=torch.int32, device=DEV))
+    kn, vn = [torch.zeros((B, L, m, Hkv, d), dtype=BF16, device=DEV) for _ in range(2)]
+    rb.reflex_pages_read(pages, 0, newest, kn, vn, start=torch.tensor([s[-1] - m for s in seq], dtype=torch.int32, device=DEV))
+    rb.reflex_cache_append_sliding(cache, [0, 1], kn, vn)
+    x = [torch.randn(B, T, h, d, generator=g).to(BF16).to(DEV) for h in (Hq, Hkv, Hkv)]
+    for l in range(L):
+        out = rb.reflex_partitioned_attention(cache, l, *x, torch.empty((B, T, Hq, d), dtype=BF16, device=DEV))
+        for b in range(B):
+            k = torch.cat([ks[b, l, :S[b], 0], kn[b, l, :, 0], x[1][b, :, 0]]).double()
+            v = torch.cat([vs[b, l, :S[b], 0], vn[b, l, :, 0], x[2][b, :, 0]]).double()
+            w = torch.softmax(torch.einsum("nhd,kd->nhk", x[0][b].double(), k) / 16, -1)
+            assert (out[b].double() - torch.einsum("nhk,kd->nhd", w, v)).abs().max() <= 2e-2
+
+
+# ---- as a program uses them ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("news", [[1, 1], [50, 31]])
+def test_captured_and_replayed(news):
+    """A graph of rotation, write, attention and read follows lengths, tables and inputs that change between replays, on a stream of its own."""
+    page, Hq, Hkv, d = 32, 8, 1, 128
+    lens = [[90, 70], [121, 64]]
+    c = Paged([128, 128], news, page, Hq, Hkv, d, BF16, rb.PAGE_E4M3)
+    c.write_all()
+    length = torch.tensor(lens[0], dtype=torch.int32, device=DEV)
+    batch = rb.PageBatch(c.batch.table, c.batch.cu, length)
+    rot = _rot(d, 2)
+    qkv = torch.randn(c.rows, Hq + 2 * Hkv, d, device=DEV).to(BF16)
+    pos = torch.randint(0, 400, (2, c.rows), dtype=torch.int32, device=DEV)
+    q, out = [torch.empty((c.rows, Hq, d), dtype=BF16, device=DEV) for _ in range(2)]
+    kv = [torch.zeros((2, 1, 128, Hkv, d), dtype=BF16, device=DEV) for _ in range(2)]
+
+    def step():
+        rb.reflex_rotary_axes(qkv[:, :Hq], q, pos, rot)
+        rb.reflex_pages_write(c.pages, 0, batch, qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:], rotary=rot, pos=pos)
+        rb.reflex_pages_attention(c.pages, 0, batch, q, out, causal=True)
+        rb.reflex_pages_read(c.pages, 0, batch, kv[0], kv[1])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    for lengths in lens:
+        length.copy_(torch.tensor(lengths, dtype=torch.int32))
+        qkv.copy_(torch.randn(qkv.shape, device=DEV))
+        graph.replay()
+        replayed = [t.clone() for t in (out, *kv)]
+        out.zero_()
+        step()
+        assert all(torch.equal(a, b) for a, b in zip(replayed, (out, *kv)))
+        c.lens = lengths
+        k, v = kv[0].cpu().double(), kv[1].cpu().double()
+        c.k[0], c.v[0] = [k[b, 0, :n] for b, n in enumerate(lengths)], [v[b, 0, :n] for b, n in enumerate(lengths)]
+        c.check(out, c.attend(q.cpu(), causal=True))
+    rb.reflex_pages_check_status(c.pages)
+
+
+def test_results_do_not_depend_on_the_order_of_blocks():
+    c = Paged([700, 300, 431], [1, 90, 33], 64, 8, 1, 256, BF16, rb.PAGE_INT8)
+    c.write_all()
+    q = c.normal(c.rows, 8, 256).to(DEV)
+    first = rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.empty_like(q), causal=True).clone()
+    for _ in range(5):
+        assert torch.equal(first, rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.empty_like(q), causal=True))
+
+
+def test_two_handles_at_once_share_pools():
+    c = Paged([500, 380], [40, 20], 64, 8, 1, 128, BF16, rb.PAGE_E4M3)
+    c.write_all()
+    p = c.pages
+    other = rb.Pages(1, c.n_pages, 64, 8, 1, 128, rb.DTYPE_BF16, rb.PAGE_E4M3, max_seqs=2, max_rows=60, k_pool=p.k_pool, v_pool=p.v_pool, k_exp=p.k_exp, v_exp=p.v_exp)
+    q = [c.normal(c.rows, 8, 128).to(DEV) for _ in range(2)]
+    want = [rb.reflex_pages_attention(p, 0, c.batch, x, torch.empty_like(x)).clone() for x in q]
+    outs, streams = [torch.empty_like(x) for x in q], [torch.cuda.Stream() for _ in q]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for pages, x, o, s in zip((p, other), q, outs, streams):
+            rb.reflex_pages_attention(pages, 0, c.batch, x, o, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, outs))
+
+
+def test_rows_far_into_a_pool():
+    """Rows whose byte offsets pass 2^32 in the pool."""
+    page, d = 128, 256
+    n_pages = (5 << 30) // (page * d)                                    # 5 GB of one-byte rows
+    pages = rb.Pages(1, n_pages, page, 8, 1, d, rb.DTYPE_BF16, rb.PAGE_INT8, max_seqs=1, max_rows=300)
+    table = torch.tensor([[n_pages - 1, 0, n_pages - 2]], dtype=torch.int32, device=DEV)
+    n = 300
+    k, v = [torch.randn(n, 1, d, device=DEV).to(BF16) for _ in range(2)]
+    length = torch.tensor([n], dtype=torch.int32, device=DEV)
+    for new in (1, n):
+        batch = rb.PageBatch(table, torch.tensor([0, new], dtype=torch.int32, device=DEV), length)
+        if new == 1:
+            rb.reflex_pages_write(pages, 0, rb.PageBatch(table, torch.tensor([0, n], dtype=torch.int32, device=DEV), length), k, v)
+            got = [torch.zeros((1, 1, n, 1, d), dtype=BF16, device=DEV) for _ in range(2)]
+            rb.reflex_pages_read(pages, 0, batch, got[0], got[1])
+            assert torch.equal(got[0][0, 0].cpu(), U.held(k.cpu(), rb.PAGE_INT8)[0].to(BF16)) and torch.equal(got[1][0, 0].cpu(), U.held(v.cpu(), rb.PAGE_INT8)[0].to(BF16))
+        q = torch.randn(new, 8, d, device=DEV).to(BF16)
+        out = rb.reflex_pages_attention(pages, 0, batch, q, torch.empty_like(q))
+        w = torch.softmax(torch.einsum("nhd,kd->nhk", q.double(), got[0][0, 0, :, 0].double()) / 16, -1)
+        want, mass = [torch.einsum("nhk,kd->nhd", w, x) for x in (got[1][0, 0, :, 0].double(), got[1][0, 0, :, 0].double().abs())]
+        assert ((out.double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 1e-3) * 1.01 * mass).all()
+    rb.reflex_pages_check_status(pages)
+
+
+def test_refusals_of_the_binding():
+    c = Paged([64], [4], 16, 8, 2, 64, BF16, rb.PAGE_INT8)
+    k, q = torch.zeros(4, 2, 64, dtype=BF16, device=DEV), torch.zeros(4, 8, 64, dtype=BF16, device=DEV)
+    out = torch.zeros((1, 1, 64, 2, 64), dtype=BF16, device=DEV)
+    write = lambda *a, **kw: rb.reflex_pages_write(c.pages, 0, c.batch, *a, **kw)      # noqa: E731
+    for bad in (lambda: write(k.float(), k), lambda: write(k, k[:3]), lambda: write(k.cpu(), k), lambda: write(k.transpose(0, 1), k),
+                lambda: write(k, k.cpu()), lambda: write(q, q),
+                lambda: write(k, k, rotary=_rot(64, 1), pos=torch.zeros((1, 3), dtype=torch.int32, device=DEV)),
+                lambda: write(k, k, rotary=_rot(64, 1), pos=torch.zeros((1, 4), dtype=torch.int64, device=DEV)),
+                lambda: rb.reflex_pages_attention(c.pages, 0, c.batch, q, q[:3].clone()), lambda: rb.reflex_pages_attention(c.pages, 0, c.batch, q.float(), q.float()),
+                lambda: rb.reflex_pages_attention(c.pages, 0, c.batch, k, k.clone()),
+                lambda: rb.reflex_pages_attention(c.pages, 0, rb.PageBatch(c.batch.table, c.batch.cu[:1], c.batch.length), q, q.clone()),
+                lambda: rb.reflex_pages_attention(c.pages, 0, rb.PageBatch(c.batch.table.long(), c.batch.cu, c.batch.length), q, q.clone()),
+                lambda: rb.reflex_pages_read(c.pages, 0, c.batch, out, out.float()), lambda: rb.reflex_pages_read(c.pages, 0, c.batch, out[..., :32], out[..., :32])):
+        with pytest.raises((ValueError, TypeError)):
+            bad()
+    for bad, code in ((lambda: rb.reflex_pages_attention(c.pages, 1, c.batch, q, q.clone()), rb.ERR_INVALID_ARG),
+                      (lambda: rb.reflex_pages_attention(c.pages, 0, c.batch, q, q), rb.ERR_INVALID_ARG),
+                      (lambda: rb.reflex_pages_attention(c.pages, 0, c.batch, torch.cat([q, q]), torch.cat([q, q])), rb.ERR_SHAPE),
+                      (lambda: rb.reflex_pages_attention(c.pages, 0, c.batch, q, q.clone(), window=-1), rb.ERR_INVALID_ARG),
+                      (lambda: write(k, k, pos=torch.zeros((1, 4), dtype=torch.int32, device=DEV)), rb.ERR_INVALID_ARG),
+                      (lambda: write(k, k, rotary=_rot(128, 1), pos=torch.zeros((1, 4), dtype=torch.int32, device=DEV)), rb.ERR_SHAPE),
+                      (lambda: rb.reflex_pages_read(c.pages, 0, c.batch, torch.cat([out, out], 1), torch.cat([out, out], 1)), rb.ERR_INVALID_ARG)):
+        with pytest.raises(rb.ReflexError) as e:
+            bad()
+        assert e.value.code == code
+    with pytest.raises(ValueError):
+        rb.Pages(1, 4, 16, 8, 2, 64, rb.DTYPE_BF16, rb.PAGE_INT8, k_pool=torch.zeros(1, 4, 2, 16, 64, dtype=torch.int8, device=DEV)[..., :32])
