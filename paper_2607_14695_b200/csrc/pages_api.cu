@@ -2,7 +2,7 @@
 #include <cstring>
 #include <new>
 
-#include "pages.cuh"
+#include "page_attention.cuh"
 
 using namespace reflex;
 
@@ -33,6 +33,21 @@ bool desc_ok(const reflex_pages_desc *d)
 
 size_t rows_of(const reflex_pages_desc &d) { return (size_t)d.n_pages * d.Hkv * d.page; }
 size_t row_bytes(const reflex_pages_desc &d) { return (size_t)d.d * (d.format == REFLEX_PAGE_SAME ? elem_size(d.dtype) : 1); }
+
+// Layout of the workspace: status word, then the partial results of split units.
+struct PagesLayout { size_t meta, ml, o, bytes; };
+size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+PagesLayout pages_layout(const reflex_pages_desc &d)
+{
+    constexpr size_t ctas = 2 * 256;            // (more than any device has SMs, twice)
+    constexpr size_t rows = 16;
+    PagesLayout w;
+    w.meta = 256;
+    w.ml = w.meta + up256(ctas * sizeof(int4));
+    w.o = w.ml + up256(2 * ctas * rows * sizeof(float2));
+    w.bytes = w.o + up256(2 * ctas * rows * (size_t)d.d * sizeof(float));
+    return w;
+}
 
 PageGeom geometry(const reflex_pages &p, int layer)
 {
@@ -105,7 +120,7 @@ int reflex_rotary_axes(const void *x, int64_t ldx, void *y, int64_t ldy, const i
 
 size_t reflex_pages_pool_bytes(const reflex_pages_desc *d) { return desc_ok(d) ? (size_t)d->L * rows_of(*d) * row_bytes(*d) : 0; }
 size_t reflex_pages_exp_bytes(const reflex_pages_desc *d) { return desc_ok(d) && d->format != REFLEX_PAGE_SAME ? (size_t)d->L * rows_of(*d) : 0; }
-size_t reflex_pages_workspace_bytes(const reflex_pages_desc *d) { return desc_ok(d) ? 256 : 0; }
+size_t reflex_pages_workspace_bytes(const reflex_pages_desc *d) { return desc_ok(d) ? pages_layout(*d).bytes : 0; }
 
 int reflex_pages_create(const reflex_pages_desc *desc, void *k_pool, void *v_pool, void *k_exp, void *v_exp, void *workspace, void *stream,
                         reflex_pages_t **out)
@@ -212,7 +227,21 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     a.qry = q; a.out = out;
     a.n_rows = n_rows; a.causal = causal; a.window = window;
     a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)d.d);
-    const cudaError_t e = launch_page_plain(a, d.dtype, d.format, (cudaStream_t)stream);
+    const int G = d.Hq / d.Hkv;
+    const long long per_seq = ((long long)n_rows * G + batch->B - 1) / batch->B;           // (token, head) rows of a sequence and KV head
+    const int token_rows = page_token_rows(d.dtype, d.format, d.d, per_seq > 1 << 20 ? 1 << 20 : (int)per_seq);
+    cudaError_t e;
+    if (token_rows) {
+        const PagesLayout w = pages_layout(d);
+        PagePartials part;
+        part.o = (float *)(p->ws + w.o); part.ml = (float2 *)(p->ws + w.ml); part.meta = (int4 *)(p->ws + w.meta);
+        part.rows = token_rows;
+        part.scale_log2 = a.scale * 1.4426950408889634f;
+        const int ctas = page_token_ctas(p->sm_count) < 512 ? page_token_ctas(p->sm_count) : 512;
+        e = launch_page_token(a, part, d.format, token_rows, ctas, (cudaStream_t)stream);
+    } else {
+        e = launch_page_plain(a, d.dtype, d.format, (cudaStream_t)stream);
+    }
     return e == cudaSuccess ? REFLEX_OK : fail_cuda(e, "page attention launch");
 }
 
