@@ -739,6 +739,14 @@ int tc2_active_clusters(int d, int cluster_ctas)
 }  // namespace
 
 // rank-2 map over a row-major bf16 matrix [rows][inner], box = box_rows x 64 elements, 128-byte swizzle (cached like the others)
+bool encode_map_bf16(CUtensorMap *out, const void *ptr, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box)
+{
+    EncodeTiledFn fn = encode_fn();
+    const cuuint32_t es[5] = {1, 1, 1, 1, 1};
+    return fn && fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool tensor_map_2d_bf16(CUtensorMap *out, const void *ptr, int inner, int rows, int box_rows)
 {
     return cache().get(out, ptr, 3, inner, rows, box_rows, 0, [](CUtensorMap *m, const void *p_, int inner_, int rows_, int box_rows_, int) -> bool {

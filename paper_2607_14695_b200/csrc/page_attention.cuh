@@ -30,23 +30,169 @@ __device__ __forceinline__ PageRange page_range(const PageSeq &s, const PageAtte
     return r;
 }
 
-// CTA c of nc works on [page_share(c), page_share(c + 1)) of a line of `total` blocks
+// ---- the line of work ----
+// A unit is a tile of `rows` consecutive (token, head of the group) rows of a sequence and a KV head; it costs what SPAN says of its tile, in blocks of
+// keys, and one at least (rows that see nothing have to be written too). Units stand in a line by sequence, tile and KV head, and
+// CTA c of nc works on blocks [page_share(c), page_share(c + 1)) of it, whatever the lengths are.
 __host__ __device__ inline long long page_share(long long c, long long total, int nc) { return c * total / nc; }
 
-// Partial results. A CTA (or pair) leaves at most two: slot 2c of the unit that it entered in the middle, slot 2c + 1 of the unit that it
-// began and did not finish. meta[c] of the latter: {first row of the sequence, first (token, head) row of the tile, rows | KV head << 16, last CTA on the unit},
-// -1 first where there is none.
+// SPAN: struct with .count (blocks) from (sequence, tile). All functions: whole warps, every lane gets the same result.
+template <typename SPAN>
+struct PageLine {
+    const PageAttention &p;
+    SPAN span;
+    int rows, G;
+
+    __device__ __forceinline__ int tiles(const PageSeq &s) const { return (int)(((long long)s.n * G + rows - 1) / rows); }
+    // blocks of a sequence's units. (With few sequences several lanes share one: `width` of them, this one is number `sub`.)
+    __device__ __forceinline__ long long seq_cost(const PageSeq &s, int sub, int width, int &longest) const
+    {
+        long long cost = 0;
+        const int n = tiles(s);
+        for (int t = sub; t < n; t += width) {
+            const int c = max(1, span(s, t).count);
+            cost += c;
+            longest = max(longest, c);
+        }
+        for (int o = 1; o < width; o <<= 1) cost += __shfl_xor_sync(0xffffffffu, cost, o);
+        return cost * p.g.Hkv;
+    }
+    __device__ __forceinline__ int width() const
+    {
+        int w = 32;
+        while (w > 1 && p.q.B * w > 32) w >>= 1;
+        return w;
+    }
+    // of sequences b0 .. b0 + 31 / width: the cost of this lane's, 0 behind the last one
+    __device__ __forceinline__ long long lane_cost(int b0, int w, int lane, int &longest) const
+    {
+        PageSeq s = {0, 0, 0, 0};
+        if (b0 + lane / w < p.q.B) s = page_seq(p, b0 + lane / w);
+        return seq_cost(s, lane % w, w, longest);
+    }
+    __device__ __forceinline__ long long total(int lane, int &longest) const
+    {
+        const int w = width();
+        long long sum = 0;
+        longest = 1;
+        for (int b0 = 0; b0 < p.q.B; b0 += 32 / w) {
+            const long long c = lane_cost(b0, w, lane, longest);
+            sum += lane % w == 0 ? c : 0;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        longest = __reduce_max_sync(0xffffffffu, longest);
+        return sum;
+    }
+
+    // ---- a place in the line: unit (s, tile, h) begins at block `at` ----
+    struct Place {
+        PageSeq s;
+        int tile, h, cost;
+        long long at;
+        decltype(span(PageSeq(), 0)) sp;
+    };
+    __device__ __forceinline__ void settle(Place &u) const { u.sp = span(u.s, u.tile); u.cost = max(1, u.sp.count); }
+    // the unit that block x (< total) belongs to
+    __device__ __forceinline__ Place find(long long x, int lane) const
+    {
+        Place u;
+        const int w = width();
+        int unused = 0;
+        u.at = 0;
+        int b = 0;
+        for (int b0 = 0; b0 < p.q.B; b0 += 32 / w) {
+            const long long c = lane_cost(b0, w, lane, unused);
+            long long incl = lane % w == 0 ? c : 0;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += y;
+            }
+            const uint32_t past = __ballot_sync(0xffffffffu, u.at + incl > x);
+            if (past) {
+                const int src = __ffs(past) - 1;          // (the first lane of its sequence's)
+                b = b0 + src / w;
+                u.at += __shfl_sync(0xffffffffu, incl - c, src);
+                break;
+            }
+            u.at += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        u.s = page_seq(p, b);
+        const int n = tiles(u.s);
+        u.tile = 0;
+        for (int t0 = 0; t0 < n; t0 += 32) {
+            const long long c = t0 + lane < n ? (long long)max(1, span(u.s, t0 + lane).count) * p.g.Hkv : 0;
+            long long incl = c;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += y;
+            }
+            const uint32_t past = __ballot_sync(0xffffffffu, u.at + incl > x);
+            if (past) {
+                const int src = __ffs(past) - 1;
+                u.tile = t0 + src;
+                u.at += __shfl_sync(0xffffffffu, incl - c, src);
+                break;
+            }
+            u.at += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        settle(u);
+        u.h = min((int)((x - u.at) / u.cost), p.g.Hkv - 1);
+        u.at += (long long)u.h * u.cost;
+        return u;
+    }
+    // the unit behind u (callable by single lanes); behind the last one u.s.b is B
+    __device__ __forceinline__ void next(Place &u) const
+    {
+        u.at += u.cost;
+        if (++u.h < p.g.Hkv) return;
+        u.h = 0;
+        if (++u.tile >= tiles(u.s)) {
+            u.tile = 0;
+            do {
+                if (++u.s.b >= p.q.B) return;
+                u.s = page_seq(p, u.s.b);
+            } while (u.s.n == 0);
+        }
+        settle(u);
+    }
+};
+
+// ---- partial results ----
+// A CTA (or pair) leaves at most two: slot 2c of the unit that it entered in the middle, slot 2c + 1 of the unit that it began and did not
+// finish; the latter's entry in `meta` says what the unit is and which CTA is the last on it.
+// (first: first (token, head) row of the tile, which lies in row 0 of the slot; rows from `half` on lie from row 128 on; b = -1: none)
+struct PageSplit { int b, row0, first, rows, h, last, half, unused; };
 struct PagePartials {
-    float *o;              // [2 CTAs][rows][d]
+    float *o;              // [2 CTAs][d / 8][rows][8], unnormalised
     float2 *ml;            // [2 CTAs][rows]: maximum in log2 units, sum
-    int4 *meta;            // [CTAs]
+    PageSplit *meta;       // [CTAs]
+    // Sequences (a byte each) whose rows page_merge_kernel computes again one by one, since what lies at a key that some rows of a
+    // tile see and others do not was not finite, and 0 times it is NaN on the tensor cores; and the blocks of that kernel that are done with them.
+    uint8_t *careful;
+    uint32_t *careful_done;
     int rows;              // rows of a slot
     float scale_log2;
 };
+__device__ __forceinline__ float *partial8(const PagePartials &part, size_t slot, int d, int r, int c0) { return part.o + ((slot * (size_t)(d >> 3) + (size_t)(c0 >> 3)) * part.rows + r) * 8; }
+// the last CTA whose share reaches block `x` of the line
+__device__ __forceinline__ int page_owner(long long x, long long total, int nc)
+{
+    int c = (int)(x * nc / total);
+    while (c > 0 && page_share(c, total, nc) > x) --c;
+    while (c + 1 < nc && page_share(c + 1, total, nc) <= x) ++c;
+    return c;
+}
 
 int page_token_ctas(int sm_count);
-int page_token_rows(int dtype, int format, int d, int rows);
+int page_token_rows(int dtype, int format, int d, int G, int rows);
 cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int ctas, cudaStream_t st);
-cudaError_t launch_page_merge(const PageAttention &a, const PagePartials &part, int ctas, cudaStream_t st);
+bool page_chunk_takes(int dtype, int G, int d);
+cudaError_t launch_page_widen(const PageAttention &a, void *k_wide, void *v_wide, int format, int sm_count, cudaStream_t st);
+// k, v: one layer's pages in bf16
+cudaError_t launch_page_chunk(const PageAttention &a, const PagePartials &part, const void *k, const void *v, int pairs, cudaStream_t st);
+cudaError_t launch_page_merge(const PageAttention &a, const PagePartials &part, int ctas, int format, int sm_count, cudaStream_t st);
 
 }  // namespace reflex

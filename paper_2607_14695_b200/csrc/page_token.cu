@@ -67,17 +67,22 @@ template <int FMT, int HD, int NT> struct Tok {
     static constexpr uint32_t SMEM = OFF_ML + kTokWarps * ROWS * 8;
 };
 
-// cost of a sequence's units, in blocks of keys: what a row tile needs, one at least (an empty unit still has rows to write)
-struct TokSpan { int lo, hi, blocks; };
-__device__ __forceinline__ TokSpan tok_span(const PageSeq &s, const PageAttention &p, int G, int rows, int rt)
-{
-    const PageRange r = page_range(s, p, rt * rows / G, min(s.n * G, (rt + 1) * rows) > 0 ? (min(s.n * G, (rt + 1) * rows) - 1) / G : 0);
-    TokSpan t;
-    t.lo = r.lo & ~15;
-    t.hi = r.hi;
-    t.blocks = t.hi > t.lo ? (t.hi - t.lo + kTokBlock - 1) / kTokBlock : 0;
-    return t;
-}
+// the blocks of keys that a tile of ROWS rows needs
+struct TokSpan { int lo, hi, count; };
+template <int ROWS>
+struct TokSpanOf {
+    const PageAttention &p;
+    int G;
+    __device__ __forceinline__ TokSpan operator()(const PageSeq &s, int tile) const
+    {
+        const PageRange r = page_range(s, p, tile * ROWS / G, (min(s.n * G, (tile + 1) * ROWS) - 1) / G);
+        TokSpan t;
+        t.lo = r.lo & ~15;
+        t.hi = r.hi;
+        t.count = t.hi > t.lo ? (t.hi - t.lo + kTokBlock - 1) / kTokBlock : 0;
+        return t;
+    }
+};
 
 template <int FMT, int HD, int NT>
 __global__ void __launch_bounds__(32 * kTokWarps, 2)
@@ -94,72 +99,25 @@ page_token_kernel(const PageAttention p, const PagePartials part)
     const int G = g.Hq / g.Hkv;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // the line of work: total and longest unit, then this CTA's share and the sequence it starts in (every warp for itself)
-    auto seq_cost = [&](const PageSeq &s, int &longest) -> long long {
-        long long cost = 0;
-        const int tiles = (s.n * G + ROWS - 1) / ROWS;
-        for (int rt = 0; rt < tiles; ++rt) {
-            const int blocks = tok_span(s, p, G, ROWS, rt).blocks;
-            cost += max(1, blocks);
-            longest = max(longest, blocks);
-        }
-        return cost * g.Hkv;
-    };
-    long long total = 0;
-    int longest = 1;
-    for (int b0 = 0; b0 < p.q.B; b0 += 32) {
-        long long c = b0 + lane < p.q.B ? seq_cost(page_seq(p, b0 + lane), longest) : 0;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) c += __shfl_xor_sync(0xffffffffu, c, o);
-        total += c;
-    }
-    longest = __reduce_max_sync(0xffffffffu, longest);
+    const TokSpanOf<ROWS> span_of{p, G};
+    const PageLine<TokSpanOf<ROWS>> line{p, span_of, ROWS, G};
+    int longest;
+    const long long total = line.total(lane, longest);
     // No more CTAs than leave each the square root of a tenth of the longest unit: a partial costs the merge a tenth of what a block costs here.
     const int least = max(1, (int)sqrtf((float)longest * 0.1f));
     const int nc = (int)min((long long)gridDim.x, (total + least - 1) / least);
     const int cta = blockIdx.x;
-    if (threadIdx.x == 0) part.meta[cta] = make_int4(-1, 0, 0, 0);
+    if (threadIdx.x == 0) part.meta[cta].b = -1;
     if (cta >= nc) return;
     const long long x0 = page_share(cta, total, nc), x1 = page_share(cta + 1, total, nc);
-    int b = 0, longest_unused = 0;
-    long long before = 0;           // cost of the sequences before b
-    for (int b0 = 0; b0 < p.q.B; b0 += 32) {
-        const long long c = b0 + lane < p.q.B ? seq_cost(page_seq(p, b0 + lane), longest_unused) : 0;
-        long long incl = c;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += y;
-        }
-        const uint32_t past = __ballot_sync(0xffffffffu, before + incl > x0);
-        if (past) {
-            const int src = __ffs(past) - 1;
-            b = b0 + src;
-            before += __shfl_sync(0xffffffffu, incl - c, src);
-            break;
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    PageSeq s = page_seq(p, b);
-    int rt = 0, h = 0;
-    long long at = before;          // where the unit (b, rt, h) begins
-    TokSpan span = tok_span(s, p, G, ROWS, 0);
-    auto next_unit = [&] {
-        at += max(1, span.blocks);
-        if (++h < g.Hkv) return;
-        h = 0;
-        if (++rt * ROWS >= s.n * G) {
-            rt = 0;
-            do { if (++b >= p.q.B) return; s = page_seq(p, b); } while (s.n == 0);
-        }
-        span = tok_span(s, p, G, ROWS, rt);
-    };
-    while (at + max(1, span.blocks) <= x0) next_unit();
+    auto u = line.find(x0, lane);
 
     for (long long x = x0; x < x1;) {
-        const int cost = max(1, span.blocks);
-        const int k0 = (int)(x - at), k1 = (int)min((long long)cost, x1 - at);
-        const int kend = min(k1, span.blocks);
+        const PageSeq s = u.s;
+        const TokSpan span = u.sp;
+        const int rt = u.tile, h = u.h, b = s.b;
+        const int k0 = (int)(x - u.at), k1 = (int)min((long long)u.cost, x1 - u.at);
+        const int kend = min(k1, span.count);
         // ---- Q of the unit's rows, in the order of K's pieces ----
         __syncthreads();             // (the last unit's results and Q have been read)
         for (int i = threadIdx.x; i < C::STEPS * NT * 32; i += 32 * kTokWarps) {
@@ -434,7 +392,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                 }
         }
         __syncthreads();
-        const bool starts = k0 == 0, ends = k1 == cost;
+        const bool starts = k0 == 0, ends = k1 == u.cost;
         const int slot = 2 * cta + (starts ? 1 : 0);
         for (int i = threadIdx.x; i < ROWS * (HD / 8); i += 32 * kTokWarps) {
             const int r = i / (HD / 8), c0 = i % (HD / 8) * 8;
@@ -461,20 +419,16 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                 for (int e = 0; e < 8; ++e) acc[e] *= inv;
                 store8((__nv_bfloat16 *)p.out + ((size_t)(s.row0 + rr / G) * g.Hq + h * G + rr % G) * HD + c0, acc);
             } else {
-                store8(part.o + ((size_t)slot * part.rows + r) * HD + c0, acc);
+                store8(partial8(part, slot, HD, r, c0), acc);
                 if (c0 == 0) part.ml[(size_t)slot * part.rows + r] = make_float2(all, sum);
             }
         }
         if (starts && !ends && threadIdx.x == 0) {
-            // who else works on this unit: the CTAs whose shares reach to its last block
-            const long long last = at + cost - 1;
-            int c_end = (int)((last * nc) / total);
-            while (page_share(c_end, total, nc) > last) --c_end;
-            while (page_share(c_end + 1, total, nc) <= last) ++c_end;
-            part.meta[cta] = make_int4(s.row0, rt * ROWS, min(ROWS, s.n * G - rt * ROWS) | (h << 16), c_end);
+            PageSplit m2 = {b, s.row0, rt * ROWS, min(ROWS, s.n * G - rt * ROWS), h, page_owner(u.at + u.cost - 1, total, nc), ROWS, 0};
+            part.meta[cta] = m2;
         }
-        x = at + k1;
-        if (ends) next_unit();
+        x = u.at + k1;
+        if (ends) line.next(u);
     }
 }
 
@@ -492,12 +446,13 @@ static cudaError_t launch_token(const PageAttention &a, const PagePartials &part
 
 int page_token_ctas(int sm_count) { return 2 * sm_count; }
 
-// rows of a tile that the kernel would be given for `rows` (token, head) rows per sequence; 0: shapes it does not take
-int page_token_rows(int dtype, int format, int d, int rows)
+// Rows of a tile for `rows` (token, head) rows per sequence and KV head on average; 0: not for this kernel.
+int page_token_rows(int dtype, int format, int d, int G, int rows)
 {
     if (dtype != REFLEX_DTYPE_BF16 || d < 64) return 0;
-    if (rows <= 8) return 8;
-    return format == REFLEX_PAGE_SAME && d == 256 ? 8 : 16;        // (16 rows of bf16 rows of 256 do not fit the registers)
+    const bool wide = format == REFLEX_PAGE_SAME && d == 256;         // (16 rows of bf16 rows of 256 do not fit the registers)
+    if (rows > (format == REFLEX_PAGE_SAME ? 16 : 64) && page_chunk_takes(dtype, G, d)) return 0;
+    return rows <= 8 || wide ? 8 : 16;
 }
 
 cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int ctas, cudaStream_t st)
@@ -513,10 +468,8 @@ cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, 
         if (a.g.d == 128) return go(f, std::integral_constant<int, 128>{});
         return go(f, std::integral_constant<int, 256>{});
     };
-    cudaError_t e = format == REFLEX_PAGE_SAME ? by_d(std::integral_constant<int, REFLEX_PAGE_SAME>{})
-                    : format == REFLEX_PAGE_E4M3 ? by_d(std::integral_constant<int, REFLEX_PAGE_E4M3>{}) : by_d(std::integral_constant<int, REFLEX_PAGE_INT8>{});
-    if (e != cudaSuccess) return e;
-    return launch_page_merge(a, part, ctas, st);
+    return format == REFLEX_PAGE_SAME ? by_d(std::integral_constant<int, REFLEX_PAGE_SAME>{})
+           : format == REFLEX_PAGE_E4M3 ? by_d(std::integral_constant<int, REFLEX_PAGE_E4M3>{}) : by_d(std::integral_constant<int, REFLEX_PAGE_INT8>{});
 }
 
 }  // namespace reflex

@@ -1,4 +1,5 @@
 // Host side of the paged prefix declared in reflex.h: argument checks, geometry, kernel selection. No call allocates device memory.
+#include <algorithm>
 #include <cstring>
 #include <new>
 
@@ -34,18 +35,23 @@ bool desc_ok(const reflex_pages_desc *d)
 size_t rows_of(const reflex_pages_desc &d) { return (size_t)d.n_pages * d.Hkv * d.page; }
 size_t row_bytes(const reflex_pages_desc &d) { return (size_t)d.d * (d.format == REFLEX_PAGE_SAME ? elem_size(d.dtype) : 1); }
 
-// Layout of the workspace: status word, then the partial results of split units.
-struct PagesLayout { size_t meta, ml, o, bytes; };
+// Layout of the workspace: status word, marked sequences, partial results of split units, one layer of pages in bf16 (8-bit formats).
+struct PagesLayout { size_t done, careful, meta, ml, o, wide, bytes; };
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+constexpr int kMostCtas = 512;              // of a launch that leaves partial results (the token kernel: two per SM)
+constexpr int kMostPairs = 128;
+bool widened(const reflex_pages_desc &d) { return d.format != REFLEX_PAGE_SAME && page_chunk_takes(d.dtype, d.Hq / d.Hkv, d.d); }
 PagesLayout pages_layout(const reflex_pages_desc &d)
 {
-    constexpr size_t ctas = 2 * 256;            // (more than any device has SMs, twice)
-    constexpr size_t rows = 16;
+    const size_t rows = page_chunk_takes(d.dtype, d.Hq / d.Hkv, d.d) ? std::max((size_t)2 * kMostCtas * 16, (size_t)2 * kMostPairs * 256) : (size_t)2 * kMostCtas * 16;
     PagesLayout w;
-    w.meta = 256;
-    w.ml = w.meta + up256(ctas * sizeof(int4));
-    w.o = w.ml + up256(2 * ctas * rows * sizeof(float2));
-    w.bytes = w.o + up256(2 * ctas * rows * (size_t)d.d * sizeof(float));
+    w.done = 128;
+    w.careful = 256;
+    w.meta = w.careful + kMaxSeqs;
+    w.ml = w.meta + up256(kMostCtas * sizeof(PageSplit));
+    w.o = w.ml + up256(rows * sizeof(float2));
+    w.wide = w.o + up256(rows * (size_t)d.d * sizeof(float));
+    w.bytes = w.wide + (widened(d) ? 2 * up256(rows_of(d) * (size_t)d.d * 2) : 0);
     return w;
 }
 
@@ -142,7 +148,7 @@ int reflex_pages_create(const reflex_pages_desc *desc, void *k_pool, void *v_poo
     p->k = (char *)k_pool; p->v = (char *)v_pool; p->ke = (char *)k_exp; p->ve = (char *)v_exp; p->ws = (char *)workspace;
     cudaError_t e = cudaGetDevice(&p->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device);
-    if (e == cudaSuccess) e = cudaMemsetAsync(workspace, 0, 256, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(workspace, 0, 256 + kMaxSeqs, (cudaStream_t)stream);
     if (e != cudaSuccess) { delete p; return fail_cuda(e, "pages set-up"); }
     *out = p;
     return REFLEX_OK;
@@ -229,19 +235,34 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)d.d);
     const int G = d.Hq / d.Hkv;
     const long long per_seq = ((long long)n_rows * G + batch->B - 1) / batch->B;           // (token, head) rows of a sequence and KV head
-    const int token_rows = page_token_rows(d.dtype, d.format, d.d, per_seq > 1 << 20 ? 1 << 20 : (int)per_seq);
+    cudaStream_t st = (cudaStream_t)stream;
+    const PagesLayout w = pages_layout(d);
+    PagePartials part;
+    part.o = (float *)(p->ws + w.o); part.ml = (float2 *)(p->ws + w.ml); part.meta = (PageSplit *)(p->ws + w.meta);
+    part.careful = (uint8_t *)(p->ws + w.careful); part.careful_done = (uint32_t *)(p->ws + w.done);
+    part.scale_log2 = a.scale * 1.4426950408889634f;
     cudaError_t e;
+    int ctas = 0;
+    const int token_rows = page_token_rows(d.dtype, d.format, d.d, G, (int)std::min(per_seq, 1ll << 20));
     if (token_rows) {
-        const PagesLayout w = pages_layout(d);
-        PagePartials part;
-        part.o = (float *)(p->ws + w.o); part.ml = (float2 *)(p->ws + w.ml); part.meta = (int4 *)(p->ws + w.meta);
         part.rows = token_rows;
-        part.scale_log2 = a.scale * 1.4426950408889634f;
-        const int ctas = page_token_ctas(p->sm_count) < 512 ? page_token_ctas(p->sm_count) : 512;
-        e = launch_page_token(a, part, d.format, token_rows, ctas, (cudaStream_t)stream);
+        ctas = std::min(page_token_ctas(p->sm_count), kMostCtas);
+        e = launch_page_token(a, part, d.format, token_rows, ctas, st);
+    } else if (page_chunk_takes(d.dtype, G, d.d)) {
+        part.rows = 256;
+        ctas = std::min(p->sm_count / 2, kMostPairs);
+        const void *k = a.g.k, *v = a.g.v;
+        e = cudaSuccess;
+        if (d.format != REFLEX_PAGE_SAME) {
+            k = p->ws + w.wide;
+            v = p->ws + w.wide + (w.bytes - w.wide) / 2;
+            e = launch_page_widen(a, (void *)k, (void *)v, d.format, p->sm_count, st);
+        }
+        if (e == cudaSuccess) e = launch_page_chunk(a, part, k, v, ctas, st);
     } else {
-        e = launch_page_plain(a, d.dtype, d.format, (cudaStream_t)stream);
+        e = launch_page_plain(a, d.dtype, d.format, st);
     }
+    if (e == cudaSuccess && ctas) e = launch_page_merge(a, part, ctas, d.format, p->sm_count, st);
     return e == cudaSuccess ? REFLEX_OK : fail_cuda(e, "page attention launch");
 }
 

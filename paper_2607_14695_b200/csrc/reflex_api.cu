@@ -233,7 +233,7 @@ static const char *wait_site_kernel(uint32_t site)
         {kSiteAttnTc2, "attn_tc_kernel"}, {kSiteGate, "attn_tc2_kernel"}, {kSiteProbe, "gate_tc_kernel"}, {kSiteQkv, "wait_limit_probe_kernel"},
         {kSiteFewRows, "norm_qkv_tc_kernel"}, {kSiteLinear, "norm_linear_small_kernel"}, {kSiteTileGemm, "linear_res_tc_kernel"},
         {kSiteChainGemm, "tile_gemm_kernel"}, {kSiteChainAttn, "chain_gemm_kernel"}, {kSiteLinearHalf, "chain_attn_kernel"},
-        {kSiteAttnPair, "linear_half_kernel"}, {kSiteEnd, "attn_pair_kernel"}};
+        {kSiteAttnPair, "linear_half_kernel"}, {kSitePages, "attn_pair_kernel"}, {kSiteEnd, "page_chunk_kernel"}};
     for (const auto &k : kKernels)
         if (site < k.end) return k.name;
     return "unknown";

@@ -36,7 +36,7 @@ struct WorkspaceLayout {
 // Wait sites of the status word: a kernel's own numbers (from 1) behind a base of its own, so that a report names the kernel (wait_site_kernel)
 enum WaitSites : uint32_t {
     kSiteAttnTc = 0, kSiteAttnTc2 = 32, kSiteGate = 64, kSiteProbe = 127, kSiteQkv = 128, kSiteFewRows = 144, kSiteLinear = 160, kSiteTileGemm = 176,
-    kSiteChainGemm = 192, kSiteChainAttn = 208, kSiteLinearHalf = 224, kSiteAttnPair = 240, kSiteEnd = 256
+    kSiteChainGemm = 192, kSiteChainAttn = 208, kSiteLinearHalf = 224, kSiteAttnPair = 240, kSitePages = 256, kSiteEnd = 272
 };
 // (what the first wait that runs out leaves in the status word)
 __device__ __forceinline__ uint32_t status_word(uint32_t site) { return 0x80000000u | (site << 16) | (blockIdx.x & 0xFFFFu); }
@@ -120,6 +120,7 @@ cudaError_t launch_attention_simt(const AttnParams &p, cudaStream_t st);
 int simt_choose_splits(const AttnParams &p, size_t partial_bytes, int sm_count);
 cudaError_t launch_attention_merge(const AttnParams &p, cudaStream_t st);  // combines nsplit (m, l, acc) partials
 bool tc_supported(const AttnParams &p);
+bool encode_map_bf16(CUtensorMap *out, const void *ptr, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box);   // 128-byte swizzle, not cached
 bool tensor_map_2d_bf16(CUtensorMap *out, const void *ptr, int inner, int rows, int box_rows);
 bool tensor_map_kv_bf16(CUtensorMap *out, const void *ptr, int rows, int Hkv, int d, int box_rows);   // [rows][Hkv][d], box = box_rows x 1 head x 64
 bool tensor_map_q_bf16(CUtensorMap *out, const void *ptr, int B, int T, int Hq, int d, int heads, int tokens);   // [B][T][Hq][d], box = tokens x heads x 64

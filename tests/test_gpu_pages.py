@@ -254,7 +254,7 @@ def test_attention_of_masked_and_unmasked_nan(fmt, news):
             row = got[int(c.cu[b]) + i]
             if b == 0:
                 assert torch.isfinite(row).all() == (not s), (b, i)
-            elif fmt != rb.PAGE_SAME or max(news) == 1:
+            else:
                 assert torch.isfinite(row).all() == (not s), (b, i)
 
 
