@@ -31,104 +31,103 @@ __device__ __forceinline__ PageRange page_range(const PageSeq &s, const PageAtte
 }
 
 // ---- the line of work ----
-// A unit is a tile of `rows` consecutive (token, head of the group) rows of a sequence and a KV head; it costs what SPAN says of its tile, in blocks of
+// A unit is a tile of consecutive (token, head of the group) rows of a sequence and a KV head; it costs what SPAN says of its tile, in blocks of
 // keys, and one at least (rows that see nothing have to be written too). Units stand in a line by sequence, tile and KV head, and
-// CTA c of nc works on blocks [page_share(c), page_share(c + 1)) of it, whatever the lengths are.
-__host__ __device__ inline long long page_share(long long c, long long total, int nc) { return c * total / nc; }
+// CTA c of nc works on blocks [of(c), of(c + 1)) of it, whatever the lengths are. (32 bits: the host refuses calls whose line could be longer.)
+struct PageShares {
+    int each, more;          // `more` CTAs have each + 1 blocks, the others `each`
+    __device__ __forceinline__ PageShares(int total, int nc) : each(total / nc), more(total % nc) {}
+    __device__ __forceinline__ int of(int c) const { return c * each + min(c, more); }
+    // the CTA that works on block x
+    __device__ __forceinline__ int owner(int x) const
+    {
+        const int longer = more * (each + 1);
+        return x < longer ? x / (each + 1) : more + (x - longer) / each;
+    }
+};
 
-// SPAN: struct with .count (blocks) from (sequence, tile). All functions: whole warps, every lane gets the same result.
+// SPAN: tiles(s) of a sequence; (s, tile) gives a struct with .count (blocks). Functions that take `lane`: whole warps, all lanes get the same.
 template <typename SPAN>
 struct PageLine {
     const PageAttention &p;
-    SPAN span;
-    int rows, G;
+    const SPAN span;
 
-    __device__ __forceinline__ int tiles(const PageSeq &s) const { return (int)(((long long)s.n * G + rows - 1) / rows); }
-    // blocks of a sequence's units. (With few sequences several lanes share one: `width` of them, this one is number `sub`.)
-    __device__ __forceinline__ long long seq_cost(const PageSeq &s, int sub, int width, int &longest) const
-    {
-        long long cost = 0;
-        const int n = tiles(s);
-        for (int t = sub; t < n; t += width) {
-            const int c = max(1, span(s, t).count);
-            cost += c;
-            longest = max(longest, c);
-        }
-        for (int o = 1; o < width; o <<= 1) cost += __shfl_xor_sync(0xffffffffu, cost, o);
-        return cost * p.g.Hkv;
-    }
+    // With few sequences several lanes share one: width() of them.
     __device__ __forceinline__ int width() const
     {
         int w = 32;
         while (w > 1 && p.q.B * w > 32) w >>= 1;
         return w;
     }
-    // of sequences b0 .. b0 + 31 / width: the cost of this lane's, 0 behind the last one
-    __device__ __forceinline__ long long lane_cost(int b0, int w, int lane, int &longest) const
+    // the blocks of sequence b0 + lane / w (0 behind the last one), in all its w lanes
+    __device__ __forceinline__ int seq_cost(int b0, int w, int lane, int &longest) const
     {
-        PageSeq s = {0, 0, 0, 0};
-        if (b0 + lane / w < p.q.B) s = page_seq(p, b0 + lane / w);
-        return seq_cost(s, lane % w, w, longest);
+        int cost = 0;
+        if (b0 + lane / w < p.q.B) {
+            const PageSeq s = page_seq(p, b0 + lane / w);
+            const int n = span.tiles(s);
+            for (int t = lane & (w - 1); t < n; t += w) {
+                const int c = max(1, span(s, t).count);
+                cost += c;
+                longest = max(longest, c);
+            }
+        }
+        for (int o = 1; o < w; o <<= 1) cost += __shfl_xor_sync(0xffffffffu, cost, o);
+        return cost * p.g.Hkv;
     }
-    __device__ __forceinline__ long long total(int lane, int &longest) const
+    __device__ __forceinline__ int total(int lane, int &longest) const
     {
         const int w = width();
-        long long sum = 0;
+        int sum = 0;
         longest = 1;
         for (int b0 = 0; b0 < p.q.B; b0 += 32 / w) {
-            const long long c = lane_cost(b0, w, lane, longest);
-            sum += lane % w == 0 ? c : 0;
+            const int c = seq_cost(b0, w, lane, longest);
+            sum += (lane & (w - 1)) == 0 ? c : 0;
         }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         longest = __reduce_max_sync(0xffffffffu, longest);
-        return sum;
+        return __reduce_add_sync(0xffffffffu, sum);
     }
 
     // ---- a place in the line: unit (s, tile, h) begins at block `at` ----
     struct Place {
         PageSeq s;
-        int tile, h, cost;
-        long long at;
+        int tiles, tile, h, cost, at;
         decltype(span(PageSeq(), 0)) sp;
     };
-    __device__ __forceinline__ void settle(Place &u) const { u.sp = span(u.s, u.tile); u.cost = max(1, u.sp.count); }
+    static __device__ __forceinline__ int scan(int c, int lane)
+    {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, c, o);
+            if (lane >= o) c += y;
+        }
+        return c;
+    }
     // the unit that block x (< total) belongs to
-    __device__ __forceinline__ Place find(long long x, int lane) const
+    __device__ __forceinline__ Place find(int x, int lane) const
     {
         Place u;
         const int w = width();
-        int unused = 0;
+        int unused = 0, b = 0;
         u.at = 0;
-        int b = 0;
         for (int b0 = 0; b0 < p.q.B; b0 += 32 / w) {
-            const long long c = lane_cost(b0, w, lane, unused);
-            long long incl = lane % w == 0 ? c : 0;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += y;
-            }
+            const int c = (lane & (w - 1)) == 0 || w == 1 ? 1 : 0, cost = seq_cost(b0, w, lane, unused) * c;
+            const int incl = scan(cost, lane);
             const uint32_t past = __ballot_sync(0xffffffffu, u.at + incl > x);
             if (past) {
                 const int src = __ffs(past) - 1;          // (the first lane of its sequence's)
                 b = b0 + src / w;
-                u.at += __shfl_sync(0xffffffffu, incl - c, src);
+                u.at += __shfl_sync(0xffffffffu, incl - cost, src);
                 break;
             }
             u.at += __shfl_sync(0xffffffffu, incl, 31);
         }
         u.s = page_seq(p, b);
-        const int n = tiles(u.s);
+        u.tiles = span.tiles(u.s);
         u.tile = 0;
-        for (int t0 = 0; t0 < n; t0 += 32) {
-            const long long c = t0 + lane < n ? (long long)max(1, span(u.s, t0 + lane).count) * p.g.Hkv : 0;
-            long long incl = c;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += y;
-            }
+        for (int t0 = 0; t0 < u.tiles; t0 += 32) {
+            const int c = t0 + lane < u.tiles ? max(1, span(u.s, t0 + lane).count) * p.g.Hkv : 0;
+            const int incl = scan(c, lane);
             const uint32_t past = __ballot_sync(0xffffffffu, u.at + incl > x);
             if (past) {
                 const int src = __ffs(past) - 1;
@@ -138,9 +137,10 @@ struct PageLine {
             }
             u.at += __shfl_sync(0xffffffffu, incl, 31);
         }
-        settle(u);
-        u.h = min((int)((x - u.at) / u.cost), p.g.Hkv - 1);
-        u.at += (long long)u.h * u.cost;
+        u.sp = span(u.s, u.tile);
+        u.cost = max(1, u.sp.count);
+        u.h = p.g.Hkv == 1 ? 0 : (x - u.at) / u.cost;
+        u.at += u.h * u.cost;
         return u;
     }
     // the unit behind u (callable by single lanes); behind the last one u.s.b is B
@@ -149,14 +149,16 @@ struct PageLine {
         u.at += u.cost;
         if (++u.h < p.g.Hkv) return;
         u.h = 0;
-        if (++u.tile >= tiles(u.s)) {
+        if (++u.tile >= u.tiles) {
             u.tile = 0;
             do {
                 if (++u.s.b >= p.q.B) return;
                 u.s = page_seq(p, u.s.b);
             } while (u.s.n == 0);
+            u.tiles = span.tiles(u.s);
         }
-        settle(u);
+        u.sp = span(u.s, u.tile);
+        u.cost = max(1, u.sp.count);
     }
 };
 
@@ -177,15 +179,6 @@ struct PagePartials {
     float scale_log2;
 };
 __device__ __forceinline__ float *partial8(const PagePartials &part, size_t slot, int d, int r, int c0) { return part.o + ((slot * (size_t)(d >> 3) + (size_t)(c0 >> 3)) * part.rows + r) * 8; }
-// the last CTA whose share reaches block `x` of the line
-__device__ __forceinline__ int page_owner(long long x, long long total, int nc)
-{
-    int c = (int)(x * nc / total);
-    while (c > 0 && page_share(c, total, nc) > x) --c;
-    while (c + 1 < nc && page_share(c + 1, total, nc) <= x) ++c;
-    return c;
-}
-
 int page_token_ctas(int sm_count);
 int page_token_rows(int dtype, int format, int d, int G, int rows);
 cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int ctas, cudaStream_t st);

@@ -4,12 +4,15 @@
 // 64 keys of K, and half of the columns of V; TMA brings them from the pages, one box per page (or per 64 tokens of a larger page), to
 // where the swizzled tile has them. S = Q K^T and O = P V accumulate in tensor memory; P (bf16) is written over the logits it came from and is
 // the A operand of P V from there. Per CTA:
-//   warp 0       TMA producer (its Q tile, its half of K, its columns of V)
-//   warp 1       MMA issuer (leader CTA): Q K^T of the next tile before P V of this one
-//   warps 2..9   softmax: two threads per row, 64 keys each; maxima through shared memory, lazy rescale of O
+//   warps 0, 2   TMA producers: its Q tile and its half of K; its columns of V (warp 3 is idle)
+//   warp 1       MMA issuer (leader CTA): Q K^T runs one tile (two at head_dim <= 128) ahead of P V
+//   warps 4..    softmax: two threads per row, 64 keys each, eight warps a tile. At head_dim 128 and 64 there are two such groups, which take the tiles
+//                in turn: each then has the time of two tiles for its chain of loads, maximum, exponentials and stores, and a scheduler
+//                has four of its warps. The threads of a row agree on the reference maximum at one named barrier per 32 rows, where the group
+//                that has had the tile before leaves the row's reference, too; O is rescaled only where it has grown by more than 2^8.
 // What bounds it: at head_dim 256 the tensor pipe (2048 cycles a tile; operand reads then take two thirds of the shared memory's bandwidth), at 128 and
-// 64 the softmax (16 K exponentials a tile and SM). Heads of 64 run as heads of 128 whose upper chunk is left out of Q K^T and whose upper columns of O
-// are never read: P V costs twice, underneath the softmax.
+// 64 the softmax (16 K exponentials a tile and SM, some 1000 issue slots a scheduler). Heads of 64 run as heads of 128 whose upper chunk is left out of
+// Q K^T and whose upper columns of O are never read: P V costs twice, underneath the softmax.
 //
 // The grid is one pair per SM pair; the tiles of all units form one line that the pairs share evenly (PageLine), so uneven sequences, causal masks and single
 // sequences fill the device alike. A unit that more than one pair works on leaves fp32 partials for page_merge_kernel.
@@ -29,7 +32,6 @@ namespace reflex {
 using namespace ptx;
 
 constexpr int kChunkKeys = 128;
-constexpr int kChunkThreads = 64 + 256;
 constexpr int kChunkRows = 256;                // of a unit
 constexpr unsigned long long kChunkWaitNs = 1000000000ull;
 constexpr float kChunkGrow = 8.0f;             // log2 units: O is rescaled only where a maximum grows by more than 2^8
@@ -41,6 +43,7 @@ struct ChunkSpan { int tile0, count, hi; };    // key tiles [tile0, tile0 + coun
 struct ChunkSpanOf {
     const PageAttention &p;
     int tokens;                                // of a unit
+    __device__ __forceinline__ int tiles(const PageSeq &s) const { return (s.n + tokens - 1) / tokens; }
     __device__ __forceinline__ ChunkSpan operator()(const PageSeq &s, int tile) const
     {
         const PageRange r = page_range(s, p, tile * tokens, min(s.n, (tile + 1) * tokens) - 1);
@@ -56,6 +59,13 @@ template <int HD, int D> struct Chunk {
     static constexpr int CH = D / 64;                           // 64-column chunks of Q and K
     static constexpr int VCH = HD / 128;                        // chunks of V of this CTA
     static constexpr int NST = HD == 256 ? 2 : 4;               // stages of K, and of V
+    static constexpr int NS = HD == 256 ? 2 : 3;                // buffers of logits and weights in tensor memory
+    static constexpr int AHEAD = NS - 1;                        // tiles that Q K^T is ahead of P V
+    static constexpr int NG = HD == 256 ? 1 : 2;                // softmax groups of 8 warps
+    static constexpr int THREADS = 128 + 256 * NG;
+    static constexpr int QFULL = 0, QEMPTY = 1, KFULL = 2, KEMPTY = KFULL + NST, VLAND = KEMPTY + NST, VEMPTY = VLAND + NST, SFULL = VEMPTY + NST, PFULL = SFULL + NS,
+                         PVDONE = PFULL + NS, OFREE = PVDONE + 4, COUNT = OFREE + 1;
+    static constexpr uint32_t BAR_BYTES = (8 * COUNT + 104 + 127) / 128 * 128;                // ... tensor memory's address, abort flag, bad units, tiles
     static constexpr uint32_t Q_BYTES = CH * 128 * 128;
     static constexpr uint32_t K_STAGE = CH * 64 * 128;
     static constexpr uint32_t V_STAGE = VCH * 128 * 128;
@@ -64,12 +74,12 @@ template <int HD, int D> struct Chunk {
     static constexpr uint32_t OFF_V = OFF_K + NST * K_STAGE;
     static constexpr uint32_t OFF_STAGE = OFF_V + NST * V_STAGE;      // two halves of 128 rows x 64 columns of the result
     static constexpr uint32_t OFF_BAR = OFF_STAGE + 2 * 128 * 128;
-    static constexpr uint32_t OFF_XMAX = OFF_BAR + 256;               // [2][128][2] row maxima
-    static constexpr uint32_t NEED = OFF_XMAX + 2 * 128 * 2 * 4;
+    static constexpr uint32_t OFF_MAX = OFF_BAR + BAR_BYTES;          // [2 tiles][128 rows][2 halves] maxima of the logits
+    static constexpr uint32_t OFF_REF = OFF_MAX + 2 * 128 * 2 * 4;    // [128] reference maxima, from group to group (two groups only)
+    static constexpr uint32_t OFF_SUM = OFF_REF + (NG - 1) * 128 * 4; // [2 NG][128] (reference, sum) at the end of a unit; one group: in the maxima's place
+    static constexpr uint32_t NEED = NG == 1 ? OFF_REF : OFF_SUM + 2 * NG * 128 * 8;
     static constexpr uint32_t TOTAL = NEED + 1024 > 232448 ? 232448 : NEED + 1024;
-    static constexpr int QFULL = 0, QEMPTY = 1, KFULL = 2, KEMPTY = KFULL + NST, VLAND = KEMPTY + NST, VEMPTY = VLAND + NST, SFULL = VEMPTY + NST, PFULL = SFULL + 2,
-                         PVDONE = PFULL + 2, OFREE = PVDONE + 2, COUNT = OFREE + 1;
-    static_assert(8 * COUNT + 8 + 32 <= 256, "barriers, tensor memory's address, abort flag, bad units");
+    static_assert(NEED <= TOTAL, "shared memory");
 };
 
 // bits [lo, hi) of a 64-bit word, whatever lo and hi are
@@ -81,14 +91,14 @@ __device__ __forceinline__ uint64_t bits64(int lo, int hi)
 }
 
 template <int HD, int D>
-__global__ void __launch_bounds__(kChunkThreads, 1)         // clusters of two
+__global__ void __launch_bounds__(Chunk<HD, D>::THREADS, 1)         // clusters of two
 page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const PageAttention p, const PagePartials part, int tile_tokens, int box)
 {
     using L = Chunk<HD, D>;
-    constexpr int CH = L::CH, VCH = L::VCH, NST = L::NST;
+    constexpr int CH = L::CH, VCH = L::VCH, NST = L::NST, NS = L::NS, AHEAD = L::AHEAD, NG = L::NG;
     constexpr uint32_t kColS = HD;
-    static_assert(HD + 2 * kChunkKeys <= 512, "tensor memory");
+    static_assert(HD + L::NS * kChunkKeys <= 512, "tensor memory");
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
     const uint32_t base = (raw_addr + 1023u) & ~1023u;
@@ -98,6 +108,8 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::OFF_BAR + 8 * L::COUNT);
     volatile uint32_t *abort_flag = tmem_slot + 1;
     volatile uint32_t *bad_unit = tmem_slot + 2;          // [8]: number (from 1) of the last unit of that residue which met a bad page
+    volatile uint32_t *tile_info = bad_unit + 8;           // [16]: what the issuer has to know of tile g (written by the leader's K producer ahead of the arrival on KFULL)
+    constexpr uint32_t kFirst = 1u, kLast = 2u, kSecond = 4u, kEnd = 8u;       // of its unit; has live keys in its second half; there is no such tile
     if ((base - raw_addr) + L::NEED > L::TOTAL) {          // (the same for every CTA: all of them leave)
         if (threadIdx.x == 0) report_page_wait(p.g.status, 15u);
         return;
@@ -106,11 +118,11 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const uint32_t rank = cluster_ctarank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int G = p.g.Hq / p.g.Hkv;
-    const ChunkSpanOf span_of{p, 2 * tile_tokens};
-    const PageLine<ChunkSpanOf> line{p, span_of, 2 * tile_tokens * G, G};
+    const PageLine<ChunkSpanOf> line{p, {p, 2 * tile_tokens}};
 
     if (threadIdx.x == 0) {
-        for (int i = 0; i < L::COUNT; ++i) mbar_init(bar(i), i == L::PFULL || i == L::PFULL + 1 || i == L::OFREE ? 16u : 1u);      // one arrival per softmax warp of either CTA
+        // (weights: an arrival per warp of the group of either CTA; the accumulator's release: of every softmax warp)
+        for (int i = 0; i < L::COUNT; ++i) mbar_init(bar(i), i >= L::PFULL && i < L::PFULL + NS ? 16u : i == L::OFREE ? 16u * NG : 1u);
         *abort_flag = 0u;
         for (int i = 0; i < 8; ++i) bad_unit[i] = 0u;
         fence_mbar_init();
@@ -142,189 +154,233 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     };
 
     int longest;
-    const long long total = line.total(lane, longest);
-    const int nc = (int)min((long long)pairs, total);
-    if (threadIdx.x == 64 && rank == 0) part.meta[pair].b = -1;      // (the thread that may write the entry later)
+    const int total = line.total(lane, longest);
+    const int nc = min(pairs, total);
+    if (threadIdx.x == 128 && rank == 0) part.meta[pair].b = -1;      // (the thread that may write the entry later)
     const bool works = pair < nc;
-    const long long x0 = works ? page_share(pair, total, nc) : 0, x1 = works ? page_share(pair + 1, total, nc) : 0;
-    using Place = typename PageLine<ChunkSpanOf>::Place;
-    // this pair's units, one after the other: the slice [k0, k1) of the unit's blocks, of which `n` are tiles of keys from tile `t0` on
-    struct Slice { Place u; long long x; int k0, k1, t0, n; };
-    auto cut = [&](Slice &w) {
-        w.k0 = (int)(w.x - w.u.at);
-        w.k1 = (int)min((long long)w.u.cost, x1 - w.u.at);
+    const PageShares shares(total, max(1, nc));
+    const int x0 = works ? shares.of(pair) : 0, x1 = works ? shares.of(pair + 1) : 0;
+    // This pair's units, one after the other: blocks [k0, k1) of unit u, of which `n` are tiles of keys, from tile `t0` on.
+    struct Slice { typename PageLine<ChunkSpanOf>::Place u; int k0, k1, t0, n; };
+    auto cut = [&](Slice &w, int x) {
+        w.k0 = x - w.u.at;
+        w.k1 = min(w.u.cost, x1 - w.u.at);
         w.t0 = w.u.sp.tile0 + w.k0;
         w.n = max(0, min(w.k1, w.u.sp.count) - w.k0);
     };
     auto step = [&](Slice &w) -> bool {      // to the next unit of the share
-        w.x = w.u.at + w.k1;
-        if (w.x >= x1) return false;
+        const int x = w.u.at + w.k1;
+        if (x >= x1) return false;
         line.next(w.u);
-        cut(w);
+        cut(w, x);
         return true;
     };
     Slice w0;
     if (works) {
         w0.u = line.find(x0, lane);
-        w0.x = x0;
-        cut(w0);
+        cut(w0, x0);
     }
+    // the tiles of the share as one sequence: number g, tile jj of unit number ui (of those that have keys)
+    struct Cursor { Slice w; int jj, g, ui; bool valid; };
+    auto settle = [&](Cursor &c) {          // at or behind c.w: the next unit with a tile
+        while (c.w.n == 0) {
+            if (!step(c.w)) { c.valid = false; return; }
+        }
+        c.jj = 0;
+    };
+    auto begin = [&]() -> Cursor {
+        Cursor c;
+        c.w = w0; c.jj = 0; c.g = 0; c.ui = 0; c.valid = true;
+        settle(c);
+        return c;
+    };
+    auto advance = [&](Cursor &c) {
+        ++c.g;
+        if (++c.jj == c.w.n) {
+            ++c.ui;
+            if (!step(c.w)) c.valid = false; else settle(c);
+        }
+    };
+    // Where a warp's tile of keys lies, box by box: lane i has the row of box i in the layer's pages (0 where it holds no key below the unit's
+    // last, or where the table is wrong: `bad`). It is looked up a tile ahead, since a table entry takes some 500 cycles to come.
+    const int per_half = 64 / box;               // boxes of 64 keys
+    auto boxes = [&](int key0, int hi) -> int { return (min(max(hi - key0, 0), 64) + box - 1) / box; };
+    auto look_up = [&](const Cursor &c, bool &bad) -> int {
+        const int key = (c.w.t0 + c.jj) * kChunkKeys + lane * box;
+        bad = false;
+        if (!c.valid || lane >= 2 * per_half || key >= c.w.u.sp.hi) return 0;
+        const int page = page_at(p.q, p.g.n_pages, c.w.u.s.b, key >> p.g.log_p);
+        bad = page < 0;
+        return bad ? 0 : (int)page_row(p.g, page, c.w.u.h) + (key & (p.g.P - 1));
+    };
 
-    if (!works) {
-        // (no unit: on to the end, where the pair leaves together)
-    } else if (warp == 0) {
-        // ---------------- TMA producer ----------------
-        if (lane == 0) {
-            // The MMA warp issues Q K^T(j + 1) before P V(j): K goes one tile ahead of V through the same list of tiles.
-            struct Cursor { Slice w; int jj, g, ui; bool valid; };
-            auto settle = [&](Cursor &c) {          // at or behind c.w: the next unit with a tile
-                while (c.w.n == 0) {
-                    if (!step(c.w)) { c.valid = false; return; }
-                }
-                c.jj = 0;
-            };
-            auto advance = [&](Cursor &c) {
-                ++c.g;
-                if (++c.jj == c.w.n) {
-                    ++c.ui;
-                    if (!step(c.w)) c.valid = false; else settle(c);
-                }
-            };
-            // boxes of the 64 keys from key0 on that hold a key below hi
-            auto boxes = [&](int key0, int hi) -> int { return (min(max(hi - key0, 0), 64) + box - 1) / box; };
-            auto row_of = [&](const Cursor &c, int key) -> int {
-                int page = page_at(p.q, p.g.n_pages, c.w.u.s.b, key >> p.g.log_p);
-                if (page < 0) { page = 0; bad_unit[c.ui & 7] = (uint32_t)c.ui + 1u; }
-                return (int)(page_row(p.g, page, c.w.u.h)) + (key & (p.g.P - 1));
-            };
-            bool ok = true;
-            auto issue_k = [&](const Cursor &c) {
-                const int st = c.g % NST, key0 = (c.w.t0 + c.jj) * kChunkKeys, hi = c.w.u.sp.hi;
-                if (c.g >= NST) ok = wait(L::KEMPTY + st, (uint32_t)(c.g / NST - 1) & 1u, 1);
-                if (!ok) return;
-                if (rank == 0) mbar_expect_tx(bar(L::KFULL + st), (uint32_t)((boxes(key0, hi) + boxes(key0 + 64, hi)) * box * 128 * CH));
-                const int mine = key0 + 64 * (int)rank, nb = boxes(mine, hi);
-                for (int i = 0; i < nb; ++i) {
-                    const int row = row_of(c, mine + i * box);
+    // (a pair without a unit goes on to the end, where it leaves together)
+    if (works && warp == 0) {
+        // ---------------- Q and K by TMA (the warp stays converged, one lane issues) ----------------
+        Cursor c = begin();
+        bool bad, ok = true;
+        int row = look_up(c, bad);
+        while (c.valid) {
+            const int st = c.g % NST, key0 = (c.w.t0 + c.jj) * kChunkKeys, hi = c.w.u.sp.hi;
+            if (c.g >= NST) ok = wait(L::KEMPTY + st, (uint32_t)(c.g / NST - 1) & 1u, 1);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            const int nb = boxes(key0 + 64 * (int)rank, hi);
+            if (rank == 0 && lane == 0) {
+                tile_info[c.g & 15] = (c.jj == 0 ? kFirst : 0u) | (c.jj + 1 == c.w.n ? kLast : 0u) | (key0 + 64 < hi ? kSecond : 0u);
+                mbar_expect_tx(bar(L::KFULL + st), (uint32_t)((boxes(key0, hi) + boxes(key0 + 64, hi)) * box * 128 * CH));
+            }
+            __syncwarp();
+            const uint32_t dst = base + L::OFF_K + st * L::K_STAGE, full = bar(L::KFULL + st) & kPeerBitMask;
+            for (int i = 0; i < nb; ++i) {
+                const int r = __shfl_sync(0xffffffffu, row, (int)rank * per_half + i);
 #pragma unroll
-                    for (int ch = 0; ch < CH; ++ch)
-                        tma2_load_2d(base + L::OFF_K + st * L::K_STAGE + ch * (64 * 128) + i * box * 128, &tm_k, bar(L::KFULL + st) & kPeerBitMask, ch * 64, row);
-                }
-            };
-            auto issue_q = [&](const Cursor &c) {
+                for (int ch = 0; ch < CH; ++ch) tma2_load_2d_elect(dst + ch * (64 * 128) + i * box * 128, &tm_k, full, ch * 64, r);
+            }
+            if (c.jj == 0) {
+                // the unit's Q, once the last Q K^T of the unit before has read the buffer
                 if (c.ui >= 1) ok = wait(L::QEMPTY, (uint32_t)(c.ui - 1) & 1u, 2);
-                if (!ok) return;
+                if (!__all_sync(0xffffffffu, ok)) break;
                 const uint32_t bytes = (uint32_t)(G * tile_tokens * 128 * CH);
-                if (rank == 0) mbar_expect_tx(bar(L::QFULL), 2 * bytes);
+                if (rank == 0) mbar_expect_tx_elect(bar(L::QFULL), 2 * bytes);
                 const int t = c.w.u.s.row0 + (2 * c.w.u.tile + (int)rank) * tile_tokens;
-                for (int ch = 0; ch < CH; ++ch) tma2_load_3d(base + L::OFF_Q + ch * (128 * 128), &tm_q, bar(L::QFULL) & kPeerBitMask, ch * 64, c.w.u.h * G, t);
-            };
-            auto issue_v = [&](const Cursor &c) {
-                const int st = c.g % NST, key0 = (c.w.t0 + c.jj) * kChunkKeys, hi = c.w.u.sp.hi;
-                if (c.g >= NST) ok = wait(L::VEMPTY + st, (uint32_t)(c.g / NST - 1) & 1u, 3);
-                if (!ok) return;
-                const int nb[2] = {boxes(key0, hi), boxes(key0 + 64, hi)};
-                int rows[2][4];
-                const bool holds = D == HD || rank == 0;          // (heads of 64: the upper columns are nobody's)
-                for (int hh = 0; hh < 2; ++hh)
-                    for (int i = 0; i < nb[hh]; ++i) rows[hh][i] = row_of(c, key0 + 64 * hh + i * box);
-                mbar_expect_tx(bar(L::VLAND + st), holds ? (uint32_t)((nb[0] + nb[1]) * box * 128 * VCH) : 0u);
-                if (!holds) return;
-                for (int hh = 0; hh < 2; ++hh)
-                    for (int i = 0; i < nb[hh]; ++i)
 #pragma unroll
-                        for (int ch = 0; ch < VCH; ++ch)
-                            tma_load_2d(base + L::OFF_V + st * L::V_STAGE + ch * (128 * 128) + hh * (64 * 128) + i * box * 128, &tm_v, bar(L::VLAND + st), ((int)rank * VCH + ch) * 64, rows[hh][i]);
-            };
-            Cursor ck;
-            ck.w = w0; ck.jj = 0; ck.g = 0; ck.ui = 0; ck.valid = true;
-            settle(ck);
-            Cursor cv = ck;
-            if (ck.valid) { issue_k(ck); if (ok) issue_q(ck); advance(ck); }
-            while (cv.valid && ok) {
-                const bool k_now = ck.valid;
-                if (k_now) { issue_k(ck); if (!ok) break; }
-                issue_v(cv);
-                if (!ok) break;
-                if (k_now) {
-                    if (ck.jj == 0) { issue_q(ck); if (!ok) break; }
-                    advance(ck);
-                }
-                advance(cv);
+                for (int ch = 0; ch < CH; ++ch) tma2_load_3d_elect(base + L::OFF_Q + ch * (128 * 128), &tm_q, bar(L::QFULL) & kPeerBitMask, ch * 64, c.w.u.h * G, t);
+            }
+            advance(c);
+            row = look_up(c, bad);
+        }
+        if (rank == 0 && !c.valid) {
+            if (c.g >= NST) ok = wait(L::KEMPTY + c.g % NST, (uint32_t)(c.g / NST - 1) & 1u, 1);
+            if (ok && lane == 0) {
+                tile_info[c.g & 15] = kEnd;
+                mbar_arrive(bar(L::KFULL + c.g % NST));
             }
         }
-    } else if (warp == 1) {
+    } else if (works && warp == 2) {
+        // ---------------- V by TMA: this CTA's columns (heads of 64: the upper columns are nobody's) ----------------
+        Cursor c = begin();
+        bool bad, ok = true;
+        int row = look_up(c, bad);
+        while (c.valid) {
+            const int st = c.g % NST, key0 = (c.w.t0 + c.jj) * kChunkKeys, hi = c.w.u.sp.hi;
+            if (c.g >= NST) ok = wait(L::VEMPTY + st, (uint32_t)(c.g / NST - 1) & 1u, 3);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            if (__any_sync(0xffffffffu, bad) && lane == 0) bad_unit[c.ui & 7] = (uint32_t)c.ui + 1u;
+            __syncwarp();
+            const int nb = D == HD || rank == 0 ? boxes(key0, hi) + boxes(key0 + 64, hi) : 0;       // (the second half has boxes only where the first is full)
+            if (lane == 0) mbar_expect_tx(bar(L::VLAND + st), (uint32_t)(nb * box * 128 * VCH));      // (by the lane that may have marked the unit)
+            __syncwarp();
+            const uint32_t dst = base + L::OFF_V + st * L::V_STAGE;
+            for (int i = 0; i < nb; ++i) {
+                const int r = __shfl_sync(0xffffffffu, row, i);
+#pragma unroll
+                for (int ch = 0; ch < VCH; ++ch) tma_load_2d_elect(dst + ch * (128 * 128) + i * box * 128, &tm_v, bar(L::VLAND + st), ((int)rank * VCH + ch) * 64, r);
+            }
+            advance(c);
+            row = look_up(c, bad);
+        }
+    } else if (works && warp == 1) {
         // ---------------- MMA issuer (leader CTA; the warp stays converged, one lane issues) ----------------
         if (rank == 0) {
             constexpr uint16_t both = 3;
             constexpr uint32_t idesc_qk = umma_idesc_bf16(256, kChunkKeys, false), idesc_pv = umma_idesc_bf16(256, HD, true);
             const uint64_t qdesc0 = umma_desc_sw128(base + L::OFF_Q, 16, 1024), kdesc0 = umma_desc_sw128(base + L::OFF_K, 16, 1024);
             const uint64_t vdesc0 = umma_desc_sw128(base + L::OFF_V, 128 * 128, 1024);
-            auto qk = [&](int gi, bool last) -> bool {
-                const int st = gi % NST, buf = gi & 1;
-                if (!wait(L::KFULL + st, (uint32_t)(gi / NST) & 1u, 4)) return false;
-                tc_fence_after();
-                uint64_t qd = qdesc0, kd = kdesc0;
-                umma_desc_advance(kd, (uint32_t)st * L::K_STAGE);
-#pragma unroll
-                for (int kk = 0; kk < D / 16; ++kk) {
-                    umma2_ss_elect(tmem_base + kColS + buf * kChunkKeys, qd, kd, idesc_qk, kk > 0 ? 1u : 0u);
-                    umma_desc_advance(qd, (kk & 3) == 3 ? 128 * 128 - 96 : 32);
-                    umma_desc_advance(kd, (kk & 3) == 3 ? 64 * 128 - 96 : 32);
-                }
-                umma2_commit_mc_elect(bar(L::KEMPTY + st), both);
-                umma2_commit_mc_elect(bar(L::SFULL + buf), both);
-                if (last) umma2_commit_mc_elect(bar(L::QEMPTY), both);
-                return true;
-            };
-            bool ok = true;
-            int gt = 0, ui = 0;
-            Slice w = w0;
-            do {
-                const int n = w.n;
-                if (n == 0) continue;
-                ok = wait(L::QFULL, (uint32_t)ui & 1u, 5) && qk(gt, n == 1);
-                for (int jj = 0; jj < n && ok; ++jj) {
-                    const int gi = gt + jj, st = gi % NST, buf = gi & 1;
-                    if (jj + 1 < n) { ok = qk(gi + 1, jj + 2 == n); if (!ok) break; }
-                    ok = wait(L::PFULL + buf, (uint32_t)(gi >> 1) & 1u, 6);
-                    if (ok && jj == 0 && ui >= 1) ok = wait(L::OFREE, (uint32_t)(ui - 1) & 1u, 7);
+            // Q K^T of tile `q` and P V of tile `v`, up to AHEAD tiles behind it. (The logits of tile g + NS go where the weights of tile g are: Q K^T of the one is
+            // issued behind P V of the other.) What a tile is comes with its keys; this warp shares its scheduler with busy ones, and walking the
+            // list of units here took 1200 cycles a tile.
+            bool ok = true, end = false;
+            int q = 0, v = 0, uq = 0, uv = 0;
+            while (ok) {
+                while (!end && q <= v + AHEAD) {
+                    const int st = q % NST, buf = q % NS;
+                    ok = wait(L::KFULL + st, (uint32_t)(q / NST) & 1u, 4);
                     if (!ok) break;
+                    const uint32_t info = tile_info[q & 15];
+                    end = (info & kEnd) != 0u;
+                    if (end) break;
+                    if (info & kFirst) {
+                        // a unit whose Q has not come yet does not hold up the products of the last one
+                        if (q > v) { if (!mbar_test_wait(bar(L::QFULL), (uint32_t)uq & 1u)) break; }
+                        else { ok = wait(L::QFULL, (uint32_t)uq & 1u, 5); if (!ok) break; }
+                        ++uq;
+                    }
                     tc_fence_after();
-                    uint64_t vd = vdesc0;
-                    umma_desc_advance(vd, (uint32_t)st * L::V_STAGE);
-                    // (a second half past the last key: its P is zero and its V was never loaded)
-                    const int ksteps = (w.t0 + jj) * kChunkKeys + 64 < w.u.sp.hi ? kChunkKeys / 16 : kChunkKeys / 32;
-#pragma unroll 4
-                    for (int kk = 0; kk < ksteps; ++kk) {
-                        umma2_ts_elect(tmem_base, tmem_base + kColS + buf * kChunkKeys + kk * 8, vd, idesc_pv, jj > 0 || kk > 0 ? 1u : 0u);
+                    uint64_t qd = qdesc0, kd = kdesc0;
+                    umma_desc_advance(kd, (uint32_t)st * L::K_STAGE);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        umma2_ss_elect(tmem_base + kColS + buf * kChunkKeys, qd, kd, idesc_qk, kk > 0 ? 1u : 0u);
+                        umma_desc_advance(qd, (kk & 3) == 3 ? 128 * 128 - 96 : 32);
+                        umma_desc_advance(kd, (kk & 3) == 3 ? 64 * 128 - 96 : 32);
+                    }
+                    umma2_commit_mc_elect(bar(L::SFULL + buf), both);
+                    umma2_commit_mc_elect(bar(L::KEMPTY + st), both);
+                    if (info & kLast) umma2_commit_mc_elect(bar(L::QEMPTY), both);
+                    ++q;
+                }
+                if (!ok || q == v) break;
+                const int st = v % NST, buf = v % NS;
+                const uint32_t info = tile_info[v & 15];
+                uint64_t vd = vdesc0;
+                umma_desc_advance(vd, (uint32_t)st * L::V_STAGE);
+                ok = wait(L::PFULL + buf, (uint32_t)(v / NS) & 1u, 6);
+                if (ok && (info & kFirst)) {
+                    if (uv >= 1) ok = wait(L::OFREE, (uint32_t)(uv - 1) & 1u, 7);
+                    ++uv;
+                }
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t p_tmem = tmem_base + kColS + buf * kChunkKeys, later = (info & kFirst) ? 0u : 1u;
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk) {
+                    umma2_ts_elect(tmem_base, p_tmem + kk * 8, vd, idesc_pv, kk > 0 ? 1u : later);
+                    umma_desc_advance(vd, 16 * 128);
+                }
+                if (info & kSecond) {              // (else its weights are zero and its V was never loaded)
+#pragma unroll
+                    for (int kk = 4; kk < 8; ++kk) {
+                        umma2_ts_elect(tmem_base, p_tmem + 64 + (kk & 3) * 8, vd, idesc_pv, 1u);
                         umma_desc_advance(vd, 16 * 128);
                     }
-                    umma2_commit_mc_elect(bar(L::VEMPTY + st), both);
-                    umma2_commit_mc_elect(bar(L::PVDONE + buf), both);
                 }
-                gt += n;
-                ++ui;
-            } while (ok && step(w));
+                umma2_commit_mc_elect(bar(L::PVDONE + (v & 3)), both);
+                umma2_commit_mc_elect(bar(L::VEMPTY + st), both);
+                ++v;
+            }
         }
-    } else {
+    } else if (works && warp >= 4) {
         // ---------------- softmax, rescaling, results ----------------
-        const int sw = warp - 2, half = sw >> 2;          // which 64 keys of the tile
-        const int row = (warp & 3) * 32 + lane;
-        const uint32_t lane_addr = (uint32_t)((warp & 3) * 32) << 16;
-        const uint32_t leader_pfull[2] = {mapa(bar(L::PFULL), 0), mapa(bar(L::PFULL + 1), 0)};
-        const uint32_t leader_ofree = mapa(bar(L::OFREE), 0);
-        float *xmax = reinterpret_cast<float *>(smem + L::OFF_XMAX);         // [2 buffers][128 rows][2 halves]
+        const int sw = warp - 4, group = sw >> 3, half = (sw >> 2) & 1, quarter = warp & 3;
+        const int row = quarter * 32 + lane;
+        const uint32_t lane_addr = (uint32_t)(quarter * 32) << 16;
+        const uint32_t leader_pfull = mapa(bar(L::PFULL), 0), leader_ofree = mapa(bar(L::OFREE), 0);
+        float *maxima = reinterpret_cast<float *>(smem + L::OFF_MAX);
+        float *ref = reinterpret_cast<float *>(smem + L::OFF_REF);
+        float2 *sums = reinterpret_cast<float2 *>(smem + (NG == 1 ? L::OFF_MAX : L::OFF_SUM));
         const int rows_here = tile_tokens * G;
-        const int tid = threadIdx.x - 64;
+        const int tid = threadIdx.x - 128;
+        const float sc = part.scale_log2;
+        // where the 16 bytes that this thread stores of rows (tid / 8), + 32 NG, .. lie behind the first row of a tile
+        constexpr int RP = 32 * NG;
+        int out_at[128 / RP];
+#pragma unroll
+        for (int k = 0; k < 128 / RP; ++k) {
+            const int r = k * RP + (tid >> 3);
+            out_at[k] = (r / G * p.g.Hq + r % G) * D + (tid & 7) * 8;
+        }
+        const int row_token = row / G;
         bool ok = true;
         int gt = 0, ui = 0;
         Slice w = w0;
+        // Row exchange: the 64 threads of a group's quarter meet at barrier 1 + quarter + 4 group. With two groups the other one's quarter has
+        // arrived there, too, with its last tile (for the first tile of all: here).
+        if (NG == 2 && group == 1) asm volatile("bar.arrive %0, 128;" ::"r"(1 + quarter) : "memory");
         do {
             const PageSeq &s = w.u.s;
             const int token0 = (2 * w.u.tile + (int)rank) * tile_tokens;         // first of this CTA's rows
-            const int t_row = token0 + row / G;
-            const bool row_live = row < rows_here && t_row < s.n;
+            const int t_row = token0 + row_token, live_rows = min(rows_here, (s.n - token0) * G);
+            const bool row_live = row < live_rows;
             const PageRange mine = page_range(s, p, min(t_row, s.n - 1), min(t_row, s.n - 1));
             const bool whole = w.k0 == 0 && w.k1 == w.u.cost;
             // keys that every row of the pair sees (either CTA's V meets the rows of both)
@@ -333,138 +389,146 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             float m_ref = -INFINITY, l = 0.f;
             auto tile = [&](auto mode_c, const int jj) {
                 constexpr bool FULL = decltype(mode_c)::value == 0;
-                constexpr bool DEAD = decltype(mode_c)::value == 2;        // a half past the unit's last key: no logits to read and no P to write
-                const int gi = gt + jj, buf = gi & 1, st = gi % NST;
+                constexpr bool DEAD = decltype(mode_c)::value == 2;        // a half past the unit's last key: no logits to read and no weights to write
+                const int gi = gt + jj, buf = gi % NS, st = gi % NST;
                 const uint32_t vph = (uint32_t)(gi / NST) & 1u;
                 const int key0 = (w.t0 + jj) * kChunkKeys + half * 64;
-                uint64_t smask = ~0ull, tmask = ~0ull;          // keys that this row sees; keys that lie below the unit's last one
-                if constexpr (!FULL) {
-                    smask = bits64(mine.lo - key0, mine.hi - key0);
-                    tmask = bits64(0, w.u.sp.hi - key0);
-                }
-                float x[64];
+                const uint32_t s_addr = tmem_base + lane_addr + kColS + buf * kChunkKeys + half * 64;
+                const uint64_t mask = FULL ? ~0ull : bits64(mine.lo - key0, mine.hi - key0);       // keys that this row sees
+                float mx = -INFINITY;
+                // One group keeps its logits in registers (168 of them a thread); two groups (96) read them from tensor memory a second time.
+                uint32_t r[2][32];
                 if constexpr (!DEAD) {
-                    ok = ok && wait(L::SFULL + buf, (uint32_t)(gi >> 1) & 1u, 8);
+                    ok = ok && wait(L::SFULL + buf, (uint32_t)(gi / NS) & 1u, 8);
                     tc_fence_after();
-                    uint32_t r[64];
-                    tmem_ld32(tmem_base + lane_addr + kColS + buf * kChunkKeys + half * 64, *reinterpret_cast<uint32_t(*)[32]>(r));
-                    tmem_ld32(tmem_base + lane_addr + kColS + buf * kChunkKeys + half * 64 + 32, *reinterpret_cast<uint32_t(*)[32]>(r + 32));
-                    tmem_wait_ld();
+                    tmem_ld32(s_addr, r[0]);
+                    if (NG == 1) tmem_ld32(s_addr + 32, r[1]);
 #pragma unroll
-                    for (int c = 0; c < 64; ++c) x[c] = __uint_as_float(r[c]);
+                    for (int c = 0; c < 2; ++c) {
+                        if (NG == 2 || c == 0) tmem_wait_ld();
+                        uint32_t (&v)[32] = r[NG == 1 ? c : 0];
+                        if constexpr (!FULL) {
+                            const uint32_t bits = (uint32_t)(mask >> (32 * c));
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!(bits & (1u << i))) v[i] = 0xff800000u;
+                        }
+                        float x[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(v[i]);
+                        float mx4[4] = {mx, x[0], x[1], x[2]};
+#pragma unroll
+                        for (int i = 3; i + 7 < 32; i += 8) {
+                            mx4[0] = max3_nan_f32(mx4[0], x[i], x[i + 1]); mx4[1] = max3_nan_f32(mx4[1], x[i + 2], x[i + 3]);
+                            mx4[2] = max3_nan_f32(mx4[2], x[i + 4], x[i + 5]); mx4[3] = max3_nan_f32(mx4[3], x[i + 6], x[i + 7]);
+                        }
+                        mx4[0] = max3_nan_f32(mx4[0], x[27], x[28]); mx4[1] = max3_nan_f32(mx4[1], x[29], x[30]); mx4[2] = max_nan_f32(mx4[2], x[31]);
+                        mx = max_nan_f32(max_nan_f32(mx4[0], mx4[1]), max_nan_f32(mx4[2], mx4[3]));
+                        if (NG == 2) tmem_ld32(s_addr + (c == 0 ? 32 : 0), r[0]);
+                    }
+                    if (!(mx < INFINITY)) l = __int_as_float(0x7fc00000);      // (a logit that is NaN or +inf; the polynomial below would lose it)
+                }
+                maxima[((gi & 1) * 128 + row) * 2 + half] = mx;
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + quarter + 4 * group), "n"(64 * NG) : "memory");
+                const float2 both = *reinterpret_cast<const float2 *>(maxima + ((gi & 1) * 128 + row) * 2);
+                const float top = fmaxf(both.x, both.y);
+                const float was = NG == 1 || jj == 0 ? m_ref : ref[row];          // the row's reference so far
+                const bool grow = jj == 0 || (top - was) * sc > kChunkGrow;
+                const float to = grow ? top : was;
+                if (NG == 2) {
+                    if (half == 0) ref[row] = to;
+                    asm volatile("bar.arrive %0, 128;" ::"r"(1 + quarter + 4 * (group ^ 1)) : "memory");
+                }
+                if (m_ref != to) { l *= m_ref == -INFINITY ? (l == l ? 0.f : 1.f) : ex2((m_ref - to) * sc); m_ref = to; }
+                if (jj > 0 && __any_sync(0xffffffffu, grow)) {
+                    const float alpha = grow ? ex2((was - to) * sc) : 1.f;
+                    ok = ok && wait(L::PVDONE + ((gi - 1) & 3), (uint32_t)((gi - 1) >> 2) & 1u, 10);
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < D / 64; ++c) {
+                        uint32_t o[32];
+                        const uint32_t o_addr = tmem_base + lane_addr + half * (D / 2) + c * 32;
+                        tmem_ld32(o_addr, o);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                        tmem_st32(o_addr, o);
+                    }
+                    tmem_wait_st();
                 }
                 if constexpr (!FULL && !DEAD) {
                     // Keys behind the last one count as zeros in V (a weight of 0 does not make a stale NaN one); a key that only some rows see must be
-                    // finite, or the sequence is done again row by row. All 128 threads of the half share the rows: half a row's columns each.
+                    // finite, or the sequence is done again row by row. The 128 threads of a half share its 64 keys: half of this CTA's columns each.
                     ok = ok && wait(L::VLAND + st, vph, 9);
                     const int key = key0 + (row & 63);
-                    const bool dead = !((tmask >> (row & 63)) & 1ull);
-                    const bool some = !dead && (key < all_lo || key >= all_hi);
-                    uint4 *vr0 = reinterpret_cast<uint4 *>(smem + L::OFF_V + st * L::V_STAGE + (half * 64 + (row & 63)) * 128) + (row >> 6) * 4;
-                    if (dead) {
+                    uint4 *v0 = reinterpret_cast<uint4 *>(smem + L::OFF_V + st * L::V_STAGE + (half * 64 + (row & 63)) * 128) + (row >> 6) * 4;
+                    if (key >= w.u.sp.hi) {
 #pragma unroll
                         for (int c = 0; c < VCH; ++c)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) vr0[c * (128 * 128 / 16) + i] = make_uint4(0, 0, 0, 0);
-                    } else if (some && (D == HD || rank == 0)) {
+                            for (int i = 0; i < 4; ++i) v0[c * (128 * 128 / 16) + ((i + row) & 3)] = make_uint4(0, 0, 0, 0);
+                    } else if ((key < all_lo || key >= all_hi) && (D == HD || rank == 0)) {
                         uint32_t odd = 0;
 #pragma unroll
                         for (int c = 0; c < VCH; ++c)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
-                                const uint4 v = vr0[c * (128 * 128 / 16) + i];
+                                const uint4 v = v0[c * (128 * 128 / 16) + ((i + row) & 3)];
                                 const uint32_t q[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) odd |= ((q[e] & 0x7f80u) == 0x7f80u) | ((q[e] & 0x7f800000u) == 0x7f800000u);
                             }
                         if (odd) part.careful[s.b] = 1;
                     }
-                }
-                float mx = -INFINITY;
-                if constexpr (!DEAD) {
-                    if (!FULL && smask != ~0ull) {
-                        const uint32_t lo = (uint32_t)smask, hi = (uint32_t)(smask >> 32);
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) {
-                            if (!(lo & (1u << c))) x[c] = -INFINITY;
-                            if (!(hi & (1u << c))) x[32 + c] = -INFINITY;
-                        }
-                    }
-                    float mx4[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-                    for (int c = 4; c + 7 < 64; c += 8) {
-                        mx4[0] = max3_nan_f32(mx4[0], x[c], x[c + 1]); mx4[1] = max3_nan_f32(mx4[1], x[c + 2], x[c + 3]);
-                        mx4[2] = max3_nan_f32(mx4[2], x[c + 4], x[c + 5]); mx4[3] = max3_nan_f32(mx4[3], x[c + 6], x[c + 7]);
-                    }
-                    mx4[0] = max3_nan_f32(mx4[0], x[60], x[61]); mx4[1] = max3_nan_f32(mx4[1], x[62], x[63]);
-                    mx = max_nan_f32(max_nan_f32(mx4[0], mx4[1]), max_nan_f32(mx4[2], mx4[3]));
-                    if (!(mx < INFINITY)) l = __int_as_float(0x7fc00000);      // (a logit that is NaN or +inf; the polynomial below would lose it)
-                }
-                // The two threads of a row agree on its maximum. Past this barrier both have their logits in registers, so P may overwrite them.
-                xmax[(buf * 128 + row) * 2 + half] = mx;
-                asm volatile("bar.sync 1, 256;" ::: "memory");
-                mx = fmaxf(xmax[(buf * 128 + row) * 2], xmax[(buf * 128 + row) * 2 + 1]);
-                if (jj == 0) m_ref = mx;
-                else {
-                    const bool grow = (mx - m_ref) * part.scale_log2 > kChunkGrow;
-                    if (__any_sync(0xffffffffu, grow)) {
-                        const float alpha = grow ? ex2((m_ref - mx) * part.scale_log2) : 1.f;
-                        if (grow) m_ref = mx;
-                        l *= alpha;
-                        ok = ok && wait(L::PVDONE + ((gi - 1) & 1), (uint32_t)((gi - 1) >> 1) & 1u, 10);
-                        tc_fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < HD / 64; ++c) {
-                            uint32_t o[32];
-                            const uint32_t o_addr = tmem_base + lane_addr + half * (HD / 2) + c * 32;
-                            tmem_ld32(o_addr, o);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                            tmem_st32(o_addr, o);
-                        }
-                        tmem_wait_st();
-                    }
+                    fence_proxy_async_smem();
                 }
                 if constexpr (!DEAD) {
-                    const float mr = m_ref == -INFINITY ? 0.f : m_ref * part.scale_log2;
-                    const uint64_t sc2 = pack_f32x2(part.scale_log2, part.scale_log2), nm2 = pack_f32x2(-mr, -mr);
+                    const float mr = m_ref == -INFINITY ? 0.f : m_ref * sc;
+                    const uint64_t sc2 = pack_f32x2(sc, sc), nm2 = pack_f32x2(-mr, -mr);
                     const Ex2PolyConsts pk = ex2_poly_consts();
-                    uint64_t sum2[4] = {0ull, 0ull, 0ull, 0ull};
-                    uint32_t packed[32];
+                    uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll
-                    for (int c = 0; c < 64; c += 2) {
-                        float y0, y1, p0, p1;
-                        unpack_f32x2(fma_f32x2(pack_f32x2(x[c], x[c + 1]), sc2, nm2), y0, y1);
-                        if (((c >> 1) & 7) < kChunkPoly) ex2_poly_f32x2(y0, y1, pk, p0, p1);
-                        else { p0 = ex2(y0); p1 = ex2(y1); }
-                        sum2[(c >> 1) & 3] = add_f32x2(sum2[(c >> 1) & 3], pack_f32x2(p0, p1));
-                        packed[c >> 1] = pack_bf16(p0, p1);
+                    for (int c = 0; c < 2; ++c) {
+                        if (NG == 2) tmem_wait_ld();
+                        uint32_t (&v)[32] = r[NG == 1 ? c : 0];
+                        const uint32_t bits = (uint32_t)(mask >> (32 * c));
+                        uint64_t part2[2] = {0ull, 0ull};
+                        uint32_t packed[16];
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            if (!FULL && NG == 2) {
+                                if (!(bits & (1u << i))) v[i] = 0xff800000u;
+                                if (!(bits & (2u << i))) v[i + 1] = 0xff800000u;
+                            }
+                            float x0, x1, p0, p1;
+                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), sc2, nm2), x0, x1);
+                            if (((i >> 1) & 7) < kChunkPoly) ex2_poly_f32x2(x0, x1, pk, p0, p1);
+                            else { p0 = ex2(x0); p1 = ex2(x1); }
+                            part2[(i >> 1) & 1] = add_f32x2(part2[(i >> 1) & 1], pack_f32x2(p0, p1));
+                            packed[i >> 1] = pack_bf16(p0, p1);
+                            // (the polynomial gives a masked key 2^-125: nothing for the sum, but its weight must be exactly 0)
+                            if (!FULL && ((i >> 1) & 7) < kChunkPoly) packed[i >> 1] &= ((bits >> i) & 1u ? 0x0000FFFFu : 0u) | ((bits >> i) & 2u ? 0xFFFF0000u : 0u);
+                        }
+                        if (NG == 2 && c == 0) tmem_ld32(s_addr + 32, r[0]);
+                        if (FULL || bits != 0u) {              // (a row that sees nothing has no sum)
+                            sum2[0] = add_f32x2(sum2[0], part2[0]);
+                            sum2[1] = add_f32x2(sum2[1], part2[1]);
+                        }
+                        // (weights of keys 32 c .. of the half take the columns of its logits 16 c ..: read, and by this thread alone)
+                        tmem_st16(s_addr + 16 * c, packed);
                     }
                     float a, b;
-                    unpack_f32x2(add_f32x2(add_f32x2(sum2[0], sum2[1]), add_f32x2(sum2[2], sum2[3])), a, b);
-                    if (!FULL && smask == 0ull) a = b = 0.f;              // (the polynomial gives masked keys 2^-125: a row that sees nothing has no sum)
+                    unpack_f32x2(add_f32x2(sum2[0], sum2[1]), a, b);
                     l += a + b;
-                    if (!FULL && smask != ~0ull) {
-                        // ... and their weights must be exactly 0
-#pragma unroll
-                        for (int c = 0; c < 64; c += 2) {
-                            if (((c >> 1) & 7) < kChunkPoly) {
-                                const uint32_t two = (uint32_t)(smask >> c) & 3u;
-                                packed[c >> 1] &= ((two & 1u) ? 0x0000FFFFu : 0u) | ((two & 2u) ? 0xFFFF0000u : 0u);
-                            }
-                        }
-                    }
-                    tmem_st32(tmem_base + lane_addr + kColS + buf * kChunkKeys + half * 32, packed);
                     tmem_wait_st();
                 }
                 if (FULL || DEAD) ok = ok && wait(L::VLAND + st, vph, 11);       // (the arrival below says that this CTA's V is in place, too)
-                fence_proxy_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(leader_pfull[buf]);
+                if (lane == 0) mbar_arrive_cluster(leader_pfull + 8u * (uint32_t)buf);
             };
-            for (int jj = 0; jj < w.n; ++jj) {
+            // (groups take the tiles of the whole share in turn)
+            for (int jj = NG == 1 || (gt & 1) == group ? 0 : 1; jj < w.n; jj += NG) {
                 const int key0 = (w.t0 + jj) * kChunkKeys + half * 64;
                 if (key0 >= all_lo && key0 + 64 <= all_hi) tile(std::integral_constant<int, 0>{}, jj);
                 else if (key0 < w.u.sp.hi) tile(std::integral_constant<int, 1>{}, jj);
@@ -473,79 +537,83 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             gt += w.n;
             const int g_last = gt - 1;
             if (w.n > 0) {
-                ok = ok && wait(L::PVDONE + (g_last & 1), (uint32_t)(g_last >> 1) & 1u, 12);
+                ok = ok && wait(L::PVDONE + (g_last & 3), (uint32_t)(g_last >> 2) & 1u, 12);
                 if (bad_unit[ui & 7] == (uint32_t)ui + 1u || !ok) l = __int_as_float(0x7fc00000);
             }
-            // the row's sums, through the maxima's buffer that the last tile did not use
-            float *xsum = xmax + ((g_last & 1) ^ 1) * 256;
-            xsum[half * 128 + row] = l;
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            l += xsum[(half ^ 1) * 128 + row];
+            // the row's sum: the groups' references may differ, the latest one is the largest
+            if (NG == 1) asm volatile("bar.sync 9, 256;" ::: "memory");         // (the sums take the maxima's place)
+            sums[(group * 2 + half) * 128 + row] = make_float2(m_ref, l);
+            asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");
+            {
+                float2 all[2 * NG];
+                m_ref = -INFINITY;
+#pragma unroll
+                for (int q = 0; q < 2 * NG; ++q) { all[q] = sums[q * 128 + row]; m_ref = fmaxf(m_ref, all[q].x); }
+                l = 0.f;
+#pragma unroll
+                for (int q = 0; q < 2 * NG; ++q) l += all[q].x == m_ref ? all[q].y : all[q].x == -INFINITY ? all[q].y * 0.f : all[q].y * ex2((all[q].x - m_ref) * sc);
+            }
             tc_fence_after();
             if (w.n > 0 && tid == 0 && bad_unit[ui & 7] == (uint32_t)ui + 1u) report_bad_page(p.g.status, s.b);
             const float inv = l == 0.f || w.n == 0 || (m_ref == -INFINITY && l == l) ? 0.f : 1.f / l;
-            const bool unit_live = token0 < s.n;             // (a pair's second tile may have no row)
+            constexpr int PARTS = 2 * NG;            // threads of a row, which share its columns
+            const int me = group * 2 + half;
+            auto take = [&](int col, auto &o) {
+                if constexpr (sizeof(o) == 128) tmem_ld32(tmem_base + lane_addr + col, o); else tmem_ld16(tmem_base + lane_addr + col, o);
+                tmem_wait_ld();
+            };
+            auto release = [&] {                     // all of this thread's columns of O are in registers: the next unit may overwrite it
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0 && w.n > 0) mbar_arrive_cluster(leader_ofree);
+            };
             if (!whole) {
-                if (half == 0 && row_live) part.ml[(size_t)slot * kChunkRows + rank * 128 + row] = make_float2(m_ref == -INFINITY ? -INFINITY : m_ref * part.scale_log2, l);
+                if (me == 0 && row_live) part.ml[(size_t)slot * kChunkRows + rank * 128 + row] = make_float2(m_ref == -INFINITY ? -INFINITY : m_ref * part.scale_log2, l);
+                constexpr int EC = D / PARTS, W = EC < 32 ? EC : 32;
 #pragma unroll 1
-                for (int c = 0; c < D / 64; ++c) {
-                    uint32_t o[32];
-                    const int col = half * (D / 2) + c * 32;
-                    tmem_ld32(tmem_base + lane_addr + col, o);
-                    tmem_wait_ld();
-                    if (c == D / 64 - 1) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0 && w.n > 0) mbar_arrive_cluster(leader_ofree);
-                    }
+                for (int c = 0; c < EC; c += W) {
+                    uint32_t o[W];
+                    take(me * EC + c, o);
+                    if (c + W == EC) release();
                     if (row_live) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) st_global_v8(partial8(part, slot, D, (int)rank * 128 + row, col + 8 * i), *reinterpret_cast<const uint32_t(*)[8]>(o + 8 * i));
+                        for (int i = 0; i < W; i += 8) st_global_v8(partial8(part, slot, D, (int)rank * 128 + row, me * EC + c + i), *reinterpret_cast<const uint32_t(*)[8]>(o + i));
                     }
                 }
-                asm volatile("bar.sync 1, 256;" ::: "memory");        // every thread has read the sums before the next unit's maxima land there
-                if (w.k0 == 0 && threadIdx.x == 64 && rank == 0) {
+                asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");        // every thread has read the sums before the next unit's maxima land there
+                if (w.k0 == 0 && tid == 0 && rank == 0) {
                     const int f = 2 * w.u.tile * rows_here;
-                    PageSplit m2 = {s.b, s.row0, f, min(2 * rows_here, s.n * G - f), w.u.h, page_owner(w.u.at + w.u.cost - 1, total, nc), rows_here, 0};
+                    PageSplit m2 = {s.b, s.row0, f, min(2 * rows_here, s.n * G - f), w.u.h, shares.owner(w.u.at + w.u.cost - 1), rows_here, 0};
                     part.meta[pair] = m2;
                 }
             } else {
                 // O / l, 64 columns at a time through the two halves of the staging area, then whole 128-byte pieces of rows to memory
-                size_t dst[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int r = (tid >> 3) + 32 * k, t = token0 + r / G;
-                    dst[k] = unit_live && r < rows_here && t < s.n ? ((size_t)(s.row0 + t) * p.g.Hq + w.u.h * G + r % G) * D + (tid & 7) * 8 : ~(size_t)0;
-                }
+                constexpr int SC = 64 / PARTS;          // columns of a thread
+                __nv_bfloat16 *tile_out = (__nv_bfloat16 *)p.out + ((size_t)(s.row0 + token0) * p.g.Hq + w.u.h * G) * D;
 #pragma unroll 1
                 for (int rnd = 0; rnd < D / 64; ++rnd) {
-                    uint32_t o[32];
-                    tmem_ld32(tmem_base + lane_addr + rnd * 64 + half * 32, o);
-                    tmem_wait_ld();
-                    if (rnd == D / 64 - 1) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0 && w.n > 0) mbar_arrive_cluster(leader_ofree);
-                    }
+                    uint32_t o[SC];
+                    take(rnd * 64 + me * SC, o);
+                    if (rnd == D / 64 - 1) release();
                     uint8_t *srow = smem + L::OFF_STAGE + (rnd & 1) * (128 * 128) + row * 128;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
+                    for (int c = 0; c < SC / 8; ++c) {
                         float f[8];
 #pragma unroll
                         for (int k = 0; k < 8; ++k) f[k] = inv == 0.f ? 0.f : __uint_as_float(o[8 * c + k]) * inv;      // (the accumulator of a unit without keys was never written)
-                        *reinterpret_cast<uint4 *>(srow + (((half * 4 + c) ^ (row & 7)) << 4)) =
+                        *reinterpret_cast<uint4 *>(srow + (((me * (SC / 8) + c) ^ (row & 7)) << 4)) =
                             make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
                     }
-                    asm volatile("bar.sync 1, 256;" ::: "memory");
+                    asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int r = (tid >> 3) + 32 * k;
-                        if (dst[k] != ~(size_t)0)
-                            *reinterpret_cast<uint4 *>((__nv_bfloat16 *)p.out + dst[k] + rnd * 64) =
+                    for (int k = 0; k < 128 / RP; ++k) {
+                        const int r = k * RP + (tid >> 3);
+                        if (r < live_rows)
+                            *reinterpret_cast<uint4 *>(tile_out + out_at[k] + rnd * 64) =
                                 *reinterpret_cast<const uint4 *>(smem + L::OFF_STAGE + (rnd & 1) * (128 * 128) + r * 128 + (((tid & 7) ^ (r & 7)) << 4));
                     }
                 }
-                if (D == 64) asm volatile("bar.sync 1, 256;" ::: "memory");      // (one round: its half, and the sums, may not be overwritten before they are read)
+                if (D == 64) asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");      // (one round: its half, and the sums, may not be overwritten before they are read)
             }
             if (w.n > 0) ++ui;
         } while (step(w));
@@ -624,7 +692,7 @@ static cudaError_t launch_chunk(const PageAttention &a, const PagePartials &part
     if (!encode_map_bf16(&tq, a.qry, 3, qd, qs, qb) || !encode_map_bf16(&tk, k, 2, kd, ks, kb) || !encode_map_bf16(&tv, v, 2, kd, ks, kb)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(2 * pairs));
-    cfg.blockDim = dim3(kChunkThreads);
+    cfg.blockDim = dim3(L::THREADS);
     cfg.dynamicSmemBytes = L::TOTAL;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];

@@ -73,6 +73,7 @@ template <int ROWS>
 struct TokSpanOf {
     const PageAttention &p;
     int G;
+    __device__ __forceinline__ int tiles(const PageSeq &s) const { return (s.n * G + ROWS - 1) / ROWS; }
     __device__ __forceinline__ TokSpan operator()(const PageSeq &s, int tile) const
     {
         const PageRange r = page_range(s, p, tile * ROWS / G, (min(s.n * G, (tile + 1) * ROWS) - 1) / G);
@@ -99,24 +100,24 @@ page_token_kernel(const PageAttention p, const PagePartials part)
     const int G = g.Hq / g.Hkv;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    const TokSpanOf<ROWS> span_of{p, G};
-    const PageLine<TokSpanOf<ROWS>> line{p, span_of, ROWS, G};
+    const PageLine<TokSpanOf<ROWS>> line{p, {p, G}};
     int longest;
-    const long long total = line.total(lane, longest);
+    const int total = line.total(lane, longest);
     // No more CTAs than leave each the square root of a tenth of the longest unit: a partial costs the merge a tenth of what a block costs here.
     const int least = max(1, (int)sqrtf((float)longest * 0.1f));
-    const int nc = (int)min((long long)gridDim.x, (total + least - 1) / least);
+    const int nc = min((int)gridDim.x, (total + least - 1) / least);
     const int cta = blockIdx.x;
     if (threadIdx.x == 0) part.meta[cta].b = -1;
     if (cta >= nc) return;
-    const long long x0 = page_share(cta, total, nc), x1 = page_share(cta + 1, total, nc);
+    const PageShares shares(total, nc);
+    const int x0 = shares.of(cta), x1 = shares.of(cta + 1);
     auto u = line.find(x0, lane);
 
-    for (long long x = x0; x < x1;) {
+    for (int x = x0; x < x1;) {
         const PageSeq s = u.s;
         const TokSpan span = u.sp;
         const int rt = u.tile, h = u.h, b = s.b;
-        const int k0 = (int)(x - u.at), k1 = (int)min((long long)u.cost, x1 - u.at);
+        const int k0 = x - u.at, k1 = min(u.cost, x1 - u.at);
         const int kend = min(k1, span.count);
         // ---- Q of the unit's rows, in the order of K's pieces ----
         __syncthreads();             // (the last unit's results and Q have been read)
@@ -424,7 +425,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
             }
         }
         if (starts && !ends && threadIdx.x == 0) {
-            PageSplit m2 = {b, s.row0, rt * ROWS, min(ROWS, s.n * G - rt * ROWS), h, page_owner(u.at + u.cost - 1, total, nc), ROWS, 0};
+            PageSplit m2 = {b, s.row0, rt * ROWS, min(ROWS, s.n * G - rt * ROWS), h, shares.owner(u.at + u.cost - 1), ROWS, 0};
             part.meta[cta] = m2;
         }
         x = u.at + k1;

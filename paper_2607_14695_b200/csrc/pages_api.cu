@@ -235,6 +235,10 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)d.d);
     const int G = d.Hq / d.Hkv;
     const long long per_seq = ((long long)n_rows * G + batch->B - 1) / batch->B;           // (token, head) rows of a sequence and KV head
+    // (the tensor-core kernels count tiles of rows times blocks of 64 keys in 32 bits)
+    if (page_chunk_takes(d.dtype, G, d.d) &&
+        ((double)n_rows * G / 8 + batch->B) * d.Hkv * ((double)batch->max_pages * d.page / 64 + 2) > 2.0e9)
+        return api_fail(REFLEX_ERR_SHAPE, "n_rows=%d, B=%d and max_pages=%d: more tiles of rows and keys than 31 bits count", n_rows, batch->B, batch->max_pages);
     cudaStream_t st = (cudaStream_t)stream;
     const PagesLayout w = pages_layout(d);
     PagePartials part;
