@@ -39,7 +39,10 @@ constexpr int kChunkPoly = 2;                  // of every 8 pairs of exponentia
 
 __device__ __forceinline__ void report_page_wait(uint32_t *status, uint32_t code) { atomicCAS(status, 0u, status_word(kSitePages + code)); }
 
-struct ChunkSpan { int tile0, count, hi; };    // key tiles [tile0, tile0 + count), keys below hi
+// A unit costs kChunkSetUp blocks before its first tile: what its Q, its masks and its results take, in tiles. (A share that ends among them
+// leaves the unit to the next pair.)
+constexpr int kChunkSetUp = 4;
+struct ChunkSpan { int tile0, tiles, hi, count; };    // key tiles [tile0, tile0 + tiles), keys below hi; blocks
 struct ChunkSpanOf {
     const PageAttention &p;
     int tokens;                                // of a unit
@@ -50,7 +53,8 @@ struct ChunkSpanOf {
         ChunkSpan c;
         c.tile0 = r.lo / kChunkKeys;
         c.hi = r.hi;
-        c.count = r.hi > r.lo ? (r.hi + kChunkKeys - 1) / kChunkKeys - c.tile0 : 0;
+        c.tiles = r.hi > r.lo ? (r.hi + kChunkKeys - 1) / kChunkKeys - c.tile0 : 0;
+        c.count = kChunkSetUp + max(1, c.tiles);
         return c;
     }
 };
@@ -76,8 +80,8 @@ template <int HD, int D> struct Chunk {
     static constexpr uint32_t OFF_BAR = OFF_STAGE + 2 * 128 * 128;
     static constexpr uint32_t OFF_MAX = OFF_BAR + BAR_BYTES;          // [2 tiles][128 rows][2 halves] maxima of the logits
     static constexpr uint32_t OFF_REF = OFF_MAX + 2 * 128 * 2 * 4;    // [128] reference maxima, from group to group (two groups only)
-    static constexpr uint32_t OFF_SUM = OFF_REF + (NG - 1) * 128 * 4; // [2 NG][128] (reference, sum) at the end of a unit; one group: in the maxima's place
-    static constexpr uint32_t NEED = NG == 1 ? OFF_REF : OFF_SUM + 2 * NG * 128 * 8;
+    static constexpr uint32_t OFF_SUM = OFF_STAGE + 128 * 128;        // [2 NG][128] (reference, sum) at the end of a unit, where the results' second 64 columns go later
+    static constexpr uint32_t NEED = OFF_REF + (NG - 1) * 128 * 4;
     static constexpr uint32_t TOTAL = NEED + 1024 > 232448 ? 232448 : NEED + 1024;
     static_assert(NEED <= TOTAL, "shared memory");
 };
@@ -160,19 +164,19 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const bool works = pair < nc;
     const PageShares shares(total, max(1, nc));
     const int x0 = works ? shares.of(pair) : 0, x1 = works ? shares.of(pair + 1) : 0;
-    // This pair's units, one after the other: blocks [k0, k1) of unit u, of which `n` are tiles of keys, from tile `t0` on.
-    struct Slice { typename PageLine<ChunkSpanOf>::Place u; int k0, k1, t0, n; };
+    // This pair's units, one after the other: tiles [k0, k1) of unit u (one at least, if only in name), `n` of keys, from tile `t0` on; x: where in the line it goes on
+    struct Slice { typename PageLine<ChunkSpanOf>::Place u; int k0, k1, t0, n, x; };
     auto cut = [&](Slice &w, int x) {
-        w.k0 = x - w.u.at;
-        w.k1 = min(w.u.cost, x1 - w.u.at);
+        w.x = min(w.u.at + w.u.cost, x1);
+        w.k0 = max(0, x - w.u.at - kChunkSetUp);
+        w.k1 = max(0, w.x - w.u.at - kChunkSetUp);
         w.t0 = w.u.sp.tile0 + w.k0;
-        w.n = max(0, min(w.k1, w.u.sp.count) - w.k0);
+        w.n = max(0, min(w.k1, w.u.sp.tiles) - w.k0);
     };
     auto step = [&](Slice &w) -> bool {      // to the next unit of the share
-        const int x = w.u.at + w.k1;
-        if (x >= x1) return false;
+        if (w.x >= x1) return false;
         line.next(w.u);
-        cut(w, x);
+        cut(w, w.x);
         return true;
     };
     Slice w0;
@@ -288,65 +292,57 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             const uint64_t vdesc0 = umma_desc_sw128(base + L::OFF_V, 128 * 128, 1024);
             // Q K^T of tile `q` and P V of tile `v`, up to AHEAD tiles behind it. (The logits of tile g + NS go where the weights of tile g are: Q K^T of the one is
             // issued behind P V of the other.) What a tile is comes with its keys; this warp shares its scheduler with busy ones, and walking the
-            // list of units here took 1200 cycles a tile.
+            // list of units here took 1200 cycles a tile. Everything that an MMA is issued with is kept uniform (votes and reductions say so to the
+            // compiler), or each of its operands is moved to the uniform registers anew.
+            auto all = [&](bool good) -> bool { return __all_sync(0xffffffffu, good); };
+            const uint32_t tm = __reduce_or_sync(0xffffffffu, tmem_base);
+            const uint32_t q_lo = (uint32_t)qdesc0, k_lo = (uint32_t)kdesc0, v_lo = (uint32_t)vdesc0, d_hi = (uint32_t)(qdesc0 >> 32), v_hi = (uint32_t)(vdesc0 >> 32);
             bool ok = true, end = false;
-            int q = 0, v = 0, uq = 0, uv = 0;
+            int q = 0, v = 0, uq = 0, uv = 0;                          // tiles, and units begun
+            int q_st = 0, q_buf = 0, v_st = 0, v_buf = 0;              // ... their stages and buffers
+            uint32_t q_sph = 0u, v_bph = 0u;                           // parities of KFULL of tile q and PFULL of tile v
             while (ok) {
-                while (!end && q <= v + AHEAD) {
-                    const int st = q % NST, buf = q % NS;
-                    ok = wait(L::KFULL + st, (uint32_t)(q / NST) & 1u, 4);
+                // A tile whose weights are there goes first: the end of a unit waits for nothing else.
+                while (!end && q <= v + AHEAD && (q == v || !all(mbar_test_wait(bar(L::PFULL + v_buf), v_bph)))) {
+                    ok = all(wait(L::KFULL + q_st, q_sph, 4));
                     if (!ok) break;
-                    const uint32_t info = tile_info[q & 15];
+                    const uint32_t info = __reduce_or_sync(0xffffffffu, tile_info[q & 15]);
                     end = (info & kEnd) != 0u;
                     if (end) break;
                     if (info & kFirst) {
                         // a unit whose Q has not come yet does not hold up the products of the last one
-                        if (q > v) { if (!mbar_test_wait(bar(L::QFULL), (uint32_t)uq & 1u)) break; }
-                        else { ok = wait(L::QFULL, (uint32_t)uq & 1u, 5); if (!ok) break; }
+                        if (q > v) { if (!all(mbar_test_wait(bar(L::QFULL), (uint32_t)uq & 1u))) break; }
+                        else { ok = all(wait(L::QFULL, (uint32_t)uq & 1u, 5)); if (!ok) break; }
                         ++uq;
                     }
                     tc_fence_after();
-                    uint64_t qd = qdesc0, kd = kdesc0;
-                    umma_desc_advance(kd, (uint32_t)st * L::K_STAGE);
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
-                        umma2_ss_elect(tmem_base + kColS + buf * kChunkKeys, qd, kd, idesc_qk, kk > 0 ? 1u : 0u);
-                        umma_desc_advance(qd, (kk & 3) == 3 ? 128 * 128 - 96 : 32);
-                        umma_desc_advance(kd, (kk & 3) == 3 ? 64 * 128 - 96 : 32);
-                    }
-                    umma2_commit_mc_elect(bar(L::SFULL + buf), both);
-                    umma2_commit_mc_elect(bar(L::KEMPTY + st), both);
+                    for (int ch = 0; ch < CH; ++ch)
+                        umma2_ss4_elect(tm + kColS + q_buf * kChunkKeys, q_lo + ch * (128 * 128 / 16), d_hi, k_lo + (uint32_t)q_st * (L::K_STAGE / 16) + ch * (64 * 128 / 16), d_hi, idesc_qk, ch > 0 ? 1u : 0u);
+                    umma2_commit_mc_elect(bar(L::SFULL + q_buf), both);
+                    umma2_commit_mc_elect(bar(L::KEMPTY + q_st), both);
                     if (info & kLast) umma2_commit_mc_elect(bar(L::QEMPTY), both);
                     ++q;
+                    if (++q_st == NST) { q_st = 0; q_sph ^= 1u; }
+                    if (++q_buf == NS) q_buf = 0;
                 }
                 if (!ok || q == v) break;
-                const int st = v % NST, buf = v % NS;
-                const uint32_t info = tile_info[v & 15];
-                uint64_t vd = vdesc0;
-                umma_desc_advance(vd, (uint32_t)st * L::V_STAGE);
-                ok = wait(L::PFULL + buf, (uint32_t)(v / NS) & 1u, 6);
+                const uint32_t info = __reduce_or_sync(0xffffffffu, tile_info[v & 15]);
+                ok = all(wait(L::PFULL + v_buf, v_bph, 6));
                 if (ok && (info & kFirst)) {
-                    if (uv >= 1) ok = wait(L::OFREE, (uint32_t)(uv - 1) & 1u, 7);
+                    if (uv >= 1) ok = all(wait(L::OFREE, (uint32_t)(uv - 1) & 1u, 7));
                     ++uv;
                 }
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t p_tmem = tmem_base + kColS + buf * kChunkKeys, later = (info & kFirst) ? 0u : 1u;
-#pragma unroll
-                for (int kk = 0; kk < 4; ++kk) {
-                    umma2_ts_elect(tmem_base, p_tmem + kk * 8, vd, idesc_pv, kk > 0 ? 1u : later);
-                    umma_desc_advance(vd, 16 * 128);
-                }
-                if (info & kSecond) {              // (else its weights are zero and its V was never loaded)
-#pragma unroll
-                    for (int kk = 4; kk < 8; ++kk) {
-                        umma2_ts_elect(tmem_base, p_tmem + 64 + (kk & 3) * 8, vd, idesc_pv, 1u);
-                        umma_desc_advance(vd, 16 * 128);
-                    }
-                }
+                const uint32_t p_tmem = tm + kColS + v_buf * kChunkKeys, v_at = v_lo + (uint32_t)v_st * (L::V_STAGE / 16);
+                umma2_ts4_elect(tm, p_tmem, v_at, v_hi, idesc_pv, (info & kFirst) ^ kFirst);
+                if (info & kSecond) umma2_ts4_elect(tm, p_tmem + 64, v_at + 64 * 128 / 16, v_hi, idesc_pv, 1u);       // (else its weights are zero and its V was never loaded)
                 umma2_commit_mc_elect(bar(L::PVDONE + (v & 3)), both);
-                umma2_commit_mc_elect(bar(L::VEMPTY + st), both);
+                umma2_commit_mc_elect(bar(L::VEMPTY + v_st), both);
                 ++v;
+                if (++v_st == NST) v_st = 0;
+                if (++v_buf == NS) { v_buf = 0; v_bph ^= 1u; }
             }
         }
     } else if (works && warp >= 4) {
@@ -357,7 +353,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         const uint32_t leader_pfull = mapa(bar(L::PFULL), 0), leader_ofree = mapa(bar(L::OFREE), 0);
         float *maxima = reinterpret_cast<float *>(smem + L::OFF_MAX);
         float *ref = reinterpret_cast<float *>(smem + L::OFF_REF);
-        float2 *sums = reinterpret_cast<float2 *>(smem + (NG == 1 ? L::OFF_MAX : L::OFF_SUM));
+        float2 *sums = reinterpret_cast<float2 *>(smem + L::OFF_SUM);
         const int rows_here = tile_tokens * G;
         const int tid = threadIdx.x - 128;
         const float sc = part.scale_log2;
@@ -377,12 +373,13 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         // arrived there, too, with its last tile (for the first tile of all: here).
         if (NG == 2 && group == 1) asm volatile("bar.arrive %0, 128;" ::"r"(1 + quarter) : "memory");
         do {
+            if (w.k1 == 0) continue;             // the share ends before the unit's first tile
             const PageSeq &s = w.u.s;
             const int token0 = (2 * w.u.tile + (int)rank) * tile_tokens;         // first of this CTA's rows
             const int t_row = token0 + row_token, live_rows = min(rows_here, (s.n - token0) * G);
             const bool row_live = row < live_rows;
             const PageRange mine = page_range(s, p, min(t_row, s.n - 1), min(t_row, s.n - 1));
-            const bool whole = w.k0 == 0 && w.k1 == w.u.cost;
+            const bool whole = w.k0 == 0 && w.k1 == w.u.cost - kChunkSetUp;
             // keys that every row of the pair sees (either CTA's V meets the rows of both)
             const int all_lo = page_range(s, p, min(s.n, 2 * (w.u.tile + 1) * tile_tokens) - 1, 0).lo, all_hi = page_range(s, p, 0, 2 * w.u.tile * tile_tokens).hi;
             const int slot = 2 * pair + (w.k0 == 0 ? 1 : 0);
@@ -541,7 +538,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (bad_unit[ui & 7] == (uint32_t)ui + 1u || !ok) l = __int_as_float(0x7fc00000);
             }
             // the row's sum: the groups' references may differ, the latest one is the largest
-            if (NG == 1) asm volatile("bar.sync 9, 256;" ::: "memory");         // (the sums take the maxima's place)
+            if (w.n == 0) asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");        // (the last unit's results may still be on their way out of there; else the tiles' weights have kept all warps together)
             sums[(group * 2 + half) * 128 + row] = make_float2(m_ref, l);
             asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");
             {

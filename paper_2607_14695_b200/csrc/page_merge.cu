@@ -1,6 +1,6 @@
 // Joins the partial results of units that several CTAs have worked on: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i, in an order that the
 // units alone decide. A thread takes 8 columns of a row (partials lie as [column group][row][8], so a warp reads a contiguous kilobyte) and has
-// the loads of 8 partials in flight; long lists (one sequence over the whole device) are cut in 8 among the warps of a block, which then add up.
+// the loads of 4 partials in flight; long lists (one sequence over the whole device) are cut in 8 among the warps of a block, which then add up.
 //
 // It also computes again, row by row, the sequences that the tensor-core kernel has marked (see PagePartials::careful).
 #include "page_plain.cuh"
@@ -20,11 +20,11 @@ __device__ __forceinline__ void merge_list(const PagePartials &part, int d, int 
     a.m = -INFINITY; a.l = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) a.o[e] = 0.f;
-    for (int i0 = first; i0 < n; i0 += 8 * step) {
-        float4 v[8][2];
-        float2 ml[8];
+    for (int i0 = first; i0 < n; i0 += 4 * step) {
+        float4 v[4][2];
+        float2 ml[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 4; ++j) {
             const int i = i0 + j * step;
             if (i < n) {
                 ml[j] = part.ml[slot(i) * part.rows + r];
@@ -34,14 +34,14 @@ __device__ __forceinline__ void merge_list(const PagePartials &part, int d, int 
         }
         float top = a.m;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, ml[j].x);
         const float old = a.m == -INFINITY ? 0.f : ptx::ex2(a.m - top);
         a.l *= a.m == -INFINITY ? 1.f : old;             // (0, or the NaN of a part that went wrong)
 #pragma unroll
         for (int e = 0; e < 8; ++e) a.o[e] *= old;
         a.m = top;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 4; ++j) {
             const float w = ml[j].x == -INFINITY ? 0.f : ptx::ex2(ml[j].x - top);
             a.l += ml[j].y * w;
             if (w == 0.f) continue;                     // (what a part that has seen nothing left there is not looked at)
@@ -53,7 +53,7 @@ __device__ __forceinline__ void merge_list(const PagePartials &part, int d, int 
 }
 
 template <int FMT>
-__global__ void __launch_bounds__(kMergeThreads)
+__global__ void __launch_bounds__(kMergeThreads, 4)
 page_merge_kernel(const PageAttention p, const PagePartials part, int ctas)
 {
     __shared__ int first_s[kMergeMost + 1];        // first piece of work of each unit that was split (by the CTA that began it)
@@ -62,32 +62,47 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int ctas)
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int d = p.g.d, groups = d >> 3, G = p.g.Hq / p.g.Hkv;
     // pieces: 256 (row, column group) items of a unit; 32 where its list of partials is cut
-    auto pieces_of = [&](int c) -> int {
-        const PageSplit &m = part.meta[c];
-        if (m.b < 0 || part.careful[m.b]) return 0;
-        const int items = m.rows * groups, per = m.last - c + 1 > kMergeLong ? 32 : 256;
-        return (items + per - 1) / per;
-    };
     // (sequences are marked before this kernel, and the marks go when its last block is done: all blocks see the same)
     bool marked = false;
     for (int b = tid; b < p.q.B; b += kMergeThreads) marked |= part.careful[b] != 0;
-    const bool any_marked = __syncthreads_or(marked);
-    if (warp == 0) {
-        int at = 0;
-        for (int c0 = 0; c0 < ctas; c0 += 32) {
-            const int n = c0 + lane < ctas ? pieces_of(c0 + lane) : 0;
-            int incl = n;
+    int pieces[kMergeMost / kMergeThreads];
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, incl, o);
-                if (lane >= o) incl += y;
+    for (int k = 0; k < kMergeMost / kMergeThreads; ++k) {
+        const int c = tid * (kMergeMost / kMergeThreads) + k;
+        pieces[k] = 0;
+        if (c < ctas) {
+            const PageSplit m = part.meta[c];
+            if (m.b >= 0 && !part.careful[m.b]) {
+                const int per = m.last - c + 1 > kMergeLong ? 32 : 256;
+                pieces[k] = (m.rows * groups + per - 1) / per;
             }
-            if (c0 + lane < ctas) first_s[c0 + lane] = at + incl - n;
-            at += __shfl_sync(0xffffffffu, incl, 31);
         }
-        if (lane == 0) first_s[ctas] = at;
     }
-    __syncthreads();
+    const bool any_marked = __syncthreads_or(marked);
+    {
+        const int mine = pieces[0] + pieces[1];
+        int incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += y;
+        }
+        int *sum_s = reinterpret_cast<int *>(scratch);
+        if (lane == 31) sum_s[warp] = incl;
+        __syncthreads();
+        int before = 0, all = 0;
+#pragma unroll
+        for (int q = 0; q < kMergeThreads / 32; ++q) {
+            if (q < warp) before += sum_s[q];
+            all += sum_s[q];
+        }
+        static_assert(kMergeMost == 2 * kMergeThreads, "two entries a thread");
+        first_s[2 * tid] = before + incl - mine;
+        first_s[2 * tid + 1] = before + incl - mine + pieces[0];
+        if (tid == 0) first_s[kMergeMost] = all;
+        if (ctas < kMergeMost && tid == 0) first_s[ctas] = all;
+        __syncthreads();
+    }
     for (int w = blockIdx.x; w < first_s[ctas]; w += gridDim.x) {
         int lo = 0, hi = ctas;                      // first_s[lo] <= w < first_s[hi]
         while (hi - lo > 1) {
@@ -150,7 +165,7 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int ctas)
 cudaError_t launch_page_merge(const PageAttention &a, const PagePartials &part, int ctas, int format, int sm_count, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(2 * sm_count));
+    cfg.gridDim = dim3((unsigned)(4 * sm_count));
     cfg.blockDim = dim3(kMergeThreads);
     cfg.stream = st;
     cudaLaunchAttribute attr;

@@ -494,6 +494,44 @@ __device__ __forceinline__ void umma2_commit_mc_elect(uint32_t bar, uint16_t cta
         ::"r"(bar), "h"(cta_mask)
         : "memory");
 }
+// Four MMAs of a chain for a warp that runs converged, 32 bytes (16 columns of a 64-column chunk) apart in A and B: one election, and nothing between
+// the instructions but an add to the low word of either descriptor. (As four calls of umma2_ss_elect beside four busy warps of the same
+// scheduler an instruction took 85 cycles to issue instead of 64.)
+__device__ __forceinline__ void umma2_ss4_elect(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q, t;\n\t.reg .b64 a, b;\n\t.reg .b32 x, y;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "mov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, p;\n\t"
+        "add.u32 x, %1, 2;\n\tadd.u32 y, %3, 2;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, t;\n\t"
+        "add.u32 x, %1, 4;\n\tadd.u32 y, %3, 4;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, t;\n\t"
+        "add.u32 x, %1, 6;\n\tadd.u32 y, %3, 6;\n\tmov.b64 a, {x, %2};\n\tmov.b64 b, {y, %4};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, t;\n\t}"
+        ::"r"(tmem_d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// ... with A in tensor memory, 8 columns (16 keys) apart, and B 16 rows of 128 bytes
+__device__ __forceinline__ void umma2_ts4_elect(uint32_t tmem_d, uint32_t tmem_a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p, q, t;\n\t.reg .b64 b;\n\t.reg .b32 x, y;\n\t"
+        "setp.ne.b32 p, %5, 0;\n\tsetp.eq.b32 t, 0, 0;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "mov.b64 b, {%2, %3};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], b, %4, p;\n\t"
+        "add.u32 x, %1, 8;\n\tadd.u32 y, %2, 128;\n\tmov.b64 b, {y, %3};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], [x], b, %4, t;\n\t"
+        "add.u32 x, %1, 16;\n\tadd.u32 y, %2, 256;\n\tmov.b64 b, {y, %3};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], [x], b, %4, t;\n\t"
+        "add.u32 x, %1, 24;\n\tadd.u32 y, %2, 384;\n\tmov.b64 b, {y, %3};\n\t"
+        "@q tcgen05.mma.cta_group::2.kind::f16 [%0], [x], b, %4, t;\n\t}"
+        ::"r"(tmem_d), "r"(tmem_a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
 // A operand in tensor memory (each CTA's own 128 rows; a 32-bit column holds two consecutive bf16 of the K axis)
 __device__ __forceinline__ void umma2_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, uint32_t accumulate)
 {
