@@ -11,7 +11,8 @@
 //                has four of its warps. The threads of a row agree on the reference maximum at one named barrier per 32 rows, where the group
 //                that has had the tile before leaves the row's reference, too; O is rescaled only where it has grown by more than 2^8.
 // What bounds it: at head_dim 256 the tensor pipe (2048 cycles a tile; operand reads then take two thirds of the shared memory's bandwidth), at 128 and
-// 64 the softmax (16 K exponentials a tile and SM, some 1000 issue slots a scheduler). Heads of 64 run as heads of 128 whose upper chunk is left out of
+// 64 the softmax (some 700 issue slots a scheduler and tile, which the helper warps need as well; a quarter of the exponentials by a
+// polynomial instead of the special-function unit cost more of them than the unit saved: 310 us for 301 at 4 x 4160 causal tokens, 16 heads of 128). Heads of 64 run as heads of 128 whose upper chunk is left out of
 // Q K^T and whose upper columns of O are never read: P V costs twice, underneath the softmax.
 //
 // The grid is one pair per SM pair; the tiles of all units form one line that the pairs share evenly (PageLine), so uneven sequences, causal masks and single
@@ -35,7 +36,6 @@ constexpr int kChunkKeys = 128;
 constexpr int kChunkRows = 256;                // of a unit
 constexpr unsigned long long kChunkWaitNs = 1000000000ull;
 constexpr float kChunkGrow = 8.0f;             // log2 units: O is rescaled only where a maximum grows by more than 2^8
-constexpr int kChunkPoly = 2;                  // of every 8 pairs of exponentials, how many go through the FMA pipe
 
 __device__ __forceinline__ void report_page_wait(uint32_t *status, uint32_t code) { atomicCAS(status, 0u, status_word(kSitePages + code)); }
 
@@ -423,7 +423,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                         mx = max_nan_f32(max_nan_f32(mx4[0], mx4[1]), max_nan_f32(mx4[2], mx4[3]));
                         if (NG == 2) tmem_ld32(s_addr + (c == 0 ? 32 : 0), r[0]);
                     }
-                    if (!(mx < INFINITY)) l = __int_as_float(0x7fc00000);      // (a logit that is NaN or +inf; the polynomial below would lose it)
+                    if (!(mx < INFINITY)) l = __int_as_float(0x7fc00000);      // (a logit that is NaN or +inf)
                 }
                 maxima[((gi & 1) * 128 + row) * 2 + half] = mx;
                 asm volatile("bar.sync %0, %1;" ::"r"(1 + quarter + 4 * group), "n"(64 * NG) : "memory");
@@ -482,14 +482,12 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if constexpr (!DEAD) {
                     const float mr = m_ref == -INFINITY ? 0.f : m_ref * sc;
                     const uint64_t sc2 = pack_f32x2(sc, sc), nm2 = pack_f32x2(-mr, -mr);
-                    const Ex2PolyConsts pk = ex2_poly_consts();
                     uint64_t sum2[2] = {0ull, 0ull};
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         if (NG == 2) tmem_wait_ld();
                         uint32_t (&v)[32] = r[NG == 1 ? c : 0];
                         const uint32_t bits = (uint32_t)(mask >> (32 * c));
-                        uint64_t part2[2] = {0ull, 0ull};
                         uint32_t packed[16];
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
@@ -499,18 +497,11 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                             }
                             float x0, x1, p0, p1;
                             unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), sc2, nm2), x0, x1);
-                            if (((i >> 1) & 7) < kChunkPoly) ex2_poly_f32x2(x0, x1, pk, p0, p1);
-                            else { p0 = ex2(x0); p1 = ex2(x1); }
-                            part2[(i >> 1) & 1] = add_f32x2(part2[(i >> 1) & 1], pack_f32x2(p0, p1));
+                            p0 = ex2(x0); p1 = ex2(x1);
+                            sum2[(i >> 1) & 1] = add_f32x2(sum2[(i >> 1) & 1], pack_f32x2(p0, p1));
                             packed[i >> 1] = pack_bf16(p0, p1);
-                            // (the polynomial gives a masked key 2^-125: nothing for the sum, but its weight must be exactly 0)
-                            if (!FULL && ((i >> 1) & 7) < kChunkPoly) packed[i >> 1] &= ((bits >> i) & 1u ? 0x0000FFFFu : 0u) | ((bits >> i) & 2u ? 0xFFFF0000u : 0u);
                         }
                         if (NG == 2 && c == 0) tmem_ld32(s_addr + 32, r[0]);
-                        if (FULL || bits != 0u) {              // (a row that sees nothing has no sum)
-                            sum2[0] = add_f32x2(sum2[0], part2[0]);
-                            sum2[1] = add_f32x2(sum2[1], part2[1]);
-                        }
                         // (weights of keys 32 c .. of the half take the columns of its logits 16 c ..: read, and by this thread alone)
                         tmem_st16(s_addr + 16 * c, packed);
                     }
