@@ -47,43 +47,44 @@ struct PageShares {
 };
 
 // SPAN: tiles(s) of a sequence; (s, tile) gives a struct with .count (blocks). Functions that take `lane`: whole warps, all lanes get the same.
+// A warp works on 32 sequences at a time; with fewer, `width` lanes share one. The first 32 (or all) are kept in registers.
 template <typename SPAN>
 struct PageLine {
     const PageAttention &p;
     const SPAN span;
+    int width, longest;              // lanes of a sequence; the longest unit
+    PageSeq mine;                    // sequence lane / width
+    int mine_cost;                   // its blocks, in the first of its lanes (0 in the others)
 
-    // With few sequences several lanes share one: width() of them.
-    __device__ __forceinline__ int width() const
-    {
-        int w = 32;
-        while (w > 1 && p.q.B * w > 32) w >>= 1;
-        return w;
-    }
-    // the blocks of sequence b0 + lane / w (0 behind the last one), in all its w lanes
-    __device__ __forceinline__ int seq_cost(int b0, int w, int lane, int &longest) const
+    // blocks of the sequence that `width` lanes hold, in the first of them
+    __device__ __forceinline__ int seq_cost(const PageSeq &s, int lane, int &longest_) const
     {
         int cost = 0;
-        if (b0 + lane / w < p.q.B) {
-            const PageSeq s = page_seq(p, b0 + lane / w);
-            const int n = span.tiles(s);
-            for (int t = lane & (w - 1); t < n; t += w) {
-                const int c = max(1, span(s, t).count);
-                cost += c;
-                longest = max(longest, c);
-            }
+        const int n = span.tiles(s);
+        for (int t = lane & (width - 1); t < n; t += width) {
+            const int c = max(1, span(s, t).count);
+            cost += c;
+            longest_ = max(longest_, c);
         }
-        for (int o = 1; o < w; o <<= 1) cost += __shfl_xor_sync(0xffffffffu, cost, o);
-        return cost * p.g.Hkv;
+        for (int o = 1; o < width; o <<= 1) cost += __shfl_xor_sync(0xffffffffu, cost, o);
+        return (lane & (width - 1)) == 0 ? cost * p.g.Hkv : 0;
     }
-    __device__ __forceinline__ int total(int lane, int &longest) const
+    __device__ __forceinline__ PageSeq seq_of(int b) const
     {
-        const int w = width();
-        int sum = 0;
+        PageSeq s = {b, 0, 0, 0};
+        if (b < p.q.B) s = page_seq(p, b);
+        return s;
+    }
+    // the length of the line
+    __device__ __forceinline__ int begin(int lane)
+    {
+        width = 32;
+        while (width > 1 && p.q.B * width > 32) width >>= 1;
+        mine = seq_of(lane / width);
         longest = 1;
-        for (int b0 = 0; b0 < p.q.B; b0 += 32 / w) {
-            const int c = seq_cost(b0, w, lane, longest);
-            sum += (lane & (w - 1)) == 0 ? c : 0;
-        }
+        mine_cost = seq_cost(mine, lane, longest);
+        int sum = mine_cost;
+        for (int b0 = 32; b0 < p.q.B; b0 += 32) sum += seq_cost(seq_of(b0 + lane), lane, longest);
         longest = __reduce_max_sync(0xffffffffu, longest);
         return __reduce_add_sync(0xffffffffu, sum);
     }
@@ -103,26 +104,30 @@ struct PageLine {
         }
         return c;
     }
-    // the unit that block x (< total) belongs to
+    // the unit that block x (< the line's length) belongs to
     __device__ __forceinline__ Place find(int x, int lane) const
     {
         Place u;
-        const int w = width();
-        int unused = 0, b = 0;
         u.at = 0;
-        for (int b0 = 0; b0 < p.q.B; b0 += 32 / w) {
-            const int c = (lane & (w - 1)) == 0 || w == 1 ? 1 : 0, cost = seq_cost(b0, w, lane, unused) * c;
+        PageSeq s = mine;
+        int cost = mine_cost, unused = 0;
+        for (int b0 = 0;;) {
             const int incl = scan(cost, lane);
             const uint32_t past = __ballot_sync(0xffffffffu, u.at + incl > x);
-            if (past) {
-                const int src = __ffs(past) - 1;          // (the first lane of its sequence's)
-                b = b0 + src / w;
+            if (past || b0 + 32 >= p.q.B) {
+                const int src = past ? __ffs(past) - 1 : 0;          // (the first lane of its sequence's)
                 u.at += __shfl_sync(0xffffffffu, incl - cost, src);
+                u.s.b = __shfl_sync(0xffffffffu, s.b, src);
+                u.s.row0 = __shfl_sync(0xffffffffu, s.row0, src);
+                u.s.n = __shfl_sync(0xffffffffu, s.n, src);
+                u.s.len = __shfl_sync(0xffffffffu, s.len, src);
                 break;
             }
             u.at += __shfl_sync(0xffffffffu, incl, 31);
+            b0 += 32;
+            s = seq_of(b0 + lane);
+            cost = seq_cost(s, lane, unused);
         }
-        u.s = page_seq(p, b);
         u.tiles = span.tiles(u.s);
         u.tile = 0;
         for (int t0 = 0; t0 < u.tiles; t0 += 32) {

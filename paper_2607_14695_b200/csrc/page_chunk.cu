@@ -4,8 +4,8 @@
 // 64 keys of K, and half of the columns of V; TMA brings them from the pages, one box per page (or per 64 tokens of a larger page), to
 // where the swizzled tile has them. S = Q K^T and O = P V accumulate in tensor memory; P (bf16) is written over the logits it came from and is
 // the A operand of P V from there. Per CTA:
-//   warps 0, 2   TMA producers: its Q tile and its half of K; its columns of V (warp 3 is idle)
-//   warp 1       MMA issuer (leader CTA): Q K^T runs one tile (two at head_dim <= 128) ahead of P V
+//   warps 0, 2   TMA producers: its Q tile and its half of K; its columns of V. Warp 0 walks the pair's share of the work and lists its units for the others.
+//   warps 1, 3   MMA issuers (leader CTA): Q K^T runs one tile (two at head_dim <= 128) ahead of P V
 //   warps 4..    softmax: two threads per row, 64 keys each, eight warps a tile. At head_dim 128 and 64 there are two such groups, which take the tiles
 //                in turn: each then has the time of two tiles for its chain of loads, maximum, exponentials and stores, and a scheduler
 //                has four of its warps. The threads of a row agree on the reference maximum at one named barrier per 32 rows, where the group
@@ -59,16 +59,27 @@ struct ChunkSpanOf {
     }
 };
 
+// A pair's share of a unit, as warp 0 lists it for the others: tiles of keys [t0, t0 + n); none at all behind the last one (n = -1).
+struct ChunkUnit {
+    int b, row0, n_rows, len;      // the sequence
+    int token, h;                  // first token of the pair's rows, KV head
+    int t0, n, hi;                 // keys below hi
+    int slot;                      // of its partial result, -1: the whole unit is the pair's
+    int unused[6];
+};
+static_assert(sizeof(ChunkUnit) == 64, "list of units");
+
 template <int HD, int D> struct Chunk {
     static constexpr int CH = D / 64;                           // 64-column chunks of Q and K
     static constexpr int VCH = HD / 128;                        // chunks of V of this CTA
     static constexpr int NST = HD == 256 ? 2 : 4;               // stages of K, and of V
     static constexpr int NS = HD == 256 ? 2 : 3;                // buffers of logits and weights in tensor memory
-    static constexpr int AHEAD = NS - 1;                        // tiles that Q K^T is ahead of P V
+    static constexpr bool SPLIT = HD == 128;                    // a warp of its own for either product
     static constexpr int NG = HD == 256 ? 1 : 2;                // softmax groups of 8 warps
     static constexpr int THREADS = 128 + 256 * NG;
+    static constexpr int NU = 8;                                // units in the list
     static constexpr int QFULL = 0, QEMPTY = 1, KFULL = 2, KEMPTY = KFULL + NST, VLAND = KEMPTY + NST, VEMPTY = VLAND + NST, SFULL = VEMPTY + NST, PFULL = SFULL + NS,
-                         PVDONE = PFULL + NS, OFREE = PVDONE + 4, COUNT = OFREE + 1;
+                         PVDONE = PFULL + NS, OFREE = PVDONE + 4, UFULL = OFREE + 1, UEMPTY = UFULL + NU, COUNT = UEMPTY + NU;
     static constexpr uint32_t BAR_BYTES = (8 * COUNT + 104 + 127) / 128 * 128;                // ... tensor memory's address, abort flag, bad units, tiles
     static constexpr uint32_t Q_BYTES = CH * 128 * 128;
     static constexpr uint32_t K_STAGE = CH * 64 * 128;
@@ -76,12 +87,14 @@ template <int HD, int D> struct Chunk {
     static constexpr uint32_t OFF_Q = 0;
     static constexpr uint32_t OFF_K = OFF_Q + Q_BYTES;
     static constexpr uint32_t OFF_V = OFF_K + NST * K_STAGE;
-    static constexpr uint32_t OFF_STAGE = OFF_V + NST * V_STAGE;      // two halves of 128 rows x 64 columns of the result
-    static constexpr uint32_t OFF_BAR = OFF_STAGE + 2 * 128 * 128;
-    static constexpr uint32_t OFF_MAX = OFF_BAR + BAR_BYTES;          // [2 tiles][128 rows][2 halves] maxima of the logits
-    static constexpr uint32_t OFF_REF = OFF_MAX + 2 * 128 * 2 * 4;    // [128] reference maxima, from group to group (two groups only)
-    static constexpr uint32_t OFF_SUM = OFF_STAGE + 128 * 128;        // [2 NG][128] (reference, sum) at the end of a unit, where the results' second 64 columns go later
-    static constexpr uint32_t NEED = OFF_REF + (NG - 1) * 128 * 4;
+    static constexpr uint32_t OFF_STAGE = OFF_V + NST * V_STAGE;      // of each group: 128 rows x 64 columns of the result
+    static constexpr uint32_t OFF_BAR = OFF_STAGE + NG * 128 * 128;
+    static constexpr uint32_t OFF_UNITS = OFF_BAR + BAR_BYTES;       // [NU] ChunkUnit
+    static constexpr uint32_t OFF_MAX = OFF_UNITS + NU * 64;          // [2 tiles][128 rows][2 halves] maxima of the logits
+    static constexpr uint32_t OFF_REF = OFF_MAX + 2 * 128 * 2 * 4;    // [128] reference maxima, from group to group
+    static constexpr uint32_t OFF_SUM = OFF_REF + 128 * 4;            // [2 units][2 NG][128] (reference, sum) of a row's threads
+    static constexpr uint32_t OFF_ROWS = OFF_SUM + 2 * 2 * NG * 128 * 8;
+    static constexpr uint32_t NEED = OFF_ROWS + 128 * 4;
     static constexpr uint32_t TOTAL = NEED + 1024 > 232448 ? 232448 : NEED + 1024;
     static_assert(NEED <= TOTAL, "shared memory");
 };
@@ -100,7 +113,8 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                   const PageAttention p, const PagePartials part, int tile_tokens, int box)
 {
     using L = Chunk<HD, D>;
-    constexpr int CH = L::CH, VCH = L::VCH, NST = L::NST, NS = L::NS, AHEAD = L::AHEAD, NG = L::NG;
+    constexpr int CH = L::CH, VCH = L::VCH, NST = L::NST, NS = L::NS, NG = L::NG;
+    constexpr bool SPLIT = L::SPLIT;
     constexpr uint32_t kColS = HD;
     static_assert(HD + L::NS * kChunkKeys <= 512, "tensor memory");
     extern __shared__ uint8_t smem_raw[];
@@ -112,7 +126,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(smem + L::OFF_BAR + 8 * L::COUNT);
     volatile uint32_t *abort_flag = tmem_slot + 1;
     volatile uint32_t *bad_unit = tmem_slot + 2;          // [8]: number (from 1) of the last unit of that residue which met a bad page
-    volatile uint32_t *tile_info = bad_unit + 8;           // [16]: what the issuer has to know of tile g (written by the leader's K producer ahead of the arrival on KFULL)
+    volatile uint32_t *tile_info = bad_unit + 8;           // [16]: (g + 1) << 4 and what the issuers have to know of tile g (written by the leader's K producer ahead of the arrival on KFULL)
     constexpr uint32_t kFirst = 1u, kLast = 2u, kSecond = 4u, kEnd = 8u;       // of its unit; has live keys in its second half; there is no such tile
     if ((base - raw_addr) + L::NEED > L::TOTAL) {          // (the same for every CTA: all of them leave)
         if (threadIdx.x == 0) report_page_wait(p.g.status, 15u);
@@ -122,13 +136,27 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const uint32_t rank = cluster_ctarank();
     const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     const int G = p.g.Hq / p.g.Hkv;
-    const PageLine<ChunkSpanOf> line{p, {p, 2 * tile_tokens}};
+    // The K producer walks the line. It looks for its pair's place first of all: what the line is made of does not change under this kernel (only the widening of
+    // pages runs beside its start).
+    PageLine<ChunkSpanOf> line{p, {p, 2 * tile_tokens}};
+    typename PageLine<ChunkSpanOf>::Place place;
+    int total = 0, x0 = 0, x1 = 0, nc = 0;
+    if (warp == 0) {
+        total = line.begin(lane);
+        nc = min(pairs, total);
+        const PageShares shares(total, max(1, nc));
+        if (pair < nc) {
+            x0 = shares.of(pair); x1 = shares.of(pair + 1);
+            place = line.find(x0, lane);
+        }
+    }
 
     if (threadIdx.x == 0) {
-        // (weights: an arrival per warp of the group of either CTA; the accumulator's release: of every softmax warp)
-        for (int i = 0; i < L::COUNT; ++i) mbar_init(bar(i), i >= L::PFULL && i < L::PFULL + NS ? 16u : i == L::OFREE ? 16u * NG : 1u);
+        // (weights, and the accumulator's release: an arrival per warp of a group of either CTA; a unit of the list: of every softmax warp here)
+        for (int i = 0; i < L::COUNT; ++i)
+            mbar_init(bar(i), i >= L::PFULL && i < L::PFULL + NS || i == L::OFREE ? 16u : i >= L::UEMPTY ? 8u * NG : 1u);
         *abort_flag = 0u;
-        for (int i = 0; i < 8; ++i) bad_unit[i] = 0u;
+        for (int i = 0; i < 24; ++i) bad_unit[i] = 0u;           // (and tile_info)
         fence_mbar_init();
         prefetch_tmap(&tm_q); prefetch_tmap(&tm_k); prefetch_tmap(&tm_v);
     }
@@ -157,80 +185,103 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         return false;
     };
 
-    int longest;
-    const int total = line.total(lane, longest);
-    const int nc = min(pairs, total);
-    if (threadIdx.x == 128 && rank == 0) part.meta[pair].b = -1;      // (the thread that may write the entry later)
-    const bool works = pair < nc;
-    const PageShares shares(total, max(1, nc));
-    const int x0 = works ? shares.of(pair) : 0, x1 = works ? shares.of(pair + 1) : 0;
-    // This pair's units, one after the other: tiles [k0, k1) of unit u (one at least, if only in name), `n` of keys, from tile `t0` on; x: where in the line it goes on
-    struct Slice { typename PageLine<ChunkSpanOf>::Place u; int k0, k1, t0, n, x; };
-    auto cut = [&](Slice &w, int x) {
-        w.x = min(w.u.at + w.u.cost, x1);
-        w.k0 = max(0, x - w.u.at - kChunkSetUp);
-        w.k1 = max(0, w.x - w.u.at - kChunkSetUp);
-        w.t0 = w.u.sp.tile0 + w.k0;
-        w.n = max(0, min(w.k1, w.u.sp.tiles) - w.k0);
-    };
-    auto step = [&](Slice &w) -> bool {      // to the next unit of the share
-        if (w.x >= x1) return false;
-        line.next(w.u);
-        cut(w, w.x);
-        return true;
-    };
-    Slice w0;
-    if (works) {
-        w0.u = line.find(x0, lane);
-        cut(w0, x0);
-    }
-    // the tiles of the share as one sequence: number g, tile jj of unit number ui (of those that have keys)
-    struct Cursor { Slice w; int jj, g, ui; bool valid; };
-    auto settle = [&](Cursor &c) {          // at or behind c.w: the next unit with a tile
-        while (c.w.n == 0) {
-            if (!step(c.w)) { c.valid = false; return; }
+    constexpr uint16_t both = 3;               // CTAs of the pair, for commits
+    auto all = [&](bool good) -> bool { return __all_sync(0xffffffffu, good); };
+    const ChunkUnit *units = reinterpret_cast<const ChunkUnit *>(smem + L::OFF_UNITS);
+    auto unit_ready = [&](int i) -> bool { return all(wait(L::UFULL + i % L::NU, (uint32_t)(i / L::NU) & 1u, 1)); };      // the i-th of the list may be read
+
+    // the tiles of the share as one sequence: number g, tile jj of unit number i of the list, ui of those that have keys
+    struct Cursor { int b, h, t0, n, hi, q_row, jj, g, ui, i; bool valid; };
+    auto settle = [&](Cursor &c) {          // the i-th unit, or the first one behind it with a tile
+        for (;; ++c.i) {
+            c.valid = unit_ready(c.i);
+            if (!c.valid) return;
+            const ChunkUnit &u = units[c.i % L::NU];
+            c.n = u.n;
+            if (c.n != 0) {
+                c.valid = c.n > 0;
+                c.b = u.b; c.h = u.h; c.t0 = u.t0; c.hi = u.hi;
+                c.q_row = u.row0 + u.token + (int)rank * tile_tokens;
+                c.jj = 0;
+                return;
+            }
         }
-        c.jj = 0;
     };
     auto begin = [&]() -> Cursor {
-        Cursor c;
-        c.w = w0; c.jj = 0; c.g = 0; c.ui = 0; c.valid = true;
+        Cursor c = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, false};
         settle(c);
         return c;
     };
     auto advance = [&](Cursor &c) {
         ++c.g;
-        if (++c.jj == c.w.n) {
-            ++c.ui;
-            if (!step(c.w)) c.valid = false; else settle(c);
-        }
+        if (++c.jj == c.n) { ++c.ui; ++c.i; settle(c); }
     };
     // Where a warp's tile of keys lies, box by box: lane i has the row of box i in the layer's pages (0 where it holds no key below the unit's
     // last, or where the table is wrong: `bad`). It is looked up a tile ahead, since a table entry takes some 500 cycles to come.
     const int per_half = 64 / box;               // boxes of 64 keys
     auto boxes = [&](int key0, int hi) -> int { return (min(max(hi - key0, 0), 64) + box - 1) / box; };
     auto look_up = [&](const Cursor &c, bool &bad) -> int {
-        const int key = (c.w.t0 + c.jj) * kChunkKeys + lane * box;
+        const int key = (c.t0 + c.jj) * kChunkKeys + lane * box;
         bad = false;
-        if (!c.valid || lane >= 2 * per_half || key >= c.w.u.sp.hi) return 0;
-        const int page = page_at(p.q, p.g.n_pages, c.w.u.s.b, key >> p.g.log_p);
+        if (!c.valid || lane >= 2 * per_half || key >= c.hi) return 0;
+        const int page = page_at(p.q, p.g.n_pages, c.b, key >> p.g.log_p);
         bad = page < 0;
-        return bad ? 0 : (int)page_row(p.g, page, c.w.u.h) + (key & (p.g.P - 1));
+        return bad ? 0 : (int)page_row(p.g, page, c.h) + (key & (p.g.P - 1));
     };
 
-    // (a pair without a unit goes on to the end, where it leaves together)
-    if (works && warp == 0) {
-        // ---------------- Q and K by TMA (the warp stays converged, one lane issues) ----------------
-        Cursor c = begin();
+    if (warp == 0) {
+        // ---------------- the list of units; Q and K by TMA (the warp stays converged, one lane issues) ----------------
+        // A unit costs kChunkSetUp blocks ahead of its tiles; a share that ends among them leaves the unit to the next pair.
+        const PageShares shares(total, max(1, nc));
+        ChunkUnit *list = reinterpret_cast<ChunkUnit *>(smem + L::OFF_UNITS);
+        if (lane == 0 && rank == 0) part.meta[pair].b = -1;
         bool bad, ok = true;
+        Cursor c = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, false};
+        int x = x0;
+        auto publish = [&](const ChunkUnit &u) {
+            if (c.i >= L::NU) ok = ok && all(wait(L::UEMPTY + c.i % L::NU, (uint32_t)(c.i / L::NU - 1) & 1u, 13));
+            if (ok && lane == 0) {
+                list[c.i % L::NU] = u;
+                mbar_arrive(bar(L::UFULL + c.i % L::NU));
+            }
+            ++c.i;
+        };
+        auto next_unit = [&] {                   // lists units up to the next one with a tile, or to the end
+            c.valid = false;
+            while (x < x1 && ok) {
+                const int to = min(place.at + place.cost, x1);
+                const int k0 = max(0, x - place.at - kChunkSetUp), k1 = max(0, to - place.at - kChunkSetUp);
+                if (k1 > 0) {
+                    const bool whole = k0 == 0 && k1 == place.cost - kChunkSetUp;
+                    const ChunkUnit u = {place.s.b, place.s.row0, place.s.n, place.s.len, place.tile * 2 * tile_tokens, place.h, place.sp.tile0 + k0, max(0, min(k1, place.sp.tiles) - k0), place.sp.hi,
+                                         whole ? -1 : 2 * pair + (k0 == 0 ? 1 : 0), {0, 0, 0, 0, 0, 0}};
+                    publish(u);
+                    if (k0 == 0 && !whole && rank == 0 && lane == 0) {
+                        const int first = u.token * G;
+                        const PageSplit m = {u.b, u.row0, first, min(2 * tile_tokens * G, u.n_rows * G - first), u.h, shares.owner(place.at + place.cost - 1), tile_tokens * G, 0};
+                        part.meta[pair] = m;
+                    }
+                    c.b = u.b; c.h = u.h; c.t0 = u.t0; c.n = u.n; c.hi = u.hi;
+                    c.q_row = u.row0 + u.token + (int)rank * tile_tokens;
+                    c.jj = 0;
+                    c.valid = u.n > 0 && ok;
+                }
+                x = to;
+                if (x < x1) line.next(place);
+                if (c.valid) return;
+            }
+            const ChunkUnit none = {0, 0, 0, 0, 0, 0, 0, -1, 0, -1, {0, 0, 0, 0, 0, 0}};
+            publish(none);
+        };
+        next_unit();
         int row = look_up(c, bad);
         while (c.valid) {
-            const int st = c.g % NST, key0 = (c.w.t0 + c.jj) * kChunkKeys, hi = c.w.u.sp.hi;
+            const int st = c.g % NST, key0 = (c.t0 + c.jj) * kChunkKeys, hi = c.hi;
             if (c.g >= NST) ok = wait(L::KEMPTY + st, (uint32_t)(c.g / NST - 1) & 1u, 1);
             if (!__all_sync(0xffffffffu, ok)) break;
             const int nb = boxes(key0 + 64 * (int)rank, hi);
             if (rank == 0 && lane == 0) {
-                tile_info[c.g & 15] = (c.jj == 0 ? kFirst : 0u) | (c.jj + 1 == c.w.n ? kLast : 0u) | (key0 + 64 < hi ? kSecond : 0u);
+                tile_info[c.g & 15] = ((uint32_t)c.g + 1u) << 4 | (c.jj == 0 ? kFirst : 0u) | (c.jj + 1 == c.n ? kLast : 0u) | (key0 + 64 < hi ? kSecond : 0u);
                 mbar_expect_tx(bar(L::KFULL + st), (uint32_t)((boxes(key0, hi) + boxes(key0 + 64, hi)) * box * 128 * CH));
             }
             __syncwarp();
@@ -246,27 +297,27 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (!__all_sync(0xffffffffu, ok)) break;
                 const uint32_t bytes = (uint32_t)(G * tile_tokens * 128 * CH);
                 if (rank == 0) mbar_expect_tx_elect(bar(L::QFULL), 2 * bytes);
-                const int t = c.w.u.s.row0 + (2 * c.w.u.tile + (int)rank) * tile_tokens;
 #pragma unroll
-                for (int ch = 0; ch < CH; ++ch) tma2_load_3d_elect(base + L::OFF_Q + ch * (128 * 128), &tm_q, bar(L::QFULL) & kPeerBitMask, ch * 64, c.w.u.h * G, t);
+                for (int ch = 0; ch < CH; ++ch) tma2_load_3d_elect(base + L::OFF_Q + ch * (128 * 128), &tm_q, bar(L::QFULL) & kPeerBitMask, ch * 64, c.h * G, c.q_row);
             }
-            advance(c);
+            ++c.g;
+            if (++c.jj == c.n) { ++c.ui; next_unit(); }
             row = look_up(c, bad);
         }
-        if (rank == 0 && !c.valid) {
+        if (rank == 0 && !c.valid && ok) {
             if (c.g >= NST) ok = wait(L::KEMPTY + c.g % NST, (uint32_t)(c.g / NST - 1) & 1u, 1);
             if (ok && lane == 0) {
-                tile_info[c.g & 15] = kEnd;
+                tile_info[c.g & 15] = ((uint32_t)c.g + 1u) << 4 | kEnd;
                 mbar_arrive(bar(L::KFULL + c.g % NST));
             }
         }
-    } else if (works && warp == 2) {
+    } else if (warp == 2) {
         // ---------------- V by TMA: this CTA's columns (heads of 64: the upper columns are nobody's) ----------------
         Cursor c = begin();
         bool bad, ok = true;
         int row = look_up(c, bad);
         while (c.valid) {
-            const int st = c.g % NST, key0 = (c.w.t0 + c.jj) * kChunkKeys, hi = c.w.u.sp.hi;
+            const int st = c.g % NST, key0 = (c.t0 + c.jj) * kChunkKeys, hi = c.hi;
             if (c.g >= NST) ok = wait(L::VEMPTY + st, (uint32_t)(c.g / NST - 1) & 1u, 3);
             if (!__all_sync(0xffffffffu, ok)) break;
             if (__any_sync(0xffffffffu, bad) && lane == 0) bad_unit[c.ui & 7] = (uint32_t)c.ui + 1u;
@@ -283,57 +334,39 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             advance(c);
             row = look_up(c, bad);
         }
-    } else if (works && warp == 1) {
-        // ---------------- MMA issuer (leader CTA; the warp stays converged, one lane issues) ----------------
-        if (rank == 0) {
-            constexpr uint16_t both = 3;
+    } else if (warp == 1 || warp == 3) {
+        // ---------------- S = Q K^T and O += P V (leader CTA; the warps stay converged, one lane issues) ----------------
+        // Beside the busy warps of its scheduler a warp takes 450 to 700 cycles for the 8 MMAs of a product of head_dim 128, and 200 or 300 around them: there
+        // warp 3 issues P V (1850 cycles a tile with one warp for both). At 256 the MMAs take longer than that, and the order of one warp's issue saves the wait for P V's
+        // end ahead of the logits that take the place of its weights.
+        // Everything that an MMA is issued with is kept uniform (votes and reductions say so to the compiler), or each of its operands is moved to the
+        // uniform registers anew. What a tile is comes with its keys: walking the list of units here took 1200 cycles a tile.
+        if (rank == 0 && (SPLIT || warp == 1)) {
             constexpr uint32_t idesc_qk = umma_idesc_bf16(256, kChunkKeys, false), idesc_pv = umma_idesc_bf16(256, HD, true);
-            const uint64_t qdesc0 = umma_desc_sw128(base + L::OFF_Q, 16, 1024), kdesc0 = umma_desc_sw128(base + L::OFF_K, 16, 1024);
-            const uint64_t vdesc0 = umma_desc_sw128(base + L::OFF_V, 128 * 128, 1024);
-            // Q K^T of tile `q` and P V of tile `v`, up to AHEAD tiles behind it. (The logits of tile g + NS go where the weights of tile g are: Q K^T of the one is
-            // issued behind P V of the other.) What a tile is comes with its keys; this warp shares its scheduler with busy ones, and walking the
-            // list of units here took 1200 cycles a tile. Everything that an MMA is issued with is kept uniform (votes and reductions say so to the
-            // compiler), or each of its operands is moved to the uniform registers anew.
-            auto all = [&](bool good) -> bool { return __all_sync(0xffffffffu, good); };
+            const uint64_t qdesc0 = umma_desc_sw128(base + L::OFF_Q, 16, 1024), kdesc0 = umma_desc_sw128(base + L::OFF_K, 16, 1024), vdesc0 = umma_desc_sw128(base + L::OFF_V, 128 * 128, 1024);
             const uint32_t tm = __reduce_or_sync(0xffffffffu, tmem_base);
             const uint32_t q_lo = (uint32_t)qdesc0, k_lo = (uint32_t)kdesc0, v_lo = (uint32_t)vdesc0, d_hi = (uint32_t)(qdesc0 >> 32), v_hi = (uint32_t)(vdesc0 >> 32);
-            bool ok = true, end = false;
-            int q = 0, v = 0, uq = 0, uv = 0;                          // tiles, and units begun
+            int q = 0, v = 0, uq = 0, uv = 0;                          // next tile of either product, and units begun
             int q_st = 0, q_buf = 0, v_st = 0, v_buf = 0;              // ... their stages and buffers
             uint32_t q_sph = 0u, v_bph = 0u;                           // parities of KFULL of tile q and PFULL of tile v
-            while (ok) {
-                // A tile whose weights are there goes first: the end of a unit waits for nothing else.
-                while (!end && q <= v + AHEAD && (q == v || !all(mbar_test_wait(bar(L::PFULL + v_buf), v_bph)))) {
-                    ok = all(wait(L::KFULL + q_st, q_sph, 4));
-                    if (!ok) break;
-                    const uint32_t info = __reduce_or_sync(0xffffffffu, tile_info[q & 15]);
-                    end = (info & kEnd) != 0u;
-                    if (end) break;
-                    if (info & kFirst) {
-                        // a unit whose Q has not come yet does not hold up the products of the last one
-                        if (q > v) { if (!all(mbar_test_wait(bar(L::QFULL), (uint32_t)uq & 1u))) break; }
-                        else { ok = all(wait(L::QFULL, (uint32_t)uq & 1u, 5)); if (!ok) break; }
-                        ++uq;
-                    }
-                    tc_fence_after();
+            auto issue_qk = [&](uint32_t info) {
+                tc_fence_after();
 #pragma unroll
-                    for (int ch = 0; ch < CH; ++ch)
-                        umma2_ss4_elect(tm + kColS + q_buf * kChunkKeys, q_lo + ch * (128 * 128 / 16), d_hi, k_lo + (uint32_t)q_st * (L::K_STAGE / 16) + ch * (64 * 128 / 16), d_hi, idesc_qk, ch > 0 ? 1u : 0u);
-                    umma2_commit_mc_elect(bar(L::SFULL + q_buf), both);
-                    umma2_commit_mc_elect(bar(L::KEMPTY + q_st), both);
-                    if (info & kLast) umma2_commit_mc_elect(bar(L::QEMPTY), both);
-                    ++q;
-                    if (++q_st == NST) { q_st = 0; q_sph ^= 1u; }
-                    if (++q_buf == NS) q_buf = 0;
-                }
-                if (!ok || q == v) break;
-                const uint32_t info = __reduce_or_sync(0xffffffffu, tile_info[v & 15]);
-                ok = all(wait(L::PFULL + v_buf, v_bph, 6));
-                if (ok && (info & kFirst)) {
-                    if (uv >= 1) ok = all(wait(L::OFREE, (uint32_t)(uv - 1) & 1u, 7));
+                for (int ch = 0; ch < CH; ++ch)
+                    umma2_ss4_elect(tm + kColS + q_buf * kChunkKeys, q_lo + ch * (128 * 128 / 16), d_hi, k_lo + (uint32_t)q_st * (L::K_STAGE / 16) + ch * (64 * 128 / 16), d_hi, idesc_qk, ch > 0 ? 1u : 0u);
+                umma2_commit_mc_elect(bar(L::SFULL + q_buf), both);
+                umma2_commit_mc_elect(bar(L::KEMPTY + q_st), both);
+                if (info & kLast) umma2_commit_mc_elect(bar(L::QEMPTY), both);
+                ++q;
+                if (++q_st == NST) { q_st = 0; q_sph ^= 1u; }
+                if (++q_buf == NS) q_buf = 0;
+            };
+            auto issue_pv = [&](uint32_t info) -> bool {
+                if (!all(wait(L::PFULL + v_buf, v_bph, 6))) return false;
+                if (info & kFirst) {
+                    if (uv >= 1 && !all(wait(L::OFREE, (uint32_t)(uv - 1) & 1u, 7))) return false;
                     ++uv;
                 }
-                if (!ok) break;
                 tc_fence_after();
                 const uint32_t p_tmem = tm + kColS + v_buf * kChunkKeys, v_at = v_lo + (uint32_t)v_st * (L::V_STAGE / 16);
                 umma2_ts4_elect(tm, p_tmem, v_at, v_hi, idesc_pv, (info & kFirst) ^ kFirst);
@@ -343,9 +376,59 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 ++v;
                 if (++v_st == NST) v_st = 0;
                 if (++v_buf == NS) { v_buf = 0; v_bph ^= 1u; }
+                return true;
+            };
+            if (SPLIT && warp == 1) {
+                for (;;) {
+                    if (!all(wait(L::KFULL + q_st, q_sph, 4))) break;
+                    const uint32_t info = __reduce_or_sync(0xffffffffu, tile_info[q & 15]);
+                    if (info & kEnd) break;
+                    if (info & kFirst) {
+                        if (!all(wait(L::QFULL, (uint32_t)uq & 1u, 5))) break;
+                        ++uq;
+                    }
+                    // the logits go where the weights of tile q - NS were
+                    if (q >= NS && !all(wait(L::PVDONE + ((q - NS) & 3), (uint32_t)((q - NS) >> 2) & 1u, 14))) break;
+                    issue_qk(info);
+                }
+            } else if (SPLIT) {
+                for (;;) {
+                    // (a tile's entry is there long before its weights, but for the last one, which says that there is none)
+                    uint32_t info = __reduce_or_sync(0xffffffffu, tile_info[v & 15]);
+                    if (info >> 4 != (uint32_t)v + 1u) {
+                        const unsigned long long t_start = globaltimer_ns();
+                        for (uint32_t n = 1; info >> 4 != (uint32_t)v + 1u; ++n) {
+                            info = __reduce_or_sync(0xffffffffu, tile_info[v & 15]);
+                            if ((n & 255u) == 0u && !all(*abort_flag == 0u && globaltimer_ns() - t_start < kChunkWaitNs)) break;
+                        }
+                        if (info >> 4 != (uint32_t)v + 1u) { *abort_flag = 1u; report_page_wait(p.g.status, 15u); break; }
+                    }
+                    if ((info & kEnd) || !issue_pv(info)) break;
+                }
+            } else {
+                bool ok = true, end = false;
+                while (ok) {
+                    // Q K^T runs one tile ahead, but for a tile whose weights are there already: the end of a unit waits for nothing else.
+                    while (!end && q < v + NS && (q == v || !all(mbar_test_wait(bar(L::PFULL + v_buf), v_bph)))) {
+                        ok = all(wait(L::KFULL + q_st, q_sph, 4));
+                        if (!ok) break;
+                        const uint32_t info = __reduce_or_sync(0xffffffffu, tile_info[q & 15]);
+                        end = (info & kEnd) != 0u;
+                        if (end) break;
+                        if (info & kFirst) {
+                            // a unit whose Q has not come yet does not hold up the products of the last one
+                            if (q > v) { if (!all(mbar_test_wait(bar(L::QFULL), (uint32_t)uq & 1u))) break; }
+                            else { ok = all(wait(L::QFULL, (uint32_t)uq & 1u, 5)); if (!ok) break; }
+                            ++uq;
+                        }
+                        issue_qk(info);
+                    }
+                    if (!ok || q == v) break;
+                    ok = issue_pv(__reduce_or_sync(0xffffffffu, tile_info[v & 15]));
+                }
             }
         }
-    } else if (works && warp >= 4) {
+    } else {
         // ---------------- softmax, rescaling, results ----------------
         const int sw = warp - 4, group = sw >> 3, half = (sw >> 2) & 1, quarter = warp & 3;
         const int row = quarter * 32 + lane;
@@ -354,81 +437,89 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         float *maxima = reinterpret_cast<float *>(smem + L::OFF_MAX);
         float *ref = reinterpret_cast<float *>(smem + L::OFF_REF);
         float2 *sums = reinterpret_cast<float2 *>(smem + L::OFF_SUM);
-        const int rows_here = tile_tokens * G;
-        const int tid = threadIdx.x - 128;
+        const int gtid = (threadIdx.x - 128) & 255;
+        auto group_sync = [&] { asm volatile("bar.sync %0, 256;" ::"r"(11 + group) : "memory"); };
         const float sc = part.scale_log2;
-        // where the 16 bytes that this thread stores of rows (tid / 8), + 32 NG, .. lie behind the first row of a tile
-        constexpr int RP = 32 * NG;
-        int out_at[128 / RP];
-#pragma unroll
-        for (int k = 0; k < 128 / RP; ++k) {
-            const int r = k * RP + (tid >> 3);
-            out_at[k] = (r / G * p.g.Hq + r % G) * D + (tid & 7) * 8;
-        }
+        int *out_row = reinterpret_cast<int *>(smem + L::OFF_ROWS);          // [128] where a row of a tile lies behind its first one
+        if (group == 0 && half == 0) out_row[row] = (row / G * p.g.Hq + row % G) * D;
         const int row_token = row / G;
         bool ok = true;
         int gt = 0, ui = 0;
-        Slice w = w0;
         // Row exchange: the 64 threads of a group's quarter meet at barrier 1 + quarter + 4 group. With two groups the other one's quarter has
         // arrived there, too, with its last tile (for the first tile of all: here).
         if (NG == 2 && group == 1) asm volatile("bar.arrive %0, 128;" ::"r"(1 + quarter) : "memory");
-        do {
-            if (w.k1 == 0) continue;             // the share ends before the unit's first tile
-            const PageSeq &s = w.u.s;
-            const int token0 = (2 * w.u.tile + (int)rank) * tile_tokens;         // first of this CTA's rows
-            const int t_row = token0 + row_token, live_rows = min(rows_here, (s.n - token0) * G);
-            const bool row_live = row < live_rows;
-            const PageRange mine = page_range(s, p, min(t_row, s.n - 1), min(t_row, s.n - 1));
-            const bool whole = w.k0 == 0 && w.k1 == w.u.cost - kChunkSetUp;
-            // keys that every row of the pair sees (either CTA's V meets the rows of both)
-            const int all_lo = page_range(s, p, min(s.n, 2 * (w.u.tile + 1) * tile_tokens) - 1, 0).lo, all_hi = page_range(s, p, 0, 2 * w.u.tile * tile_tokens).hi;
-            const int slot = 2 * pair + (w.k0 == 0 ? 1 : 0);
+        for (int ul = 0; unit_ready(ul); ++ul) {
+            const ChunkUnit &u = units[ul % L::NU];
+            const int n = u.n, t0 = u.t0, hi = u.hi;
+            if (n < 0) break;
+            auto leave = [&] {                     // this warp is done with the list's entry
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(L::UEMPTY + ul % L::NU));
+            };
+            PageRange mine;                          // keys that this row sees
+            int all_lo, all_hi;                      // keys that every row of the pair sees (either CTA's V meets the rows of both)
+            {
+                const PageSeq s = {u.b, u.row0, u.n_rows, u.len};
+                const int t = min(u.token + (int)rank * tile_tokens + row_token, s.n - 1);
+                mine = page_range(s, p, t, t);
+                all_lo = page_range(s, p, min(s.n, u.token + 2 * tile_tokens) - 1, 0).lo;
+                all_hi = page_range(s, p, 0, u.token).hi;
+            }
             float m_ref = -INFINITY, l = 0.f;
-            auto tile = [&](auto mode_c, const int jj) {
-                constexpr bool FULL = decltype(mode_c)::value == 0;
-                constexpr bool DEAD = decltype(mode_c)::value == 2;        // a half past the unit's last key: no logits to read and no weights to write
+            // (One instance of this code for whole and for masked tiles: three, with 64 keys unrolled in each, were 40 KB that the instruction caches had to
+            // fetch again at every change, 3000 cycles of a unit.)
+#pragma unroll 1
+            for (int jj = NG == 1 || (gt & 1) == group ? 0 : 1; jj < n; jj += NG) {          // (groups take the tiles of the whole share in turn)
                 const int gi = gt + jj, buf = gi % NS, st = gi % NST;
                 const uint32_t vph = (uint32_t)(gi / NST) & 1u;
-                const int key0 = (w.t0 + jj) * kChunkKeys + half * 64;
+                const int key0 = (t0 + jj) * kChunkKeys + half * 64;
                 const uint32_t s_addr = tmem_base + lane_addr + kColS + buf * kChunkKeys + half * 64;
-                const uint64_t mask = FULL ? ~0ull : bits64(mine.lo - key0, mine.hi - key0);       // keys that this row sees
+                const bool masked = key0 < all_lo || key0 + 64 > all_hi;
+                const uint64_t mask = masked ? bits64(mine.lo - key0, mine.hi - key0) : ~0ull;       // keys that this row sees
                 float mx = -INFINITY;
                 // One group keeps its logits in registers (168 of them a thread); two groups (96) read them from tensor memory a second time.
-                uint32_t r[2][32];
-                if constexpr (!DEAD) {
-                    ok = ok && wait(L::SFULL + buf, (uint32_t)(gi / NS) & 1u, 8);
-                    tc_fence_after();
-                    tmem_ld32(s_addr, r[0]);
-                    if (NG == 1) tmem_ld32(s_addr + 32, r[1]);
+                uint32_t r[NG == 1 ? 2 : 1][32];
+                auto hide = [&](uint32_t (&v)[32], int c) {
+                    const uint32_t bits = (uint32_t)(mask >> (32 * c));
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if (NG == 2 || c == 0) tmem_wait_ld();
-                        uint32_t (&v)[32] = r[NG == 1 ? c : 0];
-                        if constexpr (!FULL) {
-                            const uint32_t bits = (uint32_t)(mask >> (32 * c));
+                    for (int i = 0; i < 32; ++i)
+                        if (!(bits & (1u << i))) v[i] = 0xff800000u;
+                };
+                ok = ok && wait(L::SFULL + buf, (uint32_t)(gi / NS) & 1u, 8);
+                tc_fence_after();
+                tmem_ld32(s_addr, r[0]);
+                if constexpr (NG == 1) tmem_ld32(s_addr + 32, r[1]);
+                auto maximum = [&](uint32_t (&v)[32], int c) {
+                    if (masked) hide(v, c);
+                    float x[32];
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (!(bits & (1u << i))) v[i] = 0xff800000u;
-                        }
-                        float x[32];
+                    for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(v[i]);
+                    float mx4[4] = {mx, x[0], x[1], x[2]};
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(v[i]);
-                        float mx4[4] = {mx, x[0], x[1], x[2]};
-#pragma unroll
-                        for (int i = 3; i + 7 < 32; i += 8) {
-                            mx4[0] = max3_nan_f32(mx4[0], x[i], x[i + 1]); mx4[1] = max3_nan_f32(mx4[1], x[i + 2], x[i + 3]);
-                            mx4[2] = max3_nan_f32(mx4[2], x[i + 4], x[i + 5]); mx4[3] = max3_nan_f32(mx4[3], x[i + 6], x[i + 7]);
-                        }
-                        mx4[0] = max3_nan_f32(mx4[0], x[27], x[28]); mx4[1] = max3_nan_f32(mx4[1], x[29], x[30]); mx4[2] = max_nan_f32(mx4[2], x[31]);
-                        mx = max_nan_f32(max_nan_f32(mx4[0], mx4[1]), max_nan_f32(mx4[2], mx4[3]));
-                        if (NG == 2) tmem_ld32(s_addr + (c == 0 ? 32 : 0), r[0]);
+                    for (int i = 3; i + 7 < 32; i += 8) {
+                        mx4[0] = max3_nan_f32(mx4[0], x[i], x[i + 1]); mx4[1] = max3_nan_f32(mx4[1], x[i + 2], x[i + 3]);
+                        mx4[2] = max3_nan_f32(mx4[2], x[i + 4], x[i + 5]); mx4[3] = max3_nan_f32(mx4[3], x[i + 6], x[i + 7]);
                     }
-                    if (!(mx < INFINITY)) l = __int_as_float(0x7fc00000);      // (a logit that is NaN or +inf)
+                    mx4[0] = max3_nan_f32(mx4[0], x[27], x[28]); mx4[1] = max3_nan_f32(mx4[1], x[29], x[30]); mx4[2] = max_nan_f32(mx4[2], x[31]);
+                    mx = max_nan_f32(max_nan_f32(mx4[0], mx4[1]), max_nan_f32(mx4[2], mx4[3]));
+                };
+                if constexpr (NG == 1) {
+                    tmem_wait_ld();
+                    maximum(r[0], 0);
+                    maximum(r[1], 1);
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        tmem_wait_ld();
+                        maximum(r[0], c);
+                        tmem_ld32(s_addr + (c == 0 ? 32 : 0), r[0]);
+                    }
                 }
+                if (!(mx < INFINITY)) l = __int_as_float(0x7fc00000);      // (a logit that is NaN or +inf)
                 maxima[((gi & 1) * 128 + row) * 2 + half] = mx;
                 asm volatile("bar.sync %0, %1;" ::"r"(1 + quarter + 4 * group), "n"(64 * NG) : "memory");
-                const float2 both = *reinterpret_cast<const float2 *>(maxima + ((gi & 1) * 128 + row) * 2);
-                const float top = fmaxf(both.x, both.y);
+                const float2 of_row = *reinterpret_cast<const float2 *>(maxima + ((gi & 1) * 128 + row) * 2);
+                const float top = fmaxf(of_row.x, of_row.y);
                 const float was = NG == 1 || jj == 0 ? m_ref : ref[row];          // the row's reference so far
                 const bool grow = jj == 0 || (top - was) * sc > kChunkGrow;
                 const float to = grow ? top : was;
@@ -439,172 +530,170 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (m_ref != to) { l *= m_ref == -INFINITY ? (l == l ? 0.f : 1.f) : ex2((m_ref - to) * sc); m_ref = to; }
                 if (jj > 0 && __any_sync(0xffffffffu, grow)) {
                     const float alpha = grow ? ex2((was - to) * sc) : 1.f;
+                    if constexpr (NG == 2) tmem_wait_ld();                  // (the second reading of the logits, which is then in its registers)
                     ok = ok && wait(L::PVDONE + ((gi - 1) & 3), (uint32_t)((gi - 1) >> 2) & 1u, 10);
                     tc_fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < D / 64; ++c) {
-                        uint32_t o[32];
-                        const uint32_t o_addr = tmem_base + lane_addr + half * (D / 2) + c * 32;
-                        tmem_ld32(o_addr, o);
+                    for (int c = 0; c < D / 2; c += 16) {
+                        uint32_t o[16];
+                        const uint32_t o_addr = tmem_base + lane_addr + half * (D / 2) + c;
+                        tmem_ld16(o_addr, o);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                        tmem_st32(o_addr, o);
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                        tmem_st16(o_addr, o);
                     }
                     tmem_wait_st();
                 }
-                if constexpr (!FULL && !DEAD) {
+                if (masked) {
+                    ok = ok && wait(L::VLAND + st, vph, 9);
                     // Keys behind the last one count as zeros in V (a weight of 0 does not make a stale NaN one); a key that only some rows see must be
                     // finite, or the sequence is done again row by row. The 128 threads of a half share its 64 keys: half of this CTA's columns each.
-                    ok = ok && wait(L::VLAND + st, vph, 9);
                     const int key = key0 + (row & 63);
                     uint4 *v0 = reinterpret_cast<uint4 *>(smem + L::OFF_V + st * L::V_STAGE + (half * 64 + (row & 63)) * 128) + (row >> 6) * 4;
-                    if (key >= w.u.sp.hi) {
-#pragma unroll
-                        for (int c = 0; c < VCH; ++c)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) v0[c * (128 * 128 / 16) + ((i + row) & 3)] = make_uint4(0, 0, 0, 0);
+                    if (key >= hi) {
+#pragma unroll 1
+                        for (int c = 0; c < 4 * VCH; ++c) v0[(c >> 2) * (128 * 128 / 16) + ((c + row) & 3)] = make_uint4(0, 0, 0, 0);
                     } else if ((key < all_lo || key >= all_hi) && (D == HD || rank == 0)) {
                         uint32_t odd = 0;
+#pragma unroll 1
+                        for (int c = 0; c < 4 * VCH; ++c) {
+                            const uint4 v = v0[(c >> 2) * (128 * 128 / 16) + ((c + row) & 3)];
+                            const uint32_t q[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                        for (int c = 0; c < VCH; ++c)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const uint4 v = v0[c * (128 * 128 / 16) + ((i + row) & 3)];
-                                const uint32_t q[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) odd |= ((q[e] & 0x7f80u) == 0x7f80u) | ((q[e] & 0x7f800000u) == 0x7f800000u);
-                            }
-                        if (odd) part.careful[s.b] = 1;
+                            for (int e = 0; e < 4; ++e) odd |= ((q[e] & 0x7f80u) == 0x7f80u) | ((q[e] & 0x7f800000u) == 0x7f800000u);
+                        }
+                        if (odd) part.careful[u.b] = 1;
                     }
                     fence_proxy_async_smem();
                 }
-                if constexpr (!DEAD) {
-                    const float mr = m_ref == -INFINITY ? 0.f : m_ref * sc;
-                    const uint64_t sc2 = pack_f32x2(sc, sc), nm2 = pack_f32x2(-mr, -mr);
-                    uint64_t sum2[2] = {0ull, 0ull};
+                const float mr = m_ref == -INFINITY ? 0.f : m_ref * sc;
+                const uint64_t sc2 = pack_f32x2(sc, sc), nm2 = pack_f32x2(-mr, -mr);
+                uint64_t sum2[2] = {0ull, 0ull};
+                auto weights = [&](uint32_t (&v)[32], int c) {
+                    uint32_t packed[16];
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        if (NG == 2) tmem_wait_ld();
-                        uint32_t (&v)[32] = r[NG == 1 ? c : 0];
-                        const uint32_t bits = (uint32_t)(mask >> (32 * c));
-                        uint32_t packed[16];
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            if (!FULL && NG == 2) {
-                                if (!(bits & (1u << i))) v[i] = 0xff800000u;
-                                if (!(bits & (2u << i))) v[i + 1] = 0xff800000u;
-                            }
-                            float x0, x1, p0, p1;
-                            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), sc2, nm2), x0, x1);
-                            p0 = ex2(x0); p1 = ex2(x1);
-                            sum2[(i >> 1) & 1] = add_f32x2(sum2[(i >> 1) & 1], pack_f32x2(p0, p1));
-                            packed[i >> 1] = pack_bf16(p0, p1);
-                        }
-                        if (NG == 2 && c == 0) tmem_ld32(s_addr + 32, r[0]);
-                        // (weights of keys 32 c .. of the half take the columns of its logits 16 c ..: read, and by this thread alone)
-                        tmem_st16(s_addr + 16 * c, packed);
+                    for (int i = 0; i < 32; i += 2) {
+                        float x0, x1;
+                        unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])), sc2, nm2), x0, x1);
+                        const float p0 = ex2(x0), p1 = ex2(x1);
+                        sum2[(i >> 1) & 1] = add_f32x2(sum2[(i >> 1) & 1], pack_f32x2(p0, p1));
+                        packed[i >> 1] = pack_bf16(p0, p1);
                     }
-                    float a, b;
-                    unpack_f32x2(add_f32x2(sum2[0], sum2[1]), a, b);
-                    l += a + b;
-                    tmem_wait_st();
+                    // (weights of keys 32 c .. of the half take the columns of its logits 16 c ..: read, and by this thread alone)
+                    tmem_st16(s_addr + 16 * c, packed);
+                };
+                if constexpr (NG == 1) {
+                    weights(r[0], 0);
+                    weights(r[1], 1);
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < 2; ++c) {
+                        tmem_wait_ld();
+                        if (masked) hide(r[0], c);
+                        weights(r[0], c);
+                        if (c == 0) tmem_ld32(s_addr + 32, r[0]);
+                    }
                 }
-                if (FULL || DEAD) ok = ok && wait(L::VLAND + st, vph, 11);       // (the arrival below says that this CTA's V is in place, too)
+                float a, b;
+                unpack_f32x2(add_f32x2(sum2[0], sum2[1]), a, b);
+                l += a + b;
+                tmem_wait_st();
+                if (!masked) ok = ok && wait(L::VLAND + st, vph, 11);       // (the arrival below says that this CTA's V is in place, too)
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(leader_pfull + 8u * (uint32_t)buf);
-            };
-            // (groups take the tiles of the whole share in turn)
-            for (int jj = NG == 1 || (gt & 1) == group ? 0 : 1; jj < w.n; jj += NG) {
-                const int key0 = (w.t0 + jj) * kChunkKeys + half * 64;
-                if (key0 >= all_lo && key0 + 64 <= all_hi) tile(std::integral_constant<int, 0>{}, jj);
-                else if (key0 < w.u.sp.hi) tile(std::integral_constant<int, 1>{}, jj);
-                else tile(std::integral_constant<int, 2>{}, jj);
             }
-            gt += w.n;
-            const int g_last = gt - 1;
-            if (w.n > 0) {
+            gt += n;
+            // The group that has had the last tile finishes the unit; the other one leaves it its references and sums and goes on to the next unit, whose first tile
+            // is its own. (It cannot come by with those of the unit after that before they are read: its tiles follow this group's.)
+            const int g_last = gt - 1, parity = NG == 2 ? ui & 1 : 0;
+            const bool finishes = NG == 1 || ((n > 0 ? g_last : gt) & 1) == group;
+            if (n > 0 && !ok) l = __int_as_float(0x7fc00000);
+            sums[((parity * NG + group) * 2 + half) * 128 + row] = make_float2(m_ref, l);
+            if (!finishes) {
+                if (n > 0) {
+                    asm volatile("bar.arrive %0, 512;" ::"r"(9 + parity) : "memory");
+                    ++ui;
+                }
+                leave();
+                continue;
+            }
+            if (n > 0) {
                 ok = ok && wait(L::PVDONE + (g_last & 3), (uint32_t)(g_last >> 2) & 1u, 12);
-                if (bad_unit[ui & 7] == (uint32_t)ui + 1u || !ok) l = __int_as_float(0x7fc00000);
+                if (NG == 2) asm volatile("bar.sync %0, 512;" ::"r"(9 + parity) : "memory");
             }
-            // the row's sum: the groups' references may differ, the latest one is the largest
-            if (w.n == 0) asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");        // (the last unit's results may still be on their way out of there; else the tiles' weights have kept all warps together)
-            sums[(group * 2 + half) * 128 + row] = make_float2(m_ref, l);
-            asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");
+            if (NG == 1 || n == 0) group_sync();
+            // the row's sum: references may differ, the latest one is the largest
             {
-                float2 all[2 * NG];
+                float2 part_of[2 * NG];
                 m_ref = -INFINITY;
 #pragma unroll
-                for (int q = 0; q < 2 * NG; ++q) { all[q] = sums[q * 128 + row]; m_ref = fmaxf(m_ref, all[q].x); }
+                for (int q = 0; q < 2 * NG; ++q) {
+                    part_of[q] = q / 2 == group || n > 0 ? sums[(parity * 2 * NG + q) * 128 + row] : make_float2(-INFINITY, 0.f);
+                    m_ref = fmaxf(m_ref, part_of[q].x);
+                }
                 l = 0.f;
 #pragma unroll
-                for (int q = 0; q < 2 * NG; ++q) l += all[q].x == m_ref ? all[q].y : all[q].x == -INFINITY ? all[q].y * 0.f : all[q].y * ex2((all[q].x - m_ref) * sc);
+                for (int q = 0; q < 2 * NG; ++q) l += part_of[q].x == m_ref ? part_of[q].y : part_of[q].x == -INFINITY ? part_of[q].y * 0.f : part_of[q].y * ex2((part_of[q].x - m_ref) * sc);
             }
+            const bool met_bad = n > 0 && bad_unit[ui & 7] == (uint32_t)ui + 1u;
+            if (met_bad || !ok) l = __int_as_float(0x7fc00000);
+            if (met_bad && gtid == 0) report_bad_page(p.g.status, u.b);
             tc_fence_after();
-            if (w.n > 0 && tid == 0 && bad_unit[ui & 7] == (uint32_t)ui + 1u) report_bad_page(p.g.status, s.b);
-            const float inv = l == 0.f || w.n == 0 || (m_ref == -INFINITY && l == l) ? 0.f : 1.f / l;
-            constexpr int PARTS = 2 * NG;            // threads of a row, which share its columns
-            const int me = group * 2 + half;
-            auto take = [&](int col, auto &o) {
-                if constexpr (sizeof(o) == 128) tmem_ld32(tmem_base + lane_addr + col, o); else tmem_ld16(tmem_base + lane_addr + col, o);
-                tmem_wait_ld();
-            };
+            const float inv = l == 0.f || n == 0 || (m_ref == -INFINITY && l == l) ? 0.f : 1.f / l;
             auto release = [&] {                     // all of this thread's columns of O are in registers: the next unit may overwrite it
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0 && w.n > 0) mbar_arrive_cluster(leader_ofree);
+                if (lane == 0 && n > 0) mbar_arrive_cluster(leader_ofree);
             };
-            if (!whole) {
-                if (me == 0 && row_live) part.ml[(size_t)slot * kChunkRows + rank * 128 + row] = make_float2(m_ref == -INFINITY ? -INFINITY : m_ref * part.scale_log2, l);
-                constexpr int EC = D / PARTS, W = EC < 32 ? EC : 32;
+            const int token0 = u.token + (int)rank * tile_tokens, live_rows = min(tile_tokens * G, (u.n_rows - token0) * G), slot = u.slot;
+            const bool row_live = row < live_rows;
+            if (slot >= 0) {
+                if (half == 0 && row_live) part.ml[(size_t)slot * kChunkRows + rank * 128 + row] = make_float2(m_ref == -INFINITY ? -INFINITY : m_ref * part.scale_log2, l);
 #pragma unroll 1
-                for (int c = 0; c < EC; c += W) {
-                    uint32_t o[W];
-                    take(me * EC + c, o);
-                    if (c + W == EC) release();
+                for (int c = 0; c < D / 2; c += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(tmem_base + lane_addr + half * (D / 2) + c, o);
+                    tmem_wait_ld();
+                    if (c + 32 == D / 2) release();
                     if (row_live) {
 #pragma unroll
-                        for (int i = 0; i < W; i += 8) st_global_v8(partial8(part, slot, D, (int)rank * 128 + row, me * EC + c + i), *reinterpret_cast<const uint32_t(*)[8]>(o + i));
+                        for (int i = 0; i < 32; i += 8) st_global_v8(partial8(part, slot, D, (int)rank * 128 + row, half * (D / 2) + c + i), *reinterpret_cast<const uint32_t(*)[8]>(o + i));
                     }
                 }
-                asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");        // every thread has read the sums before the next unit's maxima land there
-                if (w.k0 == 0 && tid == 0 && rank == 0) {
-                    const int f = 2 * w.u.tile * rows_here;
-                    PageSplit m2 = {s.b, s.row0, f, min(2 * rows_here, s.n * G - f), w.u.h, shares.owner(w.u.at + w.u.cost - 1), rows_here, 0};
-                    part.meta[pair] = m2;
-                }
             } else {
-                // O / l, 64 columns at a time through the two halves of the staging area, then whole 128-byte pieces of rows to memory
-                constexpr int SC = 64 / PARTS;          // columns of a thread
-                __nv_bfloat16 *tile_out = (__nv_bfloat16 *)p.out + ((size_t)(s.row0 + token0) * p.g.Hq + w.u.h * G) * D;
+                // O / l, 64 columns at a time through the group's staging area, then whole 128-byte pieces of rows to memory
+                __nv_bfloat16 *tile_out = (__nv_bfloat16 *)p.out + ((size_t)(u.row0 + token0) * p.g.Hq + u.h * G) * D;
 #pragma unroll 1
                 for (int rnd = 0; rnd < D / 64; ++rnd) {
-                    uint32_t o[SC];
-                    take(rnd * 64 + me * SC, o);
+                    uint32_t o[32];
+                    tmem_ld32(tmem_base + lane_addr + rnd * 64 + half * 32, o);
+                    tmem_wait_ld();
                     if (rnd == D / 64 - 1) release();
-                    uint8_t *srow = smem + L::OFF_STAGE + (rnd & 1) * (128 * 128) + row * 128;
+                    uint8_t *area = smem + L::OFF_STAGE + group * (128 * 128), *srow = area + row * 128;
+                    if (rnd > 0) group_sync();        // (read before it is written again)
 #pragma unroll
-                    for (int c = 0; c < SC / 8; ++c) {
+                    for (int c = 0; c < 4; ++c) {
                         float f[8];
 #pragma unroll
                         for (int k = 0; k < 8; ++k) f[k] = inv == 0.f ? 0.f : __uint_as_float(o[8 * c + k]) * inv;      // (the accumulator of a unit without keys was never written)
-                        *reinterpret_cast<uint4 *>(srow + (((me * (SC / 8) + c) ^ (row & 7)) << 4)) =
+                        *reinterpret_cast<uint4 *>(srow + (((half * 4 + c) ^ (row & 7)) << 4)) =
                             make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
                     }
-                    asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");
+                    group_sync();
 #pragma unroll
-                    for (int k = 0; k < 128 / RP; ++k) {
-                        const int r = k * RP + (tid >> 3);
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = k * 32 + (gtid >> 3);
                         if (r < live_rows)
-                            *reinterpret_cast<uint4 *>(tile_out + out_at[k] + rnd * 64) =
-                                *reinterpret_cast<const uint4 *>(smem + L::OFF_STAGE + (rnd & 1) * (128 * 128) + r * 128 + (((tid & 7) ^ (r & 7)) << 4));
+                            *reinterpret_cast<uint4 *>(tile_out + out_row[r] + (gtid & 7) * 8 + rnd * 64) = *reinterpret_cast<const uint4 *>(area + r * 128 + (((gtid & 7) ^ (r & 7)) << 4));
                     }
                 }
-                if (D == 64) asm volatile("bar.sync 9, %0;" ::"n"(256 * NG) : "memory");      // (one round: its half, and the sums, may not be overwritten before they are read)
             }
-            if (w.n > 0) ++ui;
-        } while (step(w));
+            leave();
+            group_sync();          // (the staging area, and the sums of one group, may be written again)
+            if (n > 0) ++ui;
+        }
     }
 
     tc_fence_before();
@@ -689,7 +778,7 @@ static cudaError_t launch_chunk(const PageAttention &a, const PagePartials &part
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = k != a.g.k ? 2 : 1;         // (early start behind the widening alone: what it reads first is not written there)
     count_launch();
     return cudaLaunchKernelEx(&cfg, page_chunk_kernel<HD, D>, tq, tk, tv, a, part, tokens, box);
 }

@@ -100,11 +100,10 @@ page_token_kernel(const PageAttention p, const PagePartials part)
     const int G = g.Hq / g.Hkv;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    const PageLine<TokSpanOf<ROWS>> line{p, {p, G}};
-    int longest;
-    const int total = line.total(lane, longest);
+    PageLine<TokSpanOf<ROWS>> line{p, {p, G}};
+    const int total = line.begin(lane);
     // No more CTAs than leave each the square root of a tenth of the longest unit: a partial costs the merge a tenth of what a block costs here.
-    const int least = max(1, (int)sqrtf((float)longest * 0.1f));
+    const int least = max(1, (int)sqrtf((float)line.longest * 0.1f));
     const int nc = min((int)gridDim.x, (total + least - 1) / least);
     const int cta = blockIdx.x;
     if (threadIdx.x == 0) part.meta[cta].b = -1;
