@@ -1,60 +1,69 @@
 // Rows into pages (reflex_pages_write: keys rotated, both quantised on the way) and back (reflex_pages_read). Both are bound by memory.
 #include "pages.cuh"
+#include "sm100_ptx.cuh"
 
 namespace reflex {
 
 constexpr int kRowThreads = 256;
 
-// One row's 16 elements of this thread into its place in the page. The TPR threads of a row agree on its largest magnitude first.
-// e0, e1: the first elements of the two chunks of 8 that the thread holds.
-template <typename T, int FMT, int TPR>
-__device__ __forceinline__ void put_row(const PageGeom &g, void *pool, uint8_t *exps, size_t row, bool live, int e0, int e1, int lane_in_row, const float *a, const float *b)
+// largest magnitude of 8 elements as its bit pattern in fp32 (the order of magnitudes is that of their patterns; a NaN's are above all others)
+template <typename T>
+__device__ __forceinline__ uint32_t largest8(const Raw8<T> &r)
 {
-    if constexpr (FMT == REFLEX_PAGE_SAME) {
-        if (!live) return;
-        store8((T *)pool + row * g.d + e0, a);
-        store8((T *)pool + row * g.d + e1, b);
+    if constexpr (sizeof(T) == 2) {
+        const uint32_t m = __vmaxu2(__vmaxu2(r.w[0].x & 0x7fff7fffu, r.w[0].y & 0x7fff7fffu), __vmaxu2(r.w[0].z & 0x7fff7fffu, r.w[0].w & 0x7fff7fffu));
+        return max(m << 16, m & 0xffff0000u);
     } else {
-        // magnitudes as bit patterns: their order is that of the numbers, and a NaN's is above all of them
-        uint32_t top = 0;
+        uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, max(__float_as_uint(a[i]) & 0x7fffffffu, __float_as_uint(b[i]) & 0x7fffffffu));
-#pragma unroll
-        for (int o = TPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (!live) return;
-        const int e = row_exponent<FMT>(top);
-        const float inv = e == 255 ? 0.f : __int_as_float((254 - e) << 23);       // 2^-(e - 127); a row that is NaN holds zeros (its elements are not looked at)
-        uint8_t *dst = (uint8_t *)pool + row * g.d;
-        uint2 wa = make_uint2(0u, 0u), wb = wa;
-        if (e != 255) {
-            wa = make_uint2(quantise4<FMT>(a, inv), quantise4<FMT>(a + 4, inv));
-            wb = make_uint2(quantise4<FMT>(b, inv), quantise4<FMT>(b + 4, inv));
-        }
-        *reinterpret_cast<uint2 *>(dst + e0) = wa;
-        *reinterpret_cast<uint2 *>(dst + e1) = wb;
-        if (lane_in_row == 0) exps[row] = (uint8_t)e;
+        for (int i = 0; i < 2; ++i) m = max(max(m, max(r.w[i].x & 0x7fffffffu, r.w[i].y & 0x7fffffffu)), max(r.w[i].z & 0x7fffffffu, r.w[i].w & 0x7fffffffu));
+        return m;
     }
 }
 
-template <typename T, int FMT, int TPR>
-__global__ void __launch_bounds__(kRowThreads)
+// The 16 elements that this thread has of a row, into the row's place in the page; `top`: their largest magnitude. The TPR threads of a row agree on the row's.
+template <int FMT, int TPR>
+__device__ __forceinline__ void put_bytes(const PageGeom &g, void *pool, uint8_t *exps, size_t row, bool live, int e0, int e1, int lane_in_row, uint32_t top, float *a, float *b)
+{
+#pragma unroll
+    for (int o = TPR / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (!live) return;
+    const int e = row_exponent<FMT>(top);
+    if (top > 0x7f000000u) {             // (larger than 2^127, or not finite: such a row holds zeros, and its elements are not looked at)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            a[i] = e == 255 ? 0.f : fminf(fmaxf(a[i], -0x1p127f), 0x1p127f);
+            b[i] = e == 255 ? 0.f : fminf(fmaxf(b[i], -0x1p127f), 0x1p127f);
+        }
+    }
+    const float inv = e == 255 ? 1.f : __int_as_float((254 - e) << 23);       // 2^-(e - 127)
+    uint8_t *dst = (uint8_t *)pool + row * g.d;
+    *reinterpret_cast<uint2 *>(dst + e0) = make_uint2(quantise4<FMT>(a, inv), quantise4<FMT>(a + 4, inv));
+    *reinterpret_cast<uint2 *>(dst + e1) = make_uint2(quantise4<FMT>(b, inv), quantise4<FMT>(b + 4, inv));
+    if (lane_in_row == 0) exps[row] = (uint8_t)e;
+}
+
+// A thread has 16 elements of a token's key rows and value rows, for several heads: eight pairs of the rotation (or, behind R, 16 neighbours).
+template <typename T, int FMT, int TPR, bool TURNS>
+__global__ void __launch_bounds__(kRowThreads, TURNS ? 2 : 4)
 page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64_t ldk, const T *v, int64_t ldv, int n_rows, const PageRotation r, int heads_per_thread)
 {
     extern __shared__ int cu_s[];
     load_cu(q, cu_s);
     constexpr int per_block = kRowThreads / TPR;
     const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-    const int R = r.rot.R;
-    const bool turns = lane * 16 < R, adj = r.rot.adjacent != 0;
+    const int R = TURNS ? r.rot.R : 0;
+    const bool turns = lane * 16 < R, adj = TURNS && r.rot.adjacent != 0;
     const int e0 = turns && !adj ? lane * 8 : lane * 16, e1 = turns && !adj ? lane * 8 + R / 2 : lane * 16 + 8;
-    TurnRate rate[8];
-    int axis[8];
-    if (turns) {
+    TurnRate rate[TURNS ? 8 : 1];
+    uint32_t axes = 0;              // four bits each
+    if (TURNS && turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            axis[i] = r.rot.axis[lane * 8 + i];
-            rate[i] = turn_rate(r.rot.freq[lane * 8 + i]);
-            if (axis[i] >= r.rot.axes) { axis[i] = 0; rate[i].lo = rate[i].hi = 0u; }
+            const int axis = r.rot.axis[lane * 8 + i];
+            rate[TURNS ? i : 0] = turn_rate(r.rot.freq[lane * 8 + i]);
+            if (axis >= r.rot.axes) rate[TURNS ? i : 0].lo = rate[TURNS ? i : 0].hi = 0u;
+            else axes |= (uint32_t)axis << (4 * i);
         }
     }
     __syncthreads();
@@ -63,71 +72,97 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
     // (whole warps stay in the loop: the threads of a row exchange their maxima)
     for (int64_t t0 = (int64_t)blockIdx.x * per_block; t0 < end; t0 += (int64_t)gridDim.x * per_block) {
         const int64_t t = t0 + sub;
-        bool live = t < end && t >= cu_s[0];
+        const bool exists = t < end && t >= cu_s[0];
+        const T *kr = k + (exists ? t : 0) * ldk, *vr = v + (exists ? t : 0) * ldv;
+        bool live = exists;
         size_t base = 0;
-        if (live) {
-            const int b = find_seq(cu_s, q.B, (int)t);
-            const int64_t at = (int64_t)q.len[b] - cu_s[b + 1] + t;
-            const int page = at >= 0 && at <= 0x7fffffff ? page_at(q, g.n_pages, b, (int)(at >> g.log_p)) : -1;
-            live = page >= 0;
-            if (live) base = page_row(g, page, 0) + (size_t)(at & (g.P - 1));
-            else if (lane == 0 && blockIdx.y == 0) report_bad_page(g.status, b);
-        }
-        float s[8], c[8];
-        if (turns && live) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) turn(rate[i], r.pos[(size_t)axis[i] * n_rows + t], s[i], c[i]);
-        }
+        float s[TURNS ? 8 : 1], c[TURNS ? 8 : 1];
         for (int h = h0; h < h1; ++h) {
-            float a[8], b[8], va[8], vb[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] = b[i] = va[i] = vb[i] = 0.f;
-            if (live) {
-                const T *kr = k + t * ldk + (size_t)h * g.d, *vr = v + t * ldv + (size_t)h * g.d;
-                load8(kr + e0, a); load8(kr + e1, b);
-                load8(vr + e0, va); load8(vr + e1, vb);
+            Raw8<T> ka = {}, kb = {}, va = {}, vb = {};
+            if (exists) {
+                ka = raw8(kr + (size_t)h * g.d + e0); kb = raw8(kr + (size_t)h * g.d + e1);
+                va = raw8(vr + (size_t)h * g.d + e0); vb = raw8(vr + (size_t)h * g.d + e1);
             }
-            if (turns && live) {
+            if (h == h0 && exists) {            // (while the first rows are on their way)
+                if (TURNS && turns) {
+#pragma unroll
+                    for (int i = 0; i < (TURNS ? 8 : 1); ++i) turn(rate[i], r.pos[(size_t)((axes >> (4 * i)) & 15u) * n_rows + t], s[i], c[i]);
+                }
+                const int b = find_seq(cu_s, q.B, (int)t);
+                const int64_t at = (int64_t)q.len[b] - cu_s[b + 1] + t;
+                const int page = at >= 0 && at <= 0x7fffffff ? page_at(q, g.n_pages, b, (int)(at >> g.log_p)) : -1;
+                live = page >= 0;
+                if (live) base = page_row(g, page, 0) + (size_t)(at & (g.P - 1));
+                else if (lane == 0 && blockIdx.y == 0) report_bad_page(g.status, b);
+            }
+            const size_t row = base + ((size_t)h << g.log_p);
+            float u[8], w[8];
+            if (TURNS || FMT != REFLEX_PAGE_SAME) { widen8(ka, u); widen8(kb, w); }
+            if (TURNS && turns) {
                 if (adj) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float &u = i < 4 ? a[2 * i] : b[2 * i - 8], &w = i < 4 ? a[2 * i + 1] : b[2 * i - 7];
-                        const float u0 = u, w0 = w;
-                        u = u0 * c[i] - w0 * s[i];
-                        w = u0 * s[i] + w0 * c[i];
+                    for (int i = 0; i < (TURNS ? 8 : 1); ++i) {
+                        float &p0 = i < 4 ? u[2 * i] : w[2 * i - 8], &p1 = i < 4 ? u[2 * i + 1] : w[2 * i - 7];
+                        const float u0 = p0, w0 = p1;
+                        p0 = u0 * c[i] - w0 * s[i];
+                        p1 = u0 * s[i] + w0 * c[i];
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float u0 = a[i], w0 = b[i];
-                        a[i] = u0 * c[i] - w0 * s[i];
-                        b[i] = u0 * s[i] + w0 * c[i];
+                    for (int i = 0; i < (TURNS ? 8 : 1); ++i) {
+                        const float u0 = u[i], w0 = w[i];
+                        u[i] = u0 * c[i] - w0 * s[i];
+                        w[i] = u0 * s[i] + w0 * c[i];
                     }
                 }
             }
-            const size_t row = base + ((size_t)h << g.log_p);
-            put_row<T, FMT, TPR>(g, g.k, g.ke, row, live, e0, e1, lane, a, b);
-            put_row<T, FMT, TPR>(g, g.v, g.ve, row, live, e0, e1, lane, va, vb);
+            if constexpr (FMT == REFLEX_PAGE_SAME) {
+                if (live) {
+                    T *kd = (T *)g.k + row * g.d, *vd = (T *)g.v + row * g.d;
+                    if (TURNS) { store8(kd + e0, u); store8(kd + e1, w); }
+                    else
+#pragma unroll
+                        for (int i = 0; i < (int)sizeof(T) / 2; ++i) { reinterpret_cast<uint4 *>(kd + e0)[i] = ka.w[i]; reinterpret_cast<uint4 *>(kd + e1)[i] = kb.w[i]; }
+#pragma unroll
+                    for (int i = 0; i < (int)sizeof(T) / 2; ++i) { reinterpret_cast<uint4 *>(vd + e0)[i] = va.w[i]; reinterpret_cast<uint4 *>(vd + e1)[i] = vb.w[i]; }
+                }
+            } else {
+                uint32_t top;
+                if (TURNS) {
+                    top = 0;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) top = max(top, max(__float_as_uint(u[i]) & 0x7fffffffu, __float_as_uint(w[i]) & 0x7fffffffu));
+                } else top = max(largest8<T>(ka), largest8<T>(kb));
+                put_bytes<FMT, TPR>(g, g.k, g.ke, row, live, e0, e1, lane, top, u, w);
+                widen8(va, u); widen8(vb, w);
+                put_bytes<FMT, TPR>(g, g.v, g.ve, row, live, e0, e1, lane, max(largest8<T>(va), largest8<T>(vb)), u, w);
+            }
         }
     }
 }
 
-// 16 elements of a row from its page: raw bits in, dtype out
+// 16 elements of a row from its page: as they lie there (bytes in the first register), and out in dtype
+template <typename T, int FMT> struct Piece { uint4 w[FMT == REFLEX_PAGE_SAME ? (int)sizeof(T) : 1]; int e; };
 template <typename T, int FMT>
-__device__ __forceinline__ void get16(const void *pool, const uint8_t *exps, size_t row, int d, int e0, bool ok, T *dst)
+__device__ __forceinline__ Piece<T, FMT> take16(const void *pool, const uint8_t *exps, size_t row, int d, int e0)
+{
+    constexpr int W = FMT == REFLEX_PAGE_SAME ? (int)sizeof(T) : 1;          // 16-byte pieces
+    Piece<T, FMT> p;
+#pragma unroll
+    for (int i = 0; i < W; ++i) p.w[i] = reinterpret_cast<const uint4 *>((const uint8_t *)pool + (row * d + e0) * W)[i];
+    p.e = FMT == REFLEX_PAGE_SAME ? 0 : exps[row];
+    return p;
+}
+template <typename T, int FMT>
+__device__ __forceinline__ void give16(const Piece<T, FMT> &p, bool ok, T *dst)
 {
     if constexpr (FMT == REFLEX_PAGE_SAME) {
-        constexpr int W = (int)sizeof(T);          // 16-byte pieces in 16 elements: 2 or 4
-        uint4 w[W];
-#pragma unroll
-        for (int i = 0; i < W; ++i) w[i] = ok ? reinterpret_cast<const uint4 *>((const T *)pool + row * d + e0)[i] : make_uint4(0u, 0u, 0u, 0u);
         const uint32_t nan = sizeof(T) == 2 ? 0x7fc07fc0u : 0x7fc00000u;
 #pragma unroll
-        for (int i = 0; i < W; ++i) reinterpret_cast<uint4 *>(dst)[i] = ok ? w[i] : make_uint4(nan, nan, nan, nan);
+        for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4 *>(dst)[i] = ok ? p.w[i] : make_uint4(nan, nan, nan, nan);
     } else {
-        const uint4 w = ok ? *reinterpret_cast<const uint4 *>((const uint8_t *)pool + row * d + e0) : make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t sc = exponent_bf16x2(ok ? exps[row] : 255);
-        const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+        const uint32_t sc = exponent_bf16x2(ok ? p.e : 255);
+        const uint32_t in[4] = {p.w[0].x, p.w[0].y, p.w[0].z, p.w[0].w};
         uint32_t o[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -135,8 +170,7 @@ __device__ __forceinline__ void get16(const void *pool, const uint8_t *exps, siz
             o[2 * i + 1] = bf16x2_mul(bytes_to_bf16x2<FMT, 2, 3>(in[i], in[i]), sc);
         }
         if constexpr (sizeof(T) == 2) {
-            reinterpret_cast<uint4 *>(dst)[0] = make_uint4(o[0], o[1], o[2], o[3]);
-            reinterpret_cast<uint4 *>(dst)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+            ptx::st_global_v8(dst, o);
         } else {
             float f[16];
 #pragma unroll
@@ -147,33 +181,45 @@ __device__ __forceinline__ void get16(const void *pool, const uint8_t *exps, siz
     }
 }
 
-// A block takes `per_block` pieces of 16 elements of one (sequence, layer), in the order in which the pages hold them: [page][head][slot][piece].
-template <typename T, int FMT>
+// A block takes DEPTH pieces of 16 elements per thread of one (sequence, layer), K and V, in the order in which the pages hold them: [page][head][slot][piece];
+// all are asked for before the first is written.
+template <typename T, int FMT, int DEPTH>
 __global__ void __launch_bounds__(kRowThreads)
-page_read_kernel(const PageGeom g, const reflex_page_batch q, const int32_t *start, T *k_out, T *v_out, int n_layers, int S_out, int per_block)
+page_read_kernel(const PageGeom g, const reflex_page_batch q, const int32_t *start, T *k_out, T *v_out, int n_layers, int S_out, int log_pieces)
 {
     const int b = blockIdx.z, l = blockIdx.y;
     const int len = q.len[b], from = start ? max(0, start[b]) : 0;
     const int first_page = from >> g.log_p;
-    const int pieces = g.d >> 4;
-    const int page_pieces = g.Hkv * g.P * pieces;
     const int64_t end = min((int64_t)len, (int64_t)from + S_out);               // positions [from, end)
     const size_t layer_rows = (size_t)g.n_pages * g.Hkv * g.P * l;
     const size_t out0 = ((size_t)b * n_layers + l) * S_out;
-    const int64_t i0 = (int64_t)blockIdx.x * per_block;
-    if (((i0 / page_pieces + first_page) << g.log_p) >= end) return;
-    for (int i = threadIdx.x; i < per_block; i += kRowThreads) {
-        const int64_t v = i0 + i;
-        const int idx = (int)(v / page_pieces) + first_page, in_page = (int)(v % page_pieces);
-        const int piece = in_page % pieces, hs = in_page / pieces, slot = hs & (g.P - 1), h = hs >> g.log_p;
+    const int per_head = g.log_p + log_pieces;                                  // (page, head) blocks of 2^per_head pieces
+    const int64_t i0 = (int64_t)blockIdx.x * (DEPTH * kRowThreads) + threadIdx.x;
+    Piece<T, FMT> pk[DEPTH], pv[DEPTH];
+    int64_t out[DEPTH];                  // -1: none
+    bool ok[DEPTH];
+#pragma unroll
+    for (int j = 0; j < DEPTH; ++j) {
+        const int64_t v = i0 + j * kRowThreads;
+        const int64_t block = v >> per_head;
+        const int idx = first_page + (int)(g.Hkv == 1 ? block : (int64_t)((uint32_t)block / (uint32_t)g.Hkv)), h = g.Hkv == 1 ? 0 : (int)((uint32_t)block % (uint32_t)g.Hkv);
+        const int piece = (int)v & ((1 << log_pieces) - 1), slot = (int)(v >> log_pieces) & (g.P - 1);
         const int64_t pos = ((int64_t)idx << g.log_p) + slot;
+        out[j] = -1;
         if (pos < from || pos >= end) continue;
         const int page = page_at(q, g.n_pages, b, idx);
+        ok[j] = page >= 0;
         if (page < 0 && piece == 0) report_bad_page(g.status, b);
         const size_t row = layer_rows + (page < 0 ? 0 : page_row(g, page, h) + slot);
-        const size_t o = ((out0 + (size_t)(pos - from)) * g.Hkv + h) * g.d + piece * 16;
-        get16<T, FMT>(g.k, g.ke, row, g.d, piece * 16, page >= 0, k_out + o);
-        get16<T, FMT>(g.v, g.ve, row, g.d, piece * 16, page >= 0, v_out + o);
+        out[j] = (int64_t)(((out0 + (size_t)(pos - from)) * g.Hkv + h) * g.d + piece * 16);
+        pk[j] = take16<T, FMT>(g.k, g.ke, row, g.d, piece * 16);
+        pv[j] = take16<T, FMT>(g.v, g.ve, row, g.d, piece * 16);
+    }
+#pragma unroll
+    for (int j = 0; j < DEPTH; ++j) {
+        if (out[j] < 0) continue;
+        give16<T, FMT>(pk[j], ok[j], k_out + out[j]);
+        give16<T, FMT>(pv[j], ok[j], v_out + out[j]);
     }
 }
 
@@ -204,7 +250,10 @@ cudaError_t launch_page_write(const PageGeom &g, const reflex_page_batch &q, con
     return by_format(dtype, format, [&](auto zero, auto f) {
         using T = decltype(zero);
         constexpr int FMT = decltype(f)::value;
-        auto go = [&](auto w) { page_write_kernel<T, FMT, decltype(w)::value><<<grid, kRowThreads, smem, st>>>(g, q, (const T *)k, ldk, (const T *)v, ldv, n_rows, r, hpt); };
+        auto go = [&](auto w) {
+            if (r.rot.R) page_write_kernel<T, FMT, decltype(w)::value, true><<<grid, kRowThreads, smem, st>>>(g, q, (const T *)k, ldk, (const T *)v, ldv, n_rows, r, hpt);
+            else page_write_kernel<T, FMT, decltype(w)::value, false><<<grid, kRowThreads, smem, st>>>(g, q, (const T *)k, ldk, (const T *)v, ldv, n_rows, r, hpt);
+        };
         if (tpr == 2) go(std::integral_constant<int, 2>{});
         else if (tpr == 4) go(std::integral_constant<int, 4>{});
         else if (tpr == 8) go(std::integral_constant<int, 8>{});
@@ -215,14 +264,21 @@ cudaError_t launch_page_write(const PageGeom &g, const reflex_page_batch &q, con
 cudaError_t launch_page_read(const PageGeom &g, const reflex_page_batch &q, const int32_t *start, void *k_out, void *v_out, int n_layers, int S_out, int dtype,
                              int format, cudaStream_t st)
 {
-    const int per_block = 4 * kRowThreads;
     // (a sequence that starts inside a page reaches into one page more)
     const int64_t pieces = (((int64_t)S_out + g.P - 1) / g.P + 1) * g.Hkv * g.P * (g.d / 16);
-    const dim3 grid((unsigned)((pieces + per_block - 1) / per_block), (unsigned)n_layers, (unsigned)q.B);
+    const int log_pieces = g.d == 32 ? 1 : g.d == 64 ? 2 : g.d == 128 ? 3 : 4;
     count_launch();
     return by_format(dtype, format, [&](auto zero, auto f) {
         using T = decltype(zero);
-        page_read_kernel<T, decltype(f)::value><<<grid, kRowThreads, 0, st>>>(g, q, start, (T *)k_out, (T *)v_out, n_layers, S_out, per_block);
+        constexpr int FMT = decltype(f)::value;
+        auto go = [&](auto depth) {
+            constexpr int DEPTH = decltype(depth)::value;
+            const dim3 grid((unsigned)((pieces + DEPTH * kRowThreads - 1) / (DEPTH * kRowThreads)), (unsigned)n_layers, (unsigned)q.B);
+            page_read_kernel<T, FMT, DEPTH><<<grid, kRowThreads, 0, st>>>(g, q, start, (T *)k_out, (T *)v_out, n_layers, S_out, log_pieces);
+        };
+        // one piece a thread where that gives no more blocks than fit the device at once, else as many as keep 64 bytes or more of K and of V in flight
+        if (pieces * n_layers * q.B <= 148ll * 8 * kRowThreads) go(std::integral_constant<int, 1>{});
+        else go(std::integral_constant<int, FMT == REFLEX_PAGE_SAME ? 8 / (int)sizeof(T) / 2 : 4>{});
     });
 }
 

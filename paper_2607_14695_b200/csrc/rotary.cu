@@ -8,13 +8,13 @@
 namespace reflex {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotHeads = 4;          // rows whose loads are in flight together
 
 // slots [0, R / 16) are eight pairs each; the d - R elements behind them are copied, 16 a slot
 template <typename T, bool ADJ>
-__global__ void __launch_bounds__(kRotThreads)
+__global__ void __launch_bounds__(kRotThreads, 2)
 rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotation r, int n, int H, int d, int heads_per_thread)
 {
+    constexpr int ROWS = 8 / (int)sizeof(T);          // rows whose loads are in flight together: 128 bytes a thread
     const int slots = d >> 4, R = r.rot.R;
     const int per_block = kRotThreads / slots;
     const int slot = threadIdx.x % slots, sub = threadIdx.x / slots;
@@ -23,49 +23,53 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
     // first elements of the two chunks of 8 that the slot holds: pairs (c, c + R / 2), or neighbours
     const int e0 = turns && !ADJ ? slot * 8 : slot * 16, e1 = turns && !ADJ ? slot * 8 + R / 2 : slot * 16 + 8;
     TurnRate rate[8];
-    int axis[8];
+    uint32_t axes = 0;              // four bits each
     if (turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            axis[i] = r.rot.axis[slot * 8 + i];
+            const int axis = r.rot.axis[slot * 8 + i];
             rate[i] = turn_rate(r.rot.freq[slot * 8 + i]);
-            if (axis[i] >= r.rot.axes) { axis[i] = 0; rate[i].lo = rate[i].hi = 0u; }
+            if (axis >= r.rot.axes) rate[i].lo = rate[i].hi = 0u;
+            else axes |= (uint32_t)axis << (4 * i);
         }
     }
     const int h0 = blockIdx.y * heads_per_thread, h1 = min(H, h0 + heads_per_thread);
     for (int64_t t = (int64_t)blockIdx.x * per_block + sub; t < n; t += (int64_t)gridDim.x * per_block) {
-        float s[8], c[8];
-        if (turns) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                turn(rate[i], r.pos[(size_t)axis[i] * n + t], s[i], c[i]);
-                if (r.inverse) s[i] = -s[i];
-            }
-        }
         const T *xr = x + t * ldx;
         T *yr = y + t * ldy;
-        for (int h = h0; h < h1; h += kRotHeads) {
-            float a[kRotHeads][8], b[kRotHeads][8];
+        float s[8], c[8];
+        for (int h = h0; h < h1; h += ROWS) {
+            Raw8<T> a[ROWS], b[ROWS];
 #pragma unroll
-            for (int k = 0; k < kRotHeads; ++k) {
-                if (h + k < h1) { load8(xr + (size_t)(h + k) * d + e0, a[k]); load8(xr + (size_t)(h + k) * d + e1, b[k]); }
+            for (int k = 0; k < ROWS; ++k) {
+                if (h + k < h1) { a[k] = raw8(xr + (size_t)(h + k) * d + e0); b[k] = raw8(xr + (size_t)(h + k) * d + e1); }
+            }
+            if (h == h0 && turns) {          // (while the first rows are on their way)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    turn(rate[i], r.pos[(size_t)((axes >> (4 * i)) & 15u) * n + t], s[i], c[i]);
+                    if (r.inverse) s[i] = -s[i];
+                }
             }
 #pragma unroll
-            for (int k = 0; k < kRotHeads; ++k) {
+            for (int k = 0; k < ROWS; ++k) {
                 if (h + k >= h1) break;
+                float u[8], v[8];
+                widen8(a[k], u);
+                widen8(b[k], v);
                 if (turns) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         // (adjacent: pair i is elements 2i, 2i + 1 of the 16)
-                        float &u = ADJ ? (i < 4 ? a[k][2 * i] : b[k][2 * i - 8]) : a[k][i];
-                        float &v = ADJ ? (i < 4 ? a[k][2 * i + 1] : b[k][2 * i - 7]) : b[k][i];
-                        const float u0 = u, v0 = v;
-                        u = u0 * c[i] - v0 * s[i];
-                        v = u0 * s[i] + v0 * c[i];
+                        float &p0 = ADJ ? (i < 4 ? u[2 * i] : v[2 * i - 8]) : u[i];
+                        float &p1 = ADJ ? (i < 4 ? u[2 * i + 1] : v[2 * i - 7]) : v[i];
+                        const float u0 = p0, v0 = p1;
+                        p0 = u0 * c[i] - v0 * s[i];
+                        p1 = u0 * s[i] + v0 * c[i];
                     }
                 }
-                store8(yr + (size_t)(h + k) * d + e0, a[k]);
-                store8(yr + (size_t)(h + k) * d + e1, b[k]);
+                store8(yr + (size_t)(h + k) * d + e0, u);
+                store8(yr + (size_t)(h + k) * d + e1, v);
             }
         }
     }
@@ -80,7 +84,7 @@ cudaError_t launch_rotary_axes(const void *x, int64_t ldx, void *y, int64_t ldy,
     hpt = hpt < 1 ? 1 : hpt > H ? H : hpt;
     const int groups = (H + hpt - 1) / hpt;
     int gx = (n + per_block - 1) / per_block;
-    const int most = (148 * 16 + groups - 1) / groups;
+    const int most = (148 * 8 + groups - 1) / groups;
     if (gx > most) gx = most;
     const dim3 grid((unsigned)gx, (unsigned)groups);
     count_launch();
