@@ -184,9 +184,10 @@ struct PagePartials {
     float scale_log2;
 };
 __device__ __forceinline__ float *partial8(const PagePartials &part, size_t slot, int d, int r, int c0) { return part.o + ((slot * (size_t)(d >> 3) + (size_t)(c0 >> 3)) * part.rows + r) * 8; }
-int page_token_ctas(int sm_count);
+constexpr int kMostCtas = 512;              // of a launch that leaves partial results
 int page_token_rows(int dtype, int format, int d, int G, int rows);
-cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int ctas, cudaStream_t st);
+// ctas: how many were launched
+cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int sm_count, int &ctas, cudaStream_t st);
 bool page_chunk_takes(int dtype, int G, int d);
 cudaError_t launch_page_widen(const PageAttention &a, void *k_wide, void *v_wide, int format, int sm_count, cudaStream_t st);
 // k, v: one layer's pages in bf16

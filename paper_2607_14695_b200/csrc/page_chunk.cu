@@ -723,14 +723,14 @@ page_widen_kernel(const PageAttention p, __nv_bfloat16 *k_wide, __nv_bfloat16 *v
             const int in_page = (int)(i % per_page);
             const size_t row = (size_t)page * g.Hkv * g.P + in_page / pieces, at = row * g.d + (in_page % pieces) * 16;
             const uint4 kw = *reinterpret_cast<const uint4 *>((const uint8_t *)g.k + at), vw = *reinterpret_cast<const uint4 *>((const uint8_t *)g.v + at);
-            const uint32_t ks = exponent_bf16x2(g.ke[row]), vs = exponent_bf16x2(g.ve[row]);
+            const uint32_t ks = exponent_bf16x2<FMT>(g.ke[row]), vs = exponent_bf16x2<FMT>(g.ve[row]);
             auto put = [&](const uint4 &q, uint32_t sc, __nv_bfloat16 *dst) {
                 const uint32_t in[4] = {q.x, q.y, q.z, q.w};
                 uint32_t o[8];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    o[2 * e] = bf16x2_mul(bytes_to_bf16x2<FMT, 0, 1>(in[e], in[e]), sc);
-                    o[2 * e + 1] = bf16x2_mul(bytes_to_bf16x2<FMT, 2, 3>(in[e], in[e]), sc);
+                    o[2 * e] = bf16x2_mul(expand2<FMT, 0, 1>(biased<FMT>(in[e])), sc);
+                    o[2 * e + 1] = bf16x2_mul(expand2<FMT, 2, 3>(biased<FMT>(in[e])), sc);
                 }
                 st_global_v8(dst, o);
             };

@@ -9,7 +9,7 @@
 namespace reflex {
 
 constexpr int kMergeThreads = 256;
-constexpr int kMergeMost = 512;           // CTAs of an attention launch, at most
+constexpr int kMergeMost = kMostCtas;
 constexpr int kMergeLong = 16;            // partials of a unit from which on its list is cut
 
 struct MergeSum { float m, l, o[8]; };
@@ -65,20 +65,25 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int ctas)
     // (sequences are marked before this kernel, and the marks go when its last block is done: all blocks see the same)
     bool marked = false;
     for (int b = tid; b < p.q.B; b += kMergeThreads) marked |= part.careful[b] != 0;
-    int pieces[kMergeMost / kMergeThreads];
+    int pieces[2], of[2];
 #pragma unroll
-    for (int k = 0; k < kMergeMost / kMergeThreads; ++k) {
-        const int c = tid * (kMergeMost / kMergeThreads) + k;
+    for (int k = 0; k < 2; ++k) {
+        const int c = 2 * tid + k;
         pieces[k] = 0;
+        of[k] = -1;
         if (c < ctas) {
             const PageSplit m = part.meta[c];
-            if (m.b >= 0 && !part.careful[m.b]) {
-                const int per = m.last - c + 1 > kMergeLong ? 32 : 256;
-                pieces[k] = (m.rows * groups + per - 1) / per;
-            }
+            of[k] = m.b;
+            const int per = m.last - c + 1 > kMergeLong ? 32 : 256;
+            if (m.b >= 0) pieces[k] = (m.rows * groups + per - 1) / per;
         }
     }
     const bool any_marked = __syncthreads_or(marked);
+    if (any_marked) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (of[k] >= 0 && part.careful[of[k]]) pieces[k] = 0;
+    }
     {
         const int mine = pieces[0] + pieces[1];
         int incl = mine;

@@ -15,7 +15,7 @@ __device__ __forceinline__ void load8_page(const void *pool, size_t at, float *f
     if constexpr (FMT == REFLEX_PAGE_SAME) load8((const T *)pool + at, f);
     else {
         const uint2 w = *reinterpret_cast<const uint2 *>((const uint8_t *)pool + at);
-        const uint32_t o[4] = {bytes_to_bf16x2<FMT, 0, 1>(w.x, w.x), bytes_to_bf16x2<FMT, 2, 3>(w.x, w.x), bytes_to_bf16x2<FMT, 0, 1>(w.y, w.y), bytes_to_bf16x2<FMT, 2, 3>(w.y, w.y)};
+        const uint32_t o[4] = {expand2<FMT, 0, 1>(biased<FMT>(w.x)), expand2<FMT, 2, 3>(biased<FMT>(w.x)), expand2<FMT, 0, 1>(biased<FMT>(w.y)), expand2<FMT, 2, 3>(biased<FMT>(w.y))};
 #pragma unroll
         for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(o[i] << 16); f[2 * i + 1] = __uint_as_float(o[i] & 0xffff0000u); }
     }
@@ -53,7 +53,7 @@ __device__ __forceinline__ void page_plain_row(const PageAttention &p, int b, in
 #pragma unroll
                 for (int e = 0; e < 8; ++e) s = fmaf(k8[e], q_s[i + e], s);
             }
-            if constexpr (FMT != REFLEX_PAGE_SAME) { s *= exponent_f32(g.ke[at]); vs = exponent_f32(g.ve[at]); }
+            if constexpr (FMT != REFLEX_PAGE_SAME) { s *= exponent_f32<FMT>(g.ke[at]); vs = exponent_f32<FMT>(g.ve[at]); }
             s *= p.scale;
         }
         float top = s;
@@ -80,7 +80,7 @@ __device__ __forceinline__ void page_plain_row(const PageAttention &p, int b, in
                 if constexpr (FMT == REFLEX_PAGE_SAME) v = (float)((const T *)g.v)[vat + lane + 32 * i];
                 else {
                     const uint32_t w8 = ((const uint8_t *)g.v)[vat + lane + 32 * i];
-                    v = __uint_as_float(bytes_to_bf16x2<FMT, 0, 0>(w8, w8) << 16);
+                    v = __uint_as_float(expand2<FMT, 0, 0>(biased<FMT>(w8)) << 16);
                 }
                 acc[i] = fmaf(wj, v, acc[i]);
             }

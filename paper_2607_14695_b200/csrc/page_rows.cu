@@ -161,13 +161,13 @@ __device__ __forceinline__ void give16(const Piece<T, FMT> &p, bool ok, T *dst)
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T); ++i) reinterpret_cast<uint4 *>(dst)[i] = ok ? p.w[i] : make_uint4(nan, nan, nan, nan);
     } else {
-        const uint32_t sc = exponent_bf16x2(ok ? p.e : 255);
+        const uint32_t sc = exponent_bf16x2<FMT>(ok ? p.e : 255);
         const uint32_t in[4] = {p.w[0].x, p.w[0].y, p.w[0].z, p.w[0].w};
         uint32_t o[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            o[2 * i] = bf16x2_mul(bytes_to_bf16x2<FMT, 0, 1>(in[i], in[i]), sc);
-            o[2 * i + 1] = bf16x2_mul(bytes_to_bf16x2<FMT, 2, 3>(in[i], in[i]), sc);
+            o[2 * i] = bf16x2_mul(expand2<FMT, 0, 1>(biased<FMT>(in[i])), sc);
+            o[2 * i + 1] = bf16x2_mul(expand2<FMT, 2, 3>(biased<FMT>(in[i])), sc);
         }
         if constexpr (sizeof(T) == 2) {
             ptx::st_global_v8(dst, o);

@@ -1,19 +1,21 @@
 // Attention of few new tokens per sequence over pages (reflex_pages_attention): one token of each stream, or a handful.
 //
 // Bound by memory: the keys and values of a (sequence, KV head) are read once for its G query heads and a tile of 8 or 16 rows (token, head).
-// Nothing is staged in shared memory: a thread asks for 16-byte pieces of the rows in the pages, and what it gets are its operands of
-// mma.m16n8k16 as they lie there, because the order of the contraction is free. With g = lane / 4 and t = lane % 4:
+// A thread asks for 16-byte pieces of the rows in the pages by cp.async and reads back its own, which are its operands of mma.m16n8k16 as they
+// lie there, because the order of the contraction is free: no barrier, no swizzle, no transposition. With g = lane / 4 and t = lane % 4:
 //   S^T = K Q^T, 16 keys by 8 query rows: thread (g, t) takes pieces of keys g and g + 8; four consecutive elements of the pieces of t = 0 .. 3 are the
 //     16 of one step over head_dim (two of a thread's for the lower half of the step, two for the upper), and Q is put down in that order;
 //   O^T = V^T P^T: thread (g, t) takes the same columns, chosen by g, of keys 2t, 2t + 1, 2t + 8, 2t + 9; a pair of keys in a register is one byte
 //     permutation, and in 8-bit formats the one that unpacks them anyway. P^T comes out of S^T's accumulators by movmatrix.
 // 8-bit rows stay unscaled in the products (they are exact in bf16): 2^e of a key scales its logits, 2^e of a value the key's weight, in fp32.
-// A warp walks every fourth block of 16 keys with a running maximum; K of the next block is asked for as soon as this one's logits exist, V
-// as soon as its products are issued, so that 6 KB or more per warp are on their way all the time.
+// A warp walks every fourth block of 16 keys with a running maximum and has two or three blocks on their way while it works on one: 150 KB or more per SM.
+// (With one block at a time in registers the loads' latency was 6000 cycles a block: 45 us for 64 streams of 3300 keys.)
 //
 // The keys of all (sequence, row tile, KV head) units form one line that the CTAs share evenly, whatever the lengths; a unit that more than one
 // CTA works on leaves fp32 partials, which page_merge_kernel joins in the order of the keys (results do not depend on timing).
 #include <math.h>
+
+#include <algorithm>
 
 #include "page_attention.cuh"
 #include "sm100_ptx.cuh"
@@ -36,17 +38,11 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
     return d;
 }
-__device__ __forceinline__ uint4 load_piece(const uint8_t *p)
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src)
 {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
-}
-__device__ __forceinline__ uint2 load_half_piece(const uint8_t *p)
-{
-    uint2 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-    return v;
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
 
 template <int FMT, int HD, int NT> struct Tok {
@@ -56,15 +52,23 @@ template <int FMT, int HD, int NT> struct Tok {
     static constexpr int KP = ROW / 64;                            // 16-byte pieces of a key per thread
     static constexpr int KEPP = BYTES ? 16 : 8;                    // elements of a piece of K
     static constexpr int VB = ROW / 8;                             // bytes of a value row per thread: 8, 16, 32, 64
+    static constexpr int VP = VB < 16 ? 1 : VB / 16;               // ... in pieces, of 8 bytes or 16
+    static constexpr int VPB = VB < 16 ? 8 : 16;
     static constexpr int VW = VB / 4;                              // ... in words
     static constexpr int VCOLS = VB < 16 ? 8 : BYTES ? 16 : 8;     // consecutive columns of a thread
     static constexpr int VPIECES = HD / 8 / VCOLS;
     static constexpr int ROWS = 8 * NT;
     static constexpr int OSTRIDE = HD + 4;                         // floats of a row of O in shared memory
-    static constexpr uint32_t OFF_O = 0;                           // [warps][ROWS][OSTRIDE]
-    static constexpr uint32_t OFF_Q = OFF_O + kTokWarps * ROWS * OSTRIDE * 4;      // [step][NT][lane] of two registers
+    // a warp's blocks of keys: pieces of K, [2 KP][lane], pieces of V, [4 VP][lane], exponents
+    static constexpr uint32_t K_BYTES = 2 * KP * 32 * 16, V_BYTES = 4 * VP * 32 * VPB;
+    static constexpr uint32_t STAGE = K_BYTES + V_BYTES + (BYTES ? 32 : 0);
+    static constexpr int STAGES = STAGE > 6 * 1024 ? 2 : STAGE > 3 * 1024 ? 3 : 4;
+    static constexpr uint32_t O_BYTES = ROWS * OSTRIDE * 4;        // a warp's share of O takes the place of its keys in the end
+    static constexpr uint32_t WARP = (STAGES * STAGE > O_BYTES ? STAGES * STAGE : O_BYTES);
+    static constexpr uint32_t OFF_Q = kTokWarps * WARP;            // [step][NT][lane] of two registers
     static constexpr uint32_t OFF_ML = OFF_Q + STEPS * NT * 256;   // [warps][ROWS] of (maximum, sum)
     static constexpr uint32_t SMEM = OFF_ML + kTokWarps * ROWS * 8;
+    static constexpr int CTAS = SMEM > 113 * 1024 ? 1 : HD * NT > 256 ? 2 : HD * NT > 64 ? 3 : 4;         // per SM
 };
 
 // the blocks of keys that a tile of ROWS rows needs
@@ -86,18 +90,19 @@ struct TokSpanOf {
 };
 
 template <int FMT, int HD, int NT>
-__global__ void __launch_bounds__(32 * kTokWarps, 2)
+__global__ void __launch_bounds__(32 * kTokWarps, (Tok<FMT, HD, NT>::CTAS))
 page_token_kernel(const PageAttention p, const PagePartials part)
 {
     using C = Tok<FMT, HD, NT>;
     constexpr int ROWS = C::ROWS;
     extern __shared__ __align__(16) uint8_t smem[];
-    float *o_s = reinterpret_cast<float *>(smem + C::OFF_O);
     uint2 *q_s = reinterpret_cast<uint2 *>(smem + C::OFF_Q);
     float2 *ml_s = reinterpret_cast<float2 *>(smem + C::OFF_ML);
     const PageGeom &g = p.g;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, t4 = lane & 3;
     const int G = g.Hq / g.Hkv;
+    uint8_t *keys = smem + warp * C::WARP;             // this warp's stages
+    const uint32_t keys_at = smem_u32(keys);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     PageLine<TokSpanOf<ROWS>> line{p, {p, G}};
@@ -115,6 +120,8 @@ page_token_kernel(const PageAttention p, const PagePartials part)
     for (int x = x0; x < x1;) {
         const PageSeq s = u.s;
         const TokSpan span = u.sp;
+        const int t_first = u.tile * ROWS / G, m_first = u.tile * ROWS - t_first * G, rows_here = min(ROWS, s.n * G - u.tile * ROWS);
+        auto token_of = [&](int r) -> int { return G == 1 ? r : (int)__umulhi((uint32_t)(m_first + r), p.g_magic); };        // of the tile's row r, from t_first on
         const int rt = u.tile, h = u.h, b = s.b;
         const int k0 = x - u.at, k1 = min(u.cost, x1 - u.at);
         const int kend = min(k1, span.count);
@@ -122,10 +129,10 @@ page_token_kernel(const PageAttention p, const PagePartials part)
         __syncthreads();             // (the last unit's results and Q have been read)
         for (int i = threadIdx.x; i < C::STEPS * NT * 32; i += 32 * kTokWarps) {
             const int ln = i & 31, nt = (i >> 5) % NT, step = (i >> 5) / NT;
-            const int r = rt * ROWS + nt * 8 + (ln >> 2);
+            const int r = nt * 8 + (ln >> 2), t = token_of(r);
             const int d0 = (C::BYTES ? 64 * (step >> 2) + 16 * (ln & 3) + 4 * (step & 3) : 32 * (step >> 1) + 8 * (ln & 3) + 4 * (step & 1));
             uint2 v = make_uint2(0u, 0u);
-            if (r < s.n * G) v = *reinterpret_cast<const uint2 *>((const __nv_bfloat16 *)p.qry + ((size_t)(s.row0 + r / G) * g.Hq + h * G + r % G) * HD + d0);
+            if (r < rows_here) v = *reinterpret_cast<const uint2 *>((const __nv_bfloat16 *)p.qry + ((size_t)(s.row0 + t_first + t) * g.Hq + h * G + m_first + r - t * G) * HD + d0);
             q_s[i] = v;
         }
         __syncthreads();
@@ -134,13 +141,13 @@ page_token_kernel(const PageAttention p, const PagePartials part)
         int lo_r[2 * NT], hi_r[2 * NT], lo_min, lo_max, hi_min, hi_max;      // (the limits of all the tile's rows)
 #pragma unroll
         for (int i = 0; i < 2 * NT; ++i) {
-            const int r = min(rt * ROWS + (i >> 1) * 8 + 2 * t4 + (i & 1), s.n * G - 1);
-            const PageRange v = page_range(s, p, r / G, r / G);
+            const int t = t_first + token_of(min((i >> 1) * 8 + 2 * t4 + (i & 1), rows_here - 1));
+            const PageRange v = page_range(s, p, t, t);
             lo_r[i] = v.lo; hi_r[i] = v.hi;
         }
         {
-            const int t_last = (min((rt + 1) * ROWS, s.n * G) - 1) / G;
-            const PageRange first = page_range(s, p, rt * ROWS / G, rt * ROWS / G), last = page_range(s, p, t_last, t_last);
+            const int t_last = t_first + token_of(rows_here - 1);
+            const PageRange first = page_range(s, p, t_first, t_first), last = page_range(s, p, t_last, t_last);
             lo_min = first.lo; hi_min = first.hi; lo_max = last.lo; hi_max = last.hi;
         }
 
@@ -157,9 +164,6 @@ page_token_kernel(const PageAttention p, const PagePartials part)
         bool bad = false;
 
         const int key0 = span.lo + warp * 16;        // keys of block i: key0 + 64 i ..
-        uint4 kr[2][C::KP];
-        uint32_t vr[4][C::VW];
-        int ke[2] = {127, 127}, ve[2] = {127, 127};
         int page_ids = -1, ids_from = k0;
         auto page_of_block = [&](int i) -> int {      // (the pages of 32 blocks are looked up together)
             if (i == k0 || i - ids_from >= 32) {
@@ -169,44 +173,63 @@ page_token_kernel(const PageAttention p, const PagePartials part)
             }
             return __shfl_sync(0xffffffffu, page_ids, i - ids_from);
         };
-        auto row_of = [&](int page, int key) -> size_t { return page_row(g, page, h) + (size_t)(key & (g.P - 1)); };
-        auto load_k = [&](size_t row) {
-            const uint8_t *base = (const uint8_t *)g.k + row * C::ROW + t4 * 16;
+        uint32_t bad_pages = 0;                       // of the blocks on their way, the first in bit 0
+        auto fetch = [&](int i) {                     // (always a group, so that groups can be counted)
+            if (i < kend) {
+                const int key = key0 + i * kTokBlock, page = page_of_block(i);
+                if (page < 0) bad_pages |= 1u << (i - k0 & 31);
+                else bad_pages &= ~(1u << (i - k0 & 31));
+                const size_t row = page_row(g, max(page, 0), h) + (size_t)(key & (g.P - 1));
+                const uint32_t dst = keys_at + (uint32_t)((i - k0) % C::STAGES) * C::STAGE;
+                const uint8_t *kb = (const uint8_t *)g.k + (row + gq) * C::ROW + t4 * 16;
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
+                for (int e = 0; e < 2; ++e)
 #pragma unroll
-                for (int j = 0; j < C::KP; ++j) kr[e][j] = load_piece(base + (size_t)(gq + 8 * e) * C::ROW + j * 64);
-            if constexpr (C::BYTES) { ke[0] = g.ke[row + gq]; ke[1] = g.ke[row + gq + 8]; }
-        };
-        auto load_v = [&](size_t row) {
-            const uint8_t *base = (const uint8_t *)g.v + row * C::ROW + gq * (C::VB < 16 ? 8 : 16);
+                    for (int j = 0; j < C::KP; ++j) copy_async<16>(dst + ((e * C::KP + j) * 32 + lane) * 16, kb + (size_t)(8 * e) * C::ROW + j * 64);
+                const uint8_t *vb = (const uint8_t *)g.v + (row + 2 * t4) * C::ROW + gq * C::VPB;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint8_t *r = base + (size_t)(2 * t4 + (e & 1) + 8 * (e >> 1)) * C::ROW;
-                if constexpr (C::VB < 16) {
-                    const uint2 v = load_half_piece(r);
-                    vr[e][0] = v.x; vr[e][1] = v.y;
-                } else {
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int j = 0; j < C::VB / 16; ++j) {
-                        const uint4 v = load_piece(r + j * 128);
-                        vr[e][4 * j] = v.x; vr[e][4 * j + 1] = v.y; vr[e][4 * j + 2] = v.z; vr[e][4 * j + 3] = v.w;
-                    }
-                }
+                    for (int j = 0; j < C::VP; ++j) copy_async<C::VPB>(dst + C::K_BYTES + ((e * C::VP + j) * 32 + lane) * C::VPB, vb + (size_t)((e & 1) + 8 * (e >> 1)) * C::ROW + j * 128);
+                if constexpr (C::BYTES)
+                    if (lane < 2) copy_async<16>(dst + C::K_BYTES + C::V_BYTES + lane * 16, (lane == 0 ? g.ke : g.ve) + row);
             }
-            if constexpr (C::BYTES) { ve[0] = g.ve[row + gq]; ve[1] = g.ve[row + gq + 8]; }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
         // O^T += V^T P^T of the loaded block; keep: which of this thread's four keys are live (the others count as zeros)
-        auto times_v = [&](const uint32_t (&pt)[NT][2], uint32_t keep) {
+        auto value_word = [&](const uint8_t *stage, int e, int i) -> uint32_t {       // word i of this thread's part of the e-th of its keys
+            return reinterpret_cast<const uint32_t *>(stage + C::K_BYTES + ((e * C::VP + i / (C::VPB / 4)) * 32 + lane) * C::VPB)[i % (C::VPB / 4)];
+        };
+        auto times_v = [&](const uint8_t *stage, const uint32_t (&pt)[NT][2], uint32_t keep, bool finite) {
+            uint32_t v[4][C::VPB / 4];
 #pragma unroll
             for (int i = 0; i < C::VW; ++i) {
+                if (i % (C::VPB / 4) == 0) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint8_t *src = stage + C::K_BYTES + ((e * C::VP + i / (C::VPB / 4)) * 32 + lane) * C::VPB;
+                        if constexpr (C::VPB == 16) *reinterpret_cast<uint4 *>(v[e]) = *reinterpret_cast<const uint4 *>(src);
+                        else *reinterpret_cast<uint2 *>(v[e]) = *reinterpret_cast<const uint2 *>(src);
+                    }
+                }
                 uint32_t w[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) w[e] = (keep >> e) & 1u ? vr[e][i] : 0u;
+                for (int e = 0; e < 4; ++e) {
+                    w[e] = v[e][i % (C::VPB / 4)];
+                    if constexpr (!C::BYTES) {
+                        if (keep != 15u && !((keep >> e) & 1u)) w[e] = 0u;
+                        if (!finite) {
+                            if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
+                            if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0x0000ffffu;
+                        }
+                    }
+                }
                 if constexpr (C::BYTES) {
-                    // four columns of four keys: two tiles of 16 (column, column + 1) pairs
-                    const uint32_t a[8] = {bytes_to_bf16x2<FMT, 0, 0>(w[0], w[1]), bytes_to_bf16x2<FMT, 1, 1>(w[0], w[1]), bytes_to_bf16x2<FMT, 0, 0>(w[2], w[3]), bytes_to_bf16x2<FMT, 1, 1>(w[2], w[3]),
-                                           bytes_to_bf16x2<FMT, 2, 2>(w[0], w[1]), bytes_to_bf16x2<FMT, 3, 3>(w[0], w[1]), bytes_to_bf16x2<FMT, 2, 2>(w[2], w[3]), bytes_to_bf16x2<FMT, 3, 3>(w[2], w[3])};
+                    // four columns of four keys: two tiles of 16 (column, column + 1) pairs. Pairs of keys are put side by side first.
+                    const uint32_t lo01 = biased<FMT>(__byte_perm(w[0], w[1], 0x5140)), hi01 = biased<FMT>(__byte_perm(w[0], w[1], 0x7362));
+                    const uint32_t lo23 = biased<FMT>(__byte_perm(w[2], w[3], 0x5140)), hi23 = biased<FMT>(__byte_perm(w[2], w[3], 0x7362));
+                    const uint32_t a[8] = {expand2<FMT, 0, 1>(lo01), expand2<FMT, 2, 3>(lo01), expand2<FMT, 0, 1>(lo23), expand2<FMT, 2, 3>(lo23),
+                                           expand2<FMT, 0, 1>(hi01), expand2<FMT, 2, 3>(hi01), expand2<FMT, 0, 1>(hi23), expand2<FMT, 2, 3>(hi23)};
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         mma_bf16(o[2 * i][nt], a[0], a[1], a[2], a[3], pt[nt][0], pt[nt][1]);
@@ -220,20 +243,18 @@ page_token_kernel(const PageAttention p, const PagePartials part)
             }
         };
 
-        size_t row = 0;
-        int page = -1;
-        if (k0 < kend) {
-            page = page_of_block(k0);
-            bad |= page < 0 && key0 + k0 * kTokBlock < span.hi;
-            row = row_of(max(page, 0), key0 + k0 * kTokBlock);
-            load_k(row);
-            load_v(row);
-        }
+#pragma unroll
+        for (int i = 0; i < C::STAGES - 1; ++i) fetch(k0 + i);
+#pragma unroll 1
         for (int i = k0; i < kend; ++i) {
             const int key = key0 + i * kTokBlock;
-            const bool more = i + 1 < kend;
-            const int page_next = more ? page_of_block(i + 1) : -1;
-            const size_t row_next = more ? row_of(max(page_next, 0), key + kTokBlock) : 0;
+            __syncwarp();                             // (the exponents of the block before have been read by all lanes)
+            fetch(i + C::STAGES - 1);
+            asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 1) : "memory");
+            __syncwarp();
+            const uint8_t *stage = keys + ((i - k0) % C::STAGES) * C::STAGE;
+            const bool lost = (bad_pages >> (i - k0 & 31)) & 1u;             // no page to read these keys from
+            bad |= lost && key < span.hi;
             // ---- logits ----
             float c[NT][2][4];
 #pragma unroll
@@ -241,26 +262,37 @@ page_token_kernel(const PageAttention p, const PagePartials part)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) c[nt][0][e] = c[nt][1][e] = 0.f;
 #pragma unroll
-            for (int step = 0; step < C::STEPS; ++step) {
-                uint32_t a0, a1, a2, a3;
-                if constexpr (C::BYTES) {
-                    const uint32_t w0 = (&kr[0][step >> 2].x)[step & 3], w1 = (&kr[1][step >> 2].x)[step & 3];
-                    a0 = bytes_to_bf16x2<FMT, 0, 1>(w0, w0); a1 = bytes_to_bf16x2<FMT, 0, 1>(w1, w1);
-                    a2 = bytes_to_bf16x2<FMT, 2, 3>(w0, w0); a3 = bytes_to_bf16x2<FMT, 2, 3>(w1, w1);
-                } else {
-                    a0 = (&kr[0][step >> 1].x)[2 * (step & 1)]; a1 = (&kr[1][step >> 1].x)[2 * (step & 1)];
-                    a2 = (&kr[0][step >> 1].x)[2 * (step & 1) + 1]; a3 = (&kr[1][step >> 1].x)[2 * (step & 1) + 1];
-                }
+            for (int j = 0; j < C::KP; ++j) {
+                uint4 k4[2];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const uint2 q = q_s[(step * NT + nt) * 32 + lane];
-                    mma_bf16(c[nt][step & 1], a0, a1, a2, a3, q.x, q.y);
+                for (int e = 0; e < 2; ++e) k4[e] = *reinterpret_cast<const uint4 *>(stage + ((e * C::KP + j) * 32 + lane) * 16);
+                const uint32_t w0[4] = {k4[0].x, k4[0].y, k4[0].z, k4[0].w}, w1[4] = {k4[1].x, k4[1].y, k4[1].z, k4[1].w};
+#pragma unroll
+                for (int u2 = 0; u2 < (C::BYTES ? 4 : 2); ++u2) {
+                    const int step = j * (C::BYTES ? 4 : 2) + u2;
+                    uint32_t a0, a1, a2, a3;
+                    if constexpr (C::BYTES) {
+                        const uint32_t x0 = biased<FMT>(w0[u2]), x1 = biased<FMT>(w1[u2]);
+                        a0 = expand2<FMT, 0, 1>(x0); a1 = expand2<FMT, 0, 1>(x1);
+                        a2 = expand2<FMT, 2, 3>(x0); a3 = expand2<FMT, 2, 3>(x1);
+                    } else {
+                        a0 = w0[2 * u2]; a1 = w1[2 * u2]; a2 = w0[2 * u2 + 1]; a3 = w1[2 * u2 + 1];
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const uint2 q = q_s[(step * NT + nt) * 32 + lane];
+                        mma_bf16(c[nt][step & 1], a0, a1, a2, a3, q.x, q.y);
+                    }
                 }
             }
-            const float ks0 = C::BYTES ? exponent_f32(ke[0]) * part.scale_log2 : part.scale_log2, ks1 = C::BYTES ? exponent_f32(ke[1]) * part.scale_log2 : part.scale_log2;
-            if (more) load_k(row_next);
+            int ke[2] = {127, 127}, ve[2] = {127, 127};
+            if constexpr (C::BYTES) {
+                const uint8_t *ex = stage + C::K_BYTES + C::V_BYTES;
+                ke[0] = ex[gq]; ke[1] = ex[gq + 8]; ve[0] = ex[16 + gq]; ve[1] = ex[16 + gq + 8];
+            }
+            const float ks0 = C::BYTES ? exponent_f32<FMT>(ke[0]) * part.scale_log2 : part.scale_log2, ks1 = C::BYTES ? exponent_f32<FMT>(ke[1]) * part.scale_log2 : part.scale_log2;
             // ---- masks, running maximum, weights ----
-            const bool whole = key >= lo_max && key + 16 <= hi_min && page >= 0;
+            const bool whole = key >= lo_max && key + 16 <= hi_min && !lost;
             float w[NT][4];            // (key g, row 2t), (g, 2t + 1), (g + 8, 2t), (g + 8, 2t + 1)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -269,7 +301,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                     w[nt][e] = (c[nt][0][e] + c[nt][1][e]) * (e < 2 ? ks0 : ks1);
                     if (!whole) {
                         const int j = key + gq + (e < 2 ? 0 : 8);
-                        if (j < lo_r[2 * nt + (e & 1)] || j >= hi_r[2 * nt + (e & 1)] || page < 0) w[nt][e] = -INFINITY;
+                        if (j < lo_r[2 * nt + (e & 1)] || j >= hi_r[2 * nt + (e & 1)] || lost) w[nt][e] = -INFINITY;
                     }
                 }
             bool grows = false;
@@ -294,7 +326,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                 }
             }
             uint32_t pt[NT][2];
-            const float vs0 = C::BYTES ? exponent_f32(ve[0]) : 1.f, vs1 = C::BYTES ? exponent_f32(ve[1]) : 1.f;
+            const float vs0 = C::BYTES ? exponent_f32<FMT>(ve[0]) : 1.f, vs1 = C::BYTES ? exponent_f32<FMT>(ve[1]) : 1.f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float v[4];
@@ -309,7 +341,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                 pt[nt][1] = transpose8x8(pack_bf16(v[2], v[3]));
             }
             // ---- values ----
-            if (whole || C::BYTES) times_v(pt, 15u);
+            if (whole || C::BYTES) times_v(stage, pt, 15u, true);
             else {
                 // A masked key has weight 0, but 0 times what lies there may be NaN: keys that no row sees count as zeros. A key that some
                 // rows see is multiplied for all of them, which does no harm while it is finite.
@@ -318,13 +350,17 @@ page_token_kernel(const PageAttention p, const PagePartials part)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = key + 2 * t4 + (e & 1) + 8 * (e >> 1);
-                    if (j >= lo_min && j < hi_max && page >= 0) {
+                    if (j >= lo_min && j < hi_max && !lost) {
                         live |= 1u << e;
 #pragma unroll
-                        for (int q = 0; q < C::VW; ++q) odd |= (vr[e][q] & 0x7f80u) == 0x7f80u || (vr[e][q] & 0x7f800000u) == 0x7f800000u;
+                        for (int q = 0; q < C::VW; ++q) {
+                            const uint32_t word = value_word(stage, e, q);
+                            odd |= (word & 0x7f80u) == 0x7f80u || (word & 0x7f800000u) == 0x7f800000u;
+                        }
                     }
                 }
-                if (__any_sync(0xffffffffu, odd)) {
+                const bool any_odd = __any_sync(0xffffffffu, odd);
+                if (any_odd) {
                     // what is not finite goes, as it is, to the rows that see it (whatever their weight), and counts as zero in the products
 #pragma unroll 1
                     for (int from = 0; from < 4; ++from) {
@@ -333,7 +369,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                             const int j = key + 2 * from + (e & 1) + 8 * (e >> 1);
 #pragma unroll
                             for (int i2 = 0; i2 < C::VW; ++i2) {
-                                const uint32_t v = __shfl_sync(0xffffffffu, vr[e][i2], (lane & ~3) | from);
+                                const uint32_t v = __shfl_sync(0xffffffffu, value_word(stage, e, i2), (lane & ~3) | from);
 #pragma unroll
                                 for (int half = 0; half < 2; ++half) {
                                     const uint32_t bits = half ? v & 0xffff0000u : v << 16;
@@ -345,22 +381,12 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                             }
                         }
                     }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int q = 0; q < C::VW; ++q) {
-                            if ((vr[e][q] & 0x7f80u) == 0x7f80u) vr[e][q] &= 0xffff0000u;
-                            if ((vr[e][q] & 0x7f800000u) == 0x7f800000u) vr[e][q] &= 0x0000ffffu;
-                        }
                 }
-                times_v(pt, live);
+                times_v(stage, pt, live, !any_odd);
             }
-            if (more) {
-                load_v(row_next);
-                bad |= page_next < 0 && key + kTokBlock < span.hi;
-            }
-            page = page_next;
         }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncwarp();                                 // (the stages may be written over)
         // ---- the warps' shares meet ----
         const bool any_bad = __any_sync(0xffffffffu, bad);
         if (any_bad && lane == 0) report_bad_page(g.status, b);
@@ -381,7 +407,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
             for (int q = 0; q < kTokWarps; ++q) all = fmaxf(all, ml_s[q * ROWS + rr].x);
             f[r] = m[r] == -INFINITY ? 0.f : ex2(m[r] - all);
             // column c of piece j: 8 VCOLS j + VCOLS g + c; register (tile, 0 / 2) holds an even / odd column of an even row's pair
-            float *dst = o_s + (warp * ROWS + rr) * C::OSTRIDE + gq * C::VCOLS;
+            float *dst = reinterpret_cast<float *>(keys) + rr * C::OSTRIDE + gq * C::VCOLS;
 #pragma unroll
             for (int j = 0; j < C::VPIECES; ++j)
 #pragma unroll
@@ -396,8 +422,8 @@ page_token_kernel(const PageAttention p, const PagePartials part)
         const int slot = 2 * cta + (starts ? 1 : 0);
         for (int i = threadIdx.x; i < ROWS * (HD / 8); i += 32 * kTokWarps) {
             const int r = i / (HD / 8), c0 = i % (HD / 8) * 8;
-            const int rr = rt * ROWS + r;
-            if (rr >= s.n * G) continue;
+            if (r >= rows_here) continue;
+            const int t = token_of(r);
             float all = -INFINITY, sum = 0.f, acc[8];
 #pragma unroll
             for (int q = 0; q < kTokWarps; ++q) all = fmaxf(all, ml_s[q * ROWS + r].x);
@@ -408,7 +434,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                 const float2 v = ml_s[q * ROWS + r];
                 // (a maximum of -inf carries no weight, a sum that is NaN is kept)
                 sum += v.x == -INFINITY ? v.y * 0.f : v.y * ex2(v.x - all);
-                const float4 *src = reinterpret_cast<const float4 *>(o_s + (q * ROWS + r) * C::OSTRIDE + c0);
+                const float4 *src = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem + q * C::WARP) + r * C::OSTRIDE + c0);
                 const float4 y0 = src[0], y1 = src[1];
                 acc[0] += y0.x; acc[1] += y0.y; acc[2] += y0.z; acc[3] += y0.w;
                 acc[4] += y1.x; acc[5] += y1.y; acc[6] += y1.z; acc[7] += y1.w;
@@ -417,7 +443,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[e] *= inv;
-                store8((__nv_bfloat16 *)p.out + ((size_t)(s.row0 + rr / G) * g.Hq + h * G + rr % G) * HD + c0, acc);
+                store8((__nv_bfloat16 *)p.out + ((size_t)(s.row0 + t_first + t) * g.Hq + h * G + m_first + r - t * G) * HD + c0, acc);
             } else {
                 store8(partial8(part, slot, HD, r, c0), acc);
                 if (c0 == 0) part.ml[(size_t)slot * part.rows + r] = make_float2(all, sum);
@@ -433,35 +459,34 @@ page_token_kernel(const PageAttention p, const PagePartials part)
 }
 
 template <int FMT, int HD, int NT>
-static cudaError_t launch_token(const PageAttention &a, const PagePartials &part, int ctas, cudaStream_t st)
+static cudaError_t launch_token(const PageAttention &a, const PagePartials &part, int sm_count, int &ctas, cudaStream_t st)
 {
     using C = Tok<FMT, HD, NT>;
     static std::atomic<unsigned long long> done{0};
     cudaError_t e = once_per_device(done, [] { return cudaFuncSetAttribute(page_token_kernel<FMT, HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM); });
     if (e != cudaSuccess) return e;
     count_launch();
+    ctas = std::min(C::CTAS * sm_count, kMostCtas);
     page_token_kernel<FMT, HD, NT><<<ctas, 32 * kTokWarps, C::SMEM, st>>>(a, part);
     return cudaGetLastError();
 }
 
-int page_token_ctas(int sm_count) { return 2 * sm_count; }
-
 // Rows of a tile for `rows` (token, head) rows per sequence and KV head on average; 0: not for this kernel.
 int page_token_rows(int dtype, int format, int d, int G, int rows)
 {
-    if (dtype != REFLEX_DTYPE_BF16 || d < 64) return 0;
+    if (dtype != REFLEX_DTYPE_BF16 || d < 64 || G > 4096) return 0;
     const bool wide = format == REFLEX_PAGE_SAME && d == 256;         // (16 rows of bf16 rows of 256 do not fit the registers)
     if (rows > (format == REFLEX_PAGE_SAME ? 16 : 64) && page_chunk_takes(dtype, G, d)) return 0;
     return rows <= 8 || wide ? 8 : 16;
 }
 
-cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int ctas, cudaStream_t st)
+cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int sm_count, int &ctas, cudaStream_t st)
 {
     auto go = [&](auto f, auto hd) -> cudaError_t {
         constexpr int FMT = decltype(f)::value, HD = decltype(hd)::value;
         if constexpr (!(FMT == REFLEX_PAGE_SAME && HD == 256))
-            if (rows == 16) return launch_token<FMT, HD, 2>(a, part, ctas, st);
-        return launch_token<FMT, HD, 1>(a, part, ctas, st);
+            if (rows == 16) return launch_token<FMT, HD, 2>(a, part, sm_count, ctas, st);
+        return launch_token<FMT, HD, 1>(a, part, sm_count, ctas, st);
     };
     auto by_d = [&](auto f) -> cudaError_t {
         if (a.g.d == 64) return go(f, std::integral_constant<int, 64>{});

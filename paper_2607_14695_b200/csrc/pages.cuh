@@ -95,29 +95,39 @@ __device__ __forceinline__ uint32_t bf16x2_sub(uint32_t a, uint32_t b)
     return r;
 }
 
-// Two bytes of an 8-bit row (byte I of w0 and byte J of w1) as the two bf16 of a register, unscaled and exact.
-//   int8: with the sign bit s and the seven bits u below it the byte is u - 128 s. 0x4300 | u is 128 + u in bf16 and 0x4300 | (byte & 0x80) is
-//   128 (1 + s): their difference is the byte.
-//   e4m3: sign, four bits of exponent and three of mantissa moved to where bf16 has them give the number times 2^(7 - 127), whether it is
-//   normal or not; the product with 2^120 is exact.
-template <int FMT, int I, int J>
-__device__ __forceinline__ uint32_t bytes_to_bf16x2(uint32_t w0, uint32_t w1)
+__device__ __forceinline__ uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c)
 {
-    if constexpr (FMT == REFLEX_PAGE_INT8) {
-        const uint32_t x = __byte_perm(w0, w1, I | (I << 4) | ((J + 4) << 8) | ((J + 4) << 12));
-        return bf16x2_sub((x & 0x007f007fu) | 0x43004300u, (x & 0x00800080u) | 0x43004300u);
-    } else {
-        const uint32_t x = __byte_perm(w0, w1, (I << 4) | ((J + 4) << 12) | I | ((J + 4) << 8)) & 0xff00ff00u;
-        return bf16x2_mul((x & 0x80008000u) | ((x >> 4) & 0x07f007f0u), 0x7b807b80u);
-    }
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
 }
-// 2^(e - 127) of an exponent byte: as a pair of bf16, and in fp32 (255: NaN)
+
+// Four bytes of an 8-bit row as they are before expand() (int8: plus 128, by the sign bits)
+template <int FMT> __device__ __forceinline__ uint32_t biased(uint32_t w) { return FMT == REFLEX_PAGE_INT8 ? w ^ 0x80808080u : w; }
+// Two bytes, in the low halves of x's halves, as two bf16: exact, times 2^-kExpandShift. Most of it on the FMA pipe: logic operations and byte permutations
+// have half its rate, and the attention of few tokens is bound by them.
+//   int8: a byte u in the low bits of a bf16 is the (subnormal) number u 2^-133; times 2^127, less 128 2^-6, is the whole number times 2^-6.
+//   e4m3: sign, four bits of exponent and three of mantissa moved to where bf16 has them (16 x moves them, and the sign bit's 128 times 240 adds what takes it
+//   from bit 11 to bit 15) give the number times 2^-120, whether it is normal or not; the product with 2^120 is exact.
+template <int FMT> constexpr int kExpandShift = FMT == REFLEX_PAGE_INT8 ? 6 : 0;
+template <int FMT>
+__device__ __forceinline__ uint32_t expand(uint32_t x)
+{
+    if constexpr (FMT == REFLEX_PAGE_INT8) return bf16x2_fma(x, 0x7f007f00u, 0xc000c000u);
+    else return bf16x2_mul((x & 0x00800080u) * 240u + x * 16u, 0x7b807b80u);
+}
+// bytes I and J of a biased word, expanded
+template <int FMT, int I, int J> __device__ __forceinline__ uint32_t expand2(uint32_t w) { return expand<FMT>(__byte_perm(w, 0u, I | 0x40 | (J << 8) | 0x4000)); }
+
+// What expanded numbers of a row are multiplied with: 2^(e - 127 + kExpandShift) of its exponent byte, as a pair of bf16 and in fp32 (255: NaN; writes leave no
+// byte below 27 or above 249)
+template <int FMT>
 __device__ __forceinline__ uint32_t exponent_bf16x2(int e)
 {
-    const uint32_t one = e == 255 ? 0x7fc0u : e == 0 ? 0x0040u : (uint32_t)e << 7;
+    const uint32_t one = e == 255 ? 0x7fc0u : (uint32_t)min(e + kExpandShift<FMT>, 254) << 7;
     return one | (one << 16);
 }
-__device__ __forceinline__ float exponent_f32(int e) { return e == 255 ? __int_as_float(0x7fc00000) : e == 0 ? 0x1p-127f : __int_as_float(e << 23); }
+template <int FMT> __device__ __forceinline__ float exponent_f32(int e) { return e == 255 ? __int_as_float(0x7fc00000) : __int_as_float(min(e + kExpandShift<FMT>, 254) << 23); }
 
 // ---- rotation angles ----
 // A pair's frequency in revolutions per position, modulo 1, as a 64-bit fraction: position times fraction, modulo 2^64, is the fraction of a
@@ -211,6 +221,7 @@ struct PageAttention {
     void *out;
     int n_rows, causal, window;
     float scale;
+    uint32_t g_magic;         // x / (Hq / Hkv) = __umulhi(x, g_magic) for x < 2^16 (and more than one head in a group)
 };
 cudaError_t launch_page_plain(const PageAttention &a, int dtype, int format, cudaStream_t st);
 

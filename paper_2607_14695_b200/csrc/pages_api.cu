@@ -38,7 +38,6 @@ size_t row_bytes(const reflex_pages_desc &d) { return (size_t)d.d * (d.format ==
 // Layout of the workspace: status word, marked sequences, partial results of split units, one layer of pages in bf16 (8-bit formats).
 struct PagesLayout { size_t done, careful, meta, ml, o, wide, bytes; };
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-constexpr int kMostCtas = 512;              // of a launch that leaves partial results (the token kernel: two per SM)
 constexpr int kMostPairs = 128;
 bool widened(const reflex_pages_desc &d) { return d.format != REFLEX_PAGE_SAME && page_chunk_takes(d.dtype, d.Hq / d.Hkv, d.d); }
 PagesLayout pages_layout(const reflex_pages_desc &d)
@@ -234,6 +233,7 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     a.n_rows = n_rows; a.causal = causal; a.window = window;
     a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)d.d);
     const int G = d.Hq / d.Hkv;
+    a.g_magic = G > 1 ? 0xffffffffu / (uint32_t)G + 1u : 0u;
     const long long per_seq = ((long long)n_rows * G + batch->B - 1) / batch->B;           // (token, head) rows of a sequence and KV head
     // (the tensor-core kernels count tiles of rows times blocks of 64 keys in 32 bits)
     if (page_chunk_takes(d.dtype, G, d.d) &&
@@ -250,8 +250,7 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     const int token_rows = page_token_rows(d.dtype, d.format, d.d, G, (int)std::min(per_seq, 1ll << 20));
     if (token_rows) {
         part.rows = token_rows;
-        ctas = std::min(page_token_ctas(p->sm_count), kMostCtas);
-        e = launch_page_token(a, part, d.format, token_rows, ctas, st);
+        e = launch_page_token(a, part, d.format, token_rows, p->sm_count, ctas, st);
     } else if (page_chunk_takes(d.dtype, G, d.d)) {
         part.rows = 256;
         ctas = std::min(p->sm_count / 2, kMostPairs);

@@ -80,7 +80,7 @@ cudaError_t launch_rotary_axes(const void *x, int64_t ldx, void *y, int64_t ldy,
     const int per_block = kRotThreads / (d / 16);
     // heads of a token go to one thread once there are threads enough without them
     const long long rows = (long long)((n + per_block - 1) / per_block) * H;
-    int hpt = (int)(rows / (148 * 8));
+    int hpt = (int)(rows / (148 * 2));
     hpt = hpt < 1 ? 1 : hpt > H ? H : hpt;
     const int groups = (H + hpt - 1) / hpt;
     int gx = (n + per_block - 1) / per_block;
