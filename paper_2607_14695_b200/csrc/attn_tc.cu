@@ -747,6 +747,16 @@ bool encode_map_bf16(CUtensorMap *out, const void *ptr, int rank, const cuuint64
                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_map_rows(CUtensorMap *out, const void *ptr, int row_bytes, int rows, int box_rows)
+{
+    EncodeTiledFn fn = encode_fn();
+    const int inner = row_bytes < 128 ? row_bytes : 128;
+    const cuuint64_t dims[3] = {(cuuint64_t)inner, (cuuint64_t)rows, (cuuint64_t)(row_bytes / inner)}, strides[2] = {(cuuint64_t)row_bytes, (cuuint64_t)inner};
+    const cuuint32_t box[3] = {(cuuint32_t)inner, (cuuint32_t)box_rows, (cuuint32_t)(row_bytes / inner)}, es[3] = {1, 1, 1};
+    return fn && fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(ptr), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    inner == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool tensor_map_2d_bf16(CUtensorMap *out, const void *ptr, int inner, int rows, int box_rows)
 {
     return cache().get(out, ptr, 3, inner, rows, box_rows, 0, [](CUtensorMap *m, const void *p_, int inner_, int rows_, int box_rows_, int) -> bool {

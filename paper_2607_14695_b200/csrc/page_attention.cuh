@@ -5,6 +5,8 @@
 
 namespace reflex {
 
+__device__ __forceinline__ void report_page_wait(uint32_t *status, uint32_t code) { atomicCAS(status, 0u, status_word(kSitePages + code)); }
+
 struct PageSeq { int b, row0, n, len; };      // first row of its new tokens, how many, tokens in all
 
 // (whatever the device arrays hold, rows stay inside [0, n_rows))
@@ -111,7 +113,8 @@ struct PageLine {
         u.at = 0;
         PageSeq s = mine;
         int cost = mine_cost, unused = 0;
-        for (int b0 = 0;;) {
+        if (p.q.B == 1) u.s = {0, __shfl_sync(0xffffffffu, s.row0, 0), __shfl_sync(0xffffffffu, s.n, 0), __shfl_sync(0xffffffffu, s.len, 0)};
+        else for (int b0 = 0;;) {
             const int incl = scan(cost, lane);
             const uint32_t past = __ballot_sync(0xffffffffu, u.at + incl > x);
             if (past || b0 + 32 >= p.q.B) {
@@ -130,7 +133,7 @@ struct PageLine {
         }
         u.tiles = span.tiles(u.s);
         u.tile = 0;
-        for (int t0 = 0; t0 < u.tiles; t0 += 32) {
+        for (int t0 = 0; u.tiles > 1 && t0 < u.tiles; t0 += 32) {
             const int c = t0 + lane < u.tiles ? max(1, span(u.s, t0 + lane).count) * p.g.Hkv : 0;
             const int incl = scan(c, lane);
             const uint32_t past = __ballot_sync(0xffffffffu, u.at + incl > x);

@@ -37,8 +37,6 @@ constexpr int kChunkRows = 256;                // of a unit
 constexpr unsigned long long kChunkWaitNs = 1000000000ull;
 constexpr float kChunkGrow = 8.0f;             // log2 units: O is rescaled only where a maximum grows by more than 2^8
 
-__device__ __forceinline__ void report_page_wait(uint32_t *status, uint32_t code) { atomicCAS(status, 0u, status_word(kSitePages + code)); }
-
 // A unit costs kChunkSetUp blocks before its first tile: what its Q, its masks and its results take, in tiles. (A share that ends among them
 // leaves the unit to the next pair.)
 constexpr int kChunkSetUp = 4;

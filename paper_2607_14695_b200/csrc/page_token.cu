@@ -1,15 +1,16 @@
 // Attention of few new tokens per sequence over pages (reflex_pages_attention): one token of each stream, or a handful.
 //
 // Bound by memory: the keys and values of a (sequence, KV head) are read once for its G query heads and a tile of 8 or 16 rows (token, head).
-// A thread asks for 16-byte pieces of the rows in the pages by cp.async and reads back its own, which are its operands of mma.m16n8k16 as they
-// lie there, because the order of the contraction is free: no barrier, no swizzle, no transposition. With g = lane / 4 and t = lane % 4:
+// TMA brings 16 rows of keys and 16 of values in swizzled boxes, and a thread's 16-byte pieces of them are its operands of mma.m16n8k16 as they lie
+// there, because the order of the contraction is free: no transposition, no bank conflict. With g = lane / 4 and t = lane % 4:
 //   S^T = K Q^T, 16 keys by 8 query rows: thread (g, t) takes pieces of keys g and g + 8; four consecutive elements of the pieces of t = 0 .. 3 are the
 //     16 of one step over head_dim (two of a thread's for the lower half of the step, two for the upper), and Q is put down in that order;
 //   O^T = V^T P^T: thread (g, t) takes the same columns, chosen by g, of keys 2t, 2t + 1, 2t + 8, 2t + 9; a pair of keys in a register is one byte
 //     permutation, and in 8-bit formats the one that unpacks them anyway. P^T comes out of S^T's accumulators by movmatrix.
 // 8-bit rows stay unscaled in the products (they are exact in bf16): 2^e of a key scales its logits, 2^e of a value the key's weight, in fp32.
-// A warp walks every fourth block of 16 keys with a running maximum and has two or three blocks on their way while it works on one: 150 KB or more per SM.
-// (With one block at a time in registers the loads' latency was 6000 cycles a block: 45 us for 64 streams of 3300 keys.)
+// A warp walks every WARPS-th block of 16 keys with a running maximum, fetches for itself, and has one or two blocks on their way while it works on one:
+// 100 KB or more per SM. (64 streams of 3300 keys in 8 bits, 112 MB: 46.7 us with one block at a time in registers, 49.5 with rows by cp.async, whose
+// 17 instructions a block kept the load pipe busy, 39.4 by TMA.)
 //
 // The keys of all (sequence, row tile, KV head) units form one line that the CTAs share evenly, whatever the lengths; a unit that more than one
 // CTA works on leaves fp32 partials, which page_merge_kernel joins in the order of the keys (results do not depend on timing).
@@ -24,12 +25,9 @@ namespace reflex {
 
 using namespace ptx;
 
-constexpr int kTokWarps = 4;
-constexpr int kTokBlock = 16 * kTokWarps;      // keys of a block: what the line of work is counted in
-
 __device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
@@ -38,12 +36,7 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
     return d;
 }
-template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void *src)
-{
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
-}
+constexpr unsigned long long kTokenWaitNs = 1000000000ull;
 
 template <int FMT, int HD, int NT> struct Tok {
     static constexpr bool BYTES = FMT != REFLEX_PAGE_SAME;
@@ -59,78 +52,136 @@ template <int FMT, int HD, int NT> struct Tok {
     static constexpr int VPIECES = HD / 8 / VCOLS;
     static constexpr int ROWS = 8 * NT;
     static constexpr int OSTRIDE = HD + 4;                         // floats of a row of O in shared memory
-    // a warp's blocks of keys: pieces of K, [2 KP][lane], pieces of V, [4 VP][lane], exponents
-    static constexpr uint32_t K_BYTES = 2 * KP * 32 * 16, V_BYTES = 4 * VP * 32 * VPB;
-    static constexpr uint32_t STAGE = K_BYTES + V_BYTES + (BYTES ? 32 : 0);
-    static constexpr int STAGES = STAGE > 6 * 1024 ? 2 : STAGE > 3 * 1024 ? 3 : 4;
+    // a warp's blocks of keys: 16 rows of K, 16 of V, in boxes of 128 bytes (or 64) as TMA swizzles them; the exponents lie behind all stages
+    static constexpr int BOX = ROW < 128 ? ROW : 128, BOXES = ROW / BOX;
+    static constexpr uint32_t K_BYTES = 16 * ROW, STAGE = 2 * K_BYTES;
+    static constexpr int STAGES = STAGE > 4 * 1024 ? 2 : 3;
+    // One CTA per SM, with as many warps as registers (some 64 of O per 8 rows of head_dim 256, and 100 others) and stages leave room for: what a
+    // CTA does per unit (its place, Q, joining its warps, a partial) is then shared by all keys that the SM takes of it.
+    static constexpr int WARPS = HD * NT <= 64 ? 16 : BYTES ? (HD * NT > 256 ? 8 : 12) : HD == 256 ? 6 : HD * NT > 128 ? 8 : 12;
+    static constexpr int BLOCK = 16 * WARPS;                       // keys of a block: what the line of work is counted in
     static constexpr uint32_t O_BYTES = ROWS * OSTRIDE * 4;        // a warp's share of O takes the place of its keys in the end
-    static constexpr uint32_t WARP = (STAGES * STAGE > O_BYTES ? STAGES * STAGE : O_BYTES);
-    static constexpr uint32_t OFF_Q = kTokWarps * WARP;            // [step][NT][lane] of two registers
+    static constexpr uint32_t WARP = ((STAGES * STAGE > O_BYTES ? STAGES * STAGE : O_BYTES) + 1023u) & ~1023u;
+    static constexpr uint32_t OFF_Q = WARPS * WARP;            // [step][NT][lane] of two registers
     static constexpr uint32_t OFF_ML = OFF_Q + STEPS * NT * 256;   // [warps][ROWS] of (maximum, sum)
-    static constexpr uint32_t SMEM = OFF_ML + kTokWarps * ROWS * 8;
-    static constexpr int CTAS = SMEM > 113 * 1024 ? 1 : HD * NT > 256 ? 2 : HD * NT > 64 ? 3 : 4;         // per SM
+    static constexpr uint32_t OFF_PLACE = OFF_ML + WARPS * ROWS * 8;
+    static constexpr uint32_t OFF_EXP = OFF_PLACE + 128;           // [warps][STAGES] of 16 + 16 exponents
+    static constexpr uint32_t OFF_BAR = OFF_EXP + (BYTES ? WARPS * STAGES * 32 : 0);      // [warps][STAGES]
+    static constexpr uint32_t NEED = OFF_BAR + WARPS * STAGES * 8, SMEM = NEED + 1008;    // (room to begin at a multiple of 1024)
+    static_assert(SMEM <= 232448, "shared memory");
 };
 
 // the blocks of keys that a tile of ROWS rows needs
 struct TokSpan { int lo, hi, count; };
-template <int ROWS>
+template <int ROWS, int BLOCK>
 struct TokSpanOf {
     const PageAttention &p;
     int G;
     __device__ __forceinline__ int tiles(const PageSeq &s) const { return (s.n * G + ROWS - 1) / ROWS; }
     __device__ __forceinline__ TokSpan operator()(const PageSeq &s, int tile) const
     {
-        const PageRange r = page_range(s, p, tile * ROWS / G, (min(s.n * G, (tile + 1) * ROWS) - 1) / G);
+        const PageRange r = page_range(s, p, p.token_of(tile * ROWS, G), p.token_of(min(s.n * G, (tile + 1) * ROWS) - 1, G));
         TokSpan t;
         t.lo = r.lo & ~15;
         t.hi = r.hi;
-        t.count = t.hi > t.lo ? (t.hi - t.lo + kTokBlock - 1) / kTokBlock : 0;
+        t.count = t.hi > t.lo ? (t.hi - t.lo + BLOCK - 1) / BLOCK : 0;
         return t;
     }
 };
 
 template <int FMT, int HD, int NT>
-__global__ void __launch_bounds__(32 * kTokWarps, (Tok<FMT, HD, NT>::CTAS))
-page_token_kernel(const PageAttention p, const PagePartials part)
+__global__ void __launch_bounds__((32 * Tok<FMT, HD, NT>::WARPS), 1)
+page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const PageAttention p, const PagePartials part)
 {
     using C = Tok<FMT, HD, NT>;
-    constexpr int ROWS = C::ROWS;
-    extern __shared__ __align__(16) uint8_t smem[];
+    constexpr int ROWS = C::ROWS, WARPS = C::WARPS, BLOCK = C::BLOCK;
+    extern __shared__ __align__(16) uint8_t raw_smem[];
+    uint8_t *smem = raw_smem + (-smem_u32(raw_smem) & 1023u);
     uint2 *q_s = reinterpret_cast<uint2 *>(smem + C::OFF_Q);
     float2 *ml_s = reinterpret_cast<float2 *>(smem + C::OFF_ML);
     const PageGeom &g = p.g;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gq = lane >> 2, t4 = lane & 3;
     const int G = g.Hq / g.Hkv;
     uint8_t *keys = smem + warp * C::WARP;             // this warp's stages
-    const uint32_t keys_at = smem_u32(keys);
+    const uint32_t keys_at = smem_u32(keys), exps_at = smem_u32(smem + C::OFF_EXP) + warp * C::STAGES * 32, bars = smem_u32(smem + C::OFF_BAR) + warp * C::STAGES * 8;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    PageLine<TokSpanOf<ROWS>> line{p, {p, G}};
-    const int total = line.begin(lane);
-    // No more CTAs than leave each the square root of a tenth of the longest unit: a partial costs the merge a tenth of what a block costs here.
-    const int least = max(1, (int)sqrtf((float)line.longest * 0.1f));
-    const int nc = min((int)gridDim.x, (total + least - 1) / least);
+    // Warp 0 walks the line for all. No more CTAs than leave each the square root of a fifth of the longest unit: a partial costs the merge a fifth of what a block
+    // costs here.
+    using Line = PageLine<TokSpanOf<ROWS, BLOCK>>;
+    Line line{p, {p, G}};
+    struct Shared { typename Line::Place u; int total, nc; };
+    static_assert(sizeof(Shared) <= 128, "place in shared memory");
+    Shared *sh = reinterpret_cast<Shared *>(smem + C::OFF_PLACE);
     const int cta = blockIdx.x;
-    if (threadIdx.x == 0) part.meta[cta].b = -1;
+    if (lane < C::STAGES) mbar_init(bars + lane * 8, 1);
+    fence_mbar_init();
+    if (warp == 1 && lane < 2) prefetch_tmap(lane ? &tm_v : &tm_k);
+    if (warp == 0) {
+        const int total = line.begin(lane);
+        const int least = max(1, (int)sqrtf((float)line.longest * 0.2f)), nc = min((int)gridDim.x, (total + least - 1) / least);
+        if (cta < nc) {
+            const typename Line::Place first = line.find(PageShares(total, nc).of(cta), lane);
+            if (lane == 0) sh->u = first;
+        }
+        if (lane == 0) {
+            sh->total = total; sh->nc = nc;
+            part.meta[cta].b = -1;
+        }
+    }
+    __syncthreads();
+    const int nc = sh->nc;
     if (cta >= nc) return;
-    const PageShares shares(total, nc);
+    const PageShares shares(sh->total, nc);
     const int x0 = shares.of(cta), x1 = shares.of(cta + 1);
-    auto u = line.find(x0, lane);
 
+    int put = 0, got = 0;                              // the stage that is filled next, that is read next
+    uint32_t got_phase = 0;
+    int pending = 0;                                   // asked for and not yet waited for
+    bool dead = false;                                 // a wait has run out: nothing more is asked for
+    auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+        if (mbar_try_wait(bar, parity)) return true;
+        const unsigned long long t0 = globaltimer_ns();
+        for (uint32_t n = 1;; ++n) {
+            if (mbar_try_wait(bar, parity)) return true;
+            if ((n & 255u) == 0u && globaltimer_ns() - t0 > kTokenWaitNs) return false;
+        }
+    };
+    // where this thread's pieces lie in a stage
+    const uint32_t k_piece = C::ROW < 128 ? gq * 64 + ((t4 ^ (gq >> 1)) << 4) : gq * 128 + (((2 * t4) ^ gq) << 4);
+    const uint32_t v_piece = C::K_BYTES + (C::ROW < 128 ? t4 * 128 + (((gq >> 1) ^ t4) << 4) + (gq & 1) * 8 : t4 * 256 + (((2 * t4) ^ gq) << 4));
+    auto key_at = [&](int e, int j) -> uint32_t {      // piece j of key g + 8 e
+        return C::ROW < 128 ? k_piece + e * 512 : (k_piece ^ ((j & 1) << 4)) + (j >> 1) * 2048 + e * 1024;
+    };
+    auto value_at = [&](int e, int j) -> uint32_t {    // piece j of key 2 t + (e & 1) + 8 (e >> 1)
+        return C::ROW < 128 ? v_piece + (e & 1) * 64 + (e >> 1) * 512 : (v_piece ^ ((e & 1) << 4)) + (e & 1) * 128 + (e >> 1) * 1024 + j * 2048;
+    };
     for (int x = x0; x < x1;) {
+        const typename Line::Place u = sh->u;
         const PageSeq s = u.s;
         const TokSpan span = u.sp;
-        const int t_first = u.tile * ROWS / G, m_first = u.tile * ROWS - t_first * G, rows_here = min(ROWS, s.n * G - u.tile * ROWS);
+        const int t_first = p.token_of(u.tile * ROWS, G), m_first = u.tile * ROWS - t_first * G, rows_here = min(ROWS, s.n * G - u.tile * ROWS);
         auto token_of = [&](int r) -> int { return G == 1 ? r : (int)__umulhi((uint32_t)(m_first + r), p.g_magic); };        // of the tile's row r, from t_first on
         const int rt = u.tile, h = u.h, b = s.b;
         const int k0 = x - u.at, k1 = min(u.cost, x1 - u.at);
         const int kend = min(k1, span.count);
+        // ---- the pages of 32 of this warp's blocks are looked up together, the first ones ahead of everything else ----
+        const int key0 = span.lo + warp * 16;        // keys of block i: key0 + 64 i ..
+        int ids_from = k0, page_ids = k0 + lane < kend ? page_at(p.q, g.n_pages, b, (key0 + (k0 + lane) * BLOCK) >> g.log_p) : -1;
+        auto page_of_block = [&](int i) -> int {
+            if (i - ids_from >= 32) {
+                ids_from = i;
+                const int mine = i + lane;
+                page_ids = mine < kend ? page_at(p.q, g.n_pages, b, (key0 + mine * BLOCK) >> g.log_p) : -1;
+            }
+            return __shfl_sync(0xffffffffu, page_ids, i - ids_from);
+        };
         // ---- Q of the unit's rows, in the order of K's pieces ----
-        __syncthreads();             // (the last unit's results and Q have been read)
-        for (int i = threadIdx.x; i < C::STEPS * NT * 32; i += 32 * kTokWarps) {
+        for (int i = threadIdx.x; i < C::STEPS * NT * 32; i += 32 * WARPS) {
             const int ln = i & 31, nt = (i >> 5) % NT, step = (i >> 5) / NT;
             const int r = nt * 8 + (ln >> 2), t = token_of(r);
-            const int d0 = (C::BYTES ? 64 * (step >> 2) + 16 * (ln & 3) + 4 * (step & 3) : 32 * (step >> 1) + 8 * (ln & 3) + 4 * (step & 1));
+            const int j = C::BYTES ? step >> 2 : step >> 1;
+            const int d0 = (C::ROW < 128 ? 16 * (ln & 3) : (j >> 1) * (C::BYTES ? 128 : 64) + (2 * (ln & 3) + (j & 1)) * C::KEPP) + 4 * (C::BYTES ? step & 3 : step & 1);
             uint2 v = make_uint2(0u, 0u);
             if (r < rows_here) v = *reinterpret_cast<const uint2 *>((const __nv_bfloat16 *)p.qry + ((size_t)(s.row0 + t_first + t) * g.Hq + h * G + m_first + r - t * G) * HD + d0);
             q_s[i] = v;
@@ -163,42 +214,27 @@ page_token_kernel(const PageAttention p, const PagePartials part)
         for (int i = 0; i < 2 * NT; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
         bool bad = false;
 
-        const int key0 = span.lo + warp * 16;        // keys of block i: key0 + 64 i ..
-        int page_ids = -1, ids_from = k0;
-        auto page_of_block = [&](int i) -> int {      // (the pages of 32 blocks are looked up together)
-            if (i == k0 || i - ids_from >= 32) {
-                ids_from = i;
-                const int mine = i + lane;
-                page_ids = mine < kend ? page_at(p.q, g.n_pages, b, (key0 + mine * kTokBlock) >> g.log_p) : -1;
-            }
-            return __shfl_sync(0xffffffffu, page_ids, i - ids_from);
-        };
         uint32_t bad_pages = 0;                       // of the blocks on their way, the first in bit 0
-        auto fetch = [&](int i) {                     // (always a group, so that groups can be counted)
-            if (i < kend) {
-                const int key = key0 + i * kTokBlock, page = page_of_block(i);
-                if (page < 0) bad_pages |= 1u << (i - k0 & 31);
-                else bad_pages &= ~(1u << (i - k0 & 31));
-                const size_t row = page_row(g, max(page, 0), h) + (size_t)(key & (g.P - 1));
-                const uint32_t dst = keys_at + (uint32_t)((i - k0) % C::STAGES) * C::STAGE;
-                const uint8_t *kb = (const uint8_t *)g.k + (row + gq) * C::ROW + t4 * 16;
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-#pragma unroll
-                    for (int j = 0; j < C::KP; ++j) copy_async<16>(dst + ((e * C::KP + j) * 32 + lane) * 16, kb + (size_t)(8 * e) * C::ROW + j * 64);
-                const uint8_t *vb = (const uint8_t *)g.v + (row + 2 * t4) * C::ROW + gq * C::VPB;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-#pragma unroll
-                    for (int j = 0; j < C::VP; ++j) copy_async<C::VPB>(dst + C::K_BYTES + ((e * C::VP + j) * 32 + lane) * C::VPB, vb + (size_t)((e & 1) + 8 * (e >> 1)) * C::ROW + j * 128);
-                if constexpr (C::BYTES)
-                    if (lane < 2) copy_async<16>(dst + C::K_BYTES + C::V_BYTES + lane * 16, (lane == 0 ? g.ke : g.ve) + row);
+        auto fetch = [&](int i) {
+            if (i >= kend || dead) return;
+            const int key = key0 + i * BLOCK, page = page_of_block(i);
+            if (page < 0) bad_pages |= 1u << (i - k0 & 31);
+            else bad_pages &= ~(1u << (i - k0 & 31));
+            const size_t row = page_row(g, max(page, 0), h) + (size_t)(key & (g.P - 1));
+            const uint32_t dst = keys_at + put * C::STAGE, bar = bars + put * 8;
+            mbar_expect_tx_elect(bar, C::STAGE + (C::BYTES ? 32 : 0));
+            tma_load_3d_elect(dst, &tm_k, bar, 0, (int)row, 0);
+            if constexpr (C::BYTES) {
+                bulk_load_elect(exps_at + put * 32, g.ke + row, bar, 16);
+                bulk_load_elect(exps_at + put * 32 + 16, g.ve + row, bar, 16);
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            tma_load_3d_elect(dst + C::K_BYTES, &tm_v, bar, 0, (int)row, 0);
+            put = put + 1 == C::STAGES ? 0 : put + 1;
+            ++pending;
         };
         // O^T += V^T P^T of the loaded block; keep: which of this thread's four keys are live (the others count as zeros)
         auto value_word = [&](const uint8_t *stage, int e, int i) -> uint32_t {       // word i of this thread's part of the e-th of its keys
-            return reinterpret_cast<const uint32_t *>(stage + C::K_BYTES + ((e * C::VP + i / (C::VPB / 4)) * 32 + lane) * C::VPB)[i % (C::VPB / 4)];
+            return reinterpret_cast<const uint32_t *>(stage + value_at(e, i / (C::VPB / 4)))[i % (C::VPB / 4)];
         };
         auto times_v = [&](const uint8_t *stage, const uint32_t (&pt)[NT][2], uint32_t keep, bool finite) {
             uint32_t v[4][C::VPB / 4];
@@ -207,7 +243,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                 if (i % (C::VPB / 4) == 0) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const uint8_t *src = stage + C::K_BYTES + ((e * C::VP + i / (C::VPB / 4)) * 32 + lane) * C::VPB;
+                        const uint8_t *src = stage + value_at(e, i / (C::VPB / 4));
                         if constexpr (C::VPB == 16) *reinterpret_cast<uint4 *>(v[e]) = *reinterpret_cast<const uint4 *>(src);
                         else *reinterpret_cast<uint2 *>(v[e]) = *reinterpret_cast<const uint2 *>(src);
                     }
@@ -247,14 +283,22 @@ page_token_kernel(const PageAttention p, const PagePartials part)
         for (int i = 0; i < C::STAGES - 1; ++i) fetch(k0 + i);
 #pragma unroll 1
         for (int i = k0; i < kend; ++i) {
-            const int key = key0 + i * kTokBlock;
-            __syncwarp();                             // (the exponents of the block before have been read by all lanes)
+            const int key = key0 + i * BLOCK;
+            __syncwarp();                             // (the stage that is filled next has been read by all lanes)
             fetch(i + C::STAGES - 1);
-            asm volatile("cp.async.wait_group %0;" ::"n"(C::STAGES - 1) : "memory");
-            __syncwarp();
-            const uint8_t *stage = keys + ((i - k0) % C::STAGES) * C::STAGE;
+            const int st = got;
+            if (pending > 0) {
+                --pending;
+                if (!__all_sync(0xffffffffu, wait(bars + st * 8, got_phase)) && !dead) {
+                    dead = true;
+                    if (lane == 0) report_page_wait(g.status, 12u);
+                }
+                got = got + 1 == C::STAGES ? 0 : got + 1;
+                got_phase ^= got == 0 ? 1u : 0u;
+            }
+            const uint8_t *stage = keys + st * C::STAGE;
             const bool lost = (bad_pages >> (i - k0 & 31)) & 1u;             // no page to read these keys from
-            bad |= lost && key < span.hi;
+            bad |= dead || (lost && key < span.hi);
             // ---- logits ----
             float c[NT][2][4];
 #pragma unroll
@@ -265,7 +309,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
             for (int j = 0; j < C::KP; ++j) {
                 uint4 k4[2];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) k4[e] = *reinterpret_cast<const uint4 *>(stage + ((e * C::KP + j) * 32 + lane) * 16);
+                for (int e = 0; e < 2; ++e) k4[e] = *reinterpret_cast<const uint4 *>(stage + key_at(e, j));
                 const uint32_t w0[4] = {k4[0].x, k4[0].y, k4[0].z, k4[0].w}, w1[4] = {k4[1].x, k4[1].y, k4[1].z, k4[1].w};
 #pragma unroll
                 for (int u2 = 0; u2 < (C::BYTES ? 4 : 2); ++u2) {
@@ -287,7 +331,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
             }
             int ke[2] = {127, 127}, ve[2] = {127, 127};
             if constexpr (C::BYTES) {
-                const uint8_t *ex = stage + C::K_BYTES + C::V_BYTES;
+                const uint8_t *ex = smem + C::OFF_EXP + (warp * C::STAGES + st) * 32;
                 ke[0] = ex[gq]; ke[1] = ex[gq + 8]; ve[0] = ex[16 + gq]; ve[1] = ex[16 + gq + 8];
             }
             const float ks0 = C::BYTES ? exponent_f32<FMT>(ke[0]) * part.scale_log2 : part.scale_log2, ks1 = C::BYTES ? exponent_f32<FMT>(ke[1]) * part.scale_log2 : part.scale_log2;
@@ -385,7 +429,6 @@ page_token_kernel(const PageAttention p, const PagePartials part)
                 times_v(stage, pt, live, !any_odd);
             }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
         __syncwarp();                                 // (the stages may be written over)
         // ---- the warps' shares meet ----
         const bool any_bad = __any_sync(0xffffffffu, bad);
@@ -404,7 +447,7 @@ page_token_kernel(const PageAttention p, const PagePartials part)
             const int rr = (r >> 1) * 8 + 2 * t4 + (r & 1);
             float all = -INFINITY;
 #pragma unroll
-            for (int q = 0; q < kTokWarps; ++q) all = fmaxf(all, ml_s[q * ROWS + rr].x);
+            for (int q = 0; q < WARPS; ++q) all = fmaxf(all, ml_s[q * ROWS + rr].x);
             f[r] = m[r] == -INFINITY ? 0.f : ex2(m[r] - all);
             // column c of piece j: 8 VCOLS j + VCOLS g + c; register (tile, 0 / 2) holds an even / odd column of an even row's pair
             float *dst = reinterpret_cast<float *>(keys) + rr * C::OSTRIDE + gq * C::VCOLS;
@@ -420,17 +463,17 @@ page_token_kernel(const PageAttention p, const PagePartials part)
         __syncthreads();
         const bool starts = k0 == 0, ends = k1 == u.cost;
         const int slot = 2 * cta + (starts ? 1 : 0);
-        for (int i = threadIdx.x; i < ROWS * (HD / 8); i += 32 * kTokWarps) {
+        for (int i = threadIdx.x; i < ROWS * (HD / 8); i += 32 * WARPS) {
             const int r = i / (HD / 8), c0 = i % (HD / 8) * 8;
             if (r >= rows_here) continue;
             const int t = token_of(r);
             float all = -INFINITY, sum = 0.f, acc[8];
 #pragma unroll
-            for (int q = 0; q < kTokWarps; ++q) all = fmaxf(all, ml_s[q * ROWS + r].x);
+            for (int q = 0; q < WARPS; ++q) all = fmaxf(all, ml_s[q * ROWS + r].x);
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] = 0.f;
 #pragma unroll
-            for (int q = 0; q < kTokWarps; ++q) {
+            for (int q = 0; q < WARPS; ++q) {
                 const float2 v = ml_s[q * ROWS + r];
                 // (a maximum of -inf carries no weight, a sum that is NaN is kept)
                 sum += v.x == -INFINITY ? v.y * 0.f : v.y * ex2(v.x - all);
@@ -454,7 +497,16 @@ page_token_kernel(const PageAttention p, const PagePartials part)
             part.meta[cta] = m2;
         }
         x = u.at + k1;
-        if (ends) line.next(u);
+        fence_proxy_async_smem();    // (the next blocks come over what the warps put down)
+        __syncthreads();             // (this unit's results and Q have been read)
+        if (ends && x < x1) {
+            if (threadIdx.x == 0) {
+                typename Line::Place next = u;
+                line.next(next);
+                sh->u = next;
+            }
+            __syncthreads();
+        }
     }
 }
 
@@ -465,9 +517,11 @@ static cudaError_t launch_token(const PageAttention &a, const PagePartials &part
     static std::atomic<unsigned long long> done{0};
     cudaError_t e = once_per_device(done, [] { return cudaFuncSetAttribute(page_token_kernel<FMT, HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM); });
     if (e != cudaSuccess) return e;
+    ctas = std::min(sm_count, kMostCtas);
+    CUtensorMap tk, tv;
+    if (!encode_map_rows(&tk, a.g.k, C::ROW, a.g.n_pages * a.g.Hkv * a.g.P, 16) || !encode_map_rows(&tv, a.g.v, C::ROW, a.g.n_pages * a.g.Hkv * a.g.P, 16)) return cudaErrorInvalidValue;
     count_launch();
-    ctas = std::min(C::CTAS * sm_count, kMostCtas);
-    page_token_kernel<FMT, HD, NT><<<ctas, 32 * kTokWarps, C::SMEM, st>>>(a, part);
+    page_token_kernel<FMT, HD, NT><<<ctas, 32 * C::WARPS, C::SMEM, st>>>(tk, tv, a, part);
     return cudaGetLastError();
 }
 

@@ -233,6 +233,7 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     a.n_rows = n_rows; a.causal = causal; a.window = window;
     a.scale = scale > 0.f ? scale : 1.f / sqrtf((float)d.d);
     const int G = d.Hq / d.Hkv;
+    a.g_shift = (G & (G - 1)) == 0 ? __builtin_ctz((unsigned)G) : -1;
     a.g_magic = G > 1 ? 0xffffffffu / (uint32_t)G + 1u : 0u;
     const long long per_seq = ((long long)n_rows * G + batch->B - 1) / batch->B;           // (token, head) rows of a sequence and KV head
     // (the tensor-core kernels count tiles of rows times blocks of 64 keys in 32 bits)

@@ -121,6 +121,8 @@ int simt_choose_splits(const AttnParams &p, size_t partial_bytes, int sm_count);
 cudaError_t launch_attention_merge(const AttnParams &p, cudaStream_t st);  // combines nsplit (m, l, acc) partials
 bool tc_supported(const AttnParams &p);
 bool encode_map_bf16(CUtensorMap *out, const void *ptr, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box);   // 128-byte swizzle, not cached
+// rows of 64 bytes, or of a multiple of 128, without gaps: boxes {128 bytes, box_rows, 128-byte pieces of a row} in 128-byte (64-byte) swizzle, not cached
+bool encode_map_rows(CUtensorMap *out, const void *ptr, int row_bytes, int rows, int box_rows);
 bool tensor_map_2d_bf16(CUtensorMap *out, const void *ptr, int inner, int rows, int box_rows);
 bool tensor_map_kv_bf16(CUtensorMap *out, const void *ptr, int rows, int Hkv, int d, int box_rows);   // [rows][Hkv][d], box = box_rows x 1 head x 64
 bool tensor_map_q_bf16(CUtensorMap *out, const void *ptr, int B, int T, int Hq, int d, int heads, int tokens);   // [B][T][Hq][d], box = tokens x heads x 64

@@ -103,6 +103,16 @@ __device__ __forceinline__ void tma_load_4d_elect(uint32_t dst, const CUtensorMa
         ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
         : "memory");
 }
+// untiled copy of `bytes` (a multiple of 16, as both addresses are)
+__device__ __forceinline__ void bulk_load_elect(uint32_t dst, const void *src, uint32_t bar, uint32_t bytes)
+{
+    asm volatile(
+        "{\n\t.reg .pred q;\n\t"
+        "elect.sync _|q, 0xffffffff;\n\t"
+        "@q cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}"
+        ::"r"(dst), "l"(src), "r"(bytes), "r"(bar)
+        : "memory");
+}
 __device__ __forceinline__ void mbar_expect_tx_elect(uint32_t bar, uint32_t bytes)
 {
     asm volatile(
