@@ -51,7 +51,6 @@ template <int FMT, int HD, int NT> struct Tok {
     static constexpr int VCOLS = VB < 16 ? 8 : BYTES ? 16 : 8;     // consecutive columns of a thread
     static constexpr int VPIECES = HD / 8 / VCOLS;
     static constexpr int ROWS = 8 * NT;
-    static constexpr int OSTRIDE = HD + 4;                         // floats of a row of O in shared memory
     // a warp's blocks of keys: 16 rows of K, 16 of V, in boxes of 128 bytes (or 64) as TMA swizzles them; the exponents lie behind all stages
     static constexpr int BOX = ROW < 128 ? ROW : 128, BOXES = ROW / BOX;
     static constexpr uint32_t K_BYTES = 16 * ROW, STAGE = 2 * K_BYTES;
@@ -60,7 +59,9 @@ template <int FMT, int HD, int NT> struct Tok {
     // CTA does per unit (its place, Q, joining its warps, a partial) is then shared by all keys that the SM takes of it.
     static constexpr int WARPS = HD * NT <= 64 ? 16 : BYTES ? (HD * NT > 256 ? 8 : 12) : HD == 256 ? 6 : HD * NT > 128 ? 8 : 12;
     static constexpr int BLOCK = 16 * WARPS;                       // keys of a block: what the line of work is counted in
-    static constexpr uint32_t O_BYTES = ROWS * OSTRIDE * 4;        // a warp's share of O takes the place of its keys in the end
+    // a warp's share of O takes the place of its keys in the end: of the last ones, while the first ones of the next unit come, if it is no larger
+    static constexpr uint32_t O_BYTES = ROWS * HD * 4;
+    static constexpr bool EARLY = O_BYTES <= STAGE;
     static constexpr uint32_t WARP = ((STAGES * STAGE > O_BYTES ? STAGES * STAGE : O_BYTES) + 1023u) & ~1023u;
     static constexpr uint32_t OFF_Q = WARPS * WARP;            // [step][NT][lane] of two registers
     static constexpr uint32_t OFF_ML = OFF_Q + STEPS * NT * 256;   // [warps][ROWS] of (maximum, sum)
@@ -110,7 +111,7 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     // costs here.
     using Line = PageLine<TokSpanOf<ROWS, BLOCK>>;
     Line line{p, {p, G}};
-    struct Shared { typename Line::Place u; int total, nc; };
+    struct Shared { typename Line::Place u; int total, nc; };      // (u: the first unit, and later the next)
     static_assert(sizeof(Shared) <= 128, "place in shared memory");
     Shared *sh = reinterpret_cast<Shared *>(smem + C::OFF_PLACE);
     const int cta = blockIdx.x;
@@ -156,38 +157,75 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     auto value_at = [&](int e, int j) -> uint32_t {    // piece j of key 2 t + (e & 1) + 8 (e >> 1)
         return C::ROW < 128 ? v_piece + (e & 1) * 64 + (e >> 1) * 512 : (v_piece ^ ((e & 1) << 4)) + (e & 1) * 128 + (e >> 1) * 1024 + j * 2048;
     };
-    for (int x = x0; x < x1;) {
-        const typename Line::Place u = sh->u;
-        const PageSeq s = u.s;
-        const TokSpan span = u.sp;
-        const int t_first = p.token_of(u.tile * ROWS, G), m_first = u.tile * ROWS - t_first * G, rows_here = min(ROWS, s.n * G - u.tile * ROWS);
-        auto token_of = [&](int r) -> int { return G == 1 ? r : (int)__umulhi((uint32_t)(m_first + r), p.g_magic); };        // of the tile's row r, from t_first on
-        const int rt = u.tile, h = u.h, b = s.b;
-        const int k0 = x - u.at, k1 = min(u.cost, x1 - u.at);
-        const int kend = min(k1, span.count);
-        // ---- the pages of 32 of this warp's blocks are looked up together, the first ones ahead of everything else ----
-        const int key0 = span.lo + warp * 16;        // keys of block i: key0 + 64 i ..
-        int ids_from = k0, page_ids = k0 + lane < kend ? page_at(p.q, g.n_pages, b, (key0 + (k0 + lane) * BLOCK) >> g.log_p) : -1;
-        auto page_of_block = [&](int i) -> int {
-            if (i - ids_from >= 32) {
-                ids_from = i;
-                const int mine = i + lane;
-                page_ids = mine < kend ? page_at(p.q, g.n_pages, b, (key0 + mine * BLOCK) >> g.log_p) : -1;
-            }
-            return __shfl_sync(0xffffffffu, page_ids, i - ids_from);
-        };
-        // ---- Q of the unit's rows, in the order of K's pieces ----
+    // ---- the unit at hand ----
+    typename Line::Place u;
+    int t_first, m_first, rows_here, k0, k1, kend, key0, ids_from, page_ids;
+    uint32_t bad_pages;                                // of the blocks on their way, the first in bit 0
+    auto token_of = [&](int r) -> int { return G == 1 ? r : (int)__umulhi((uint32_t)(m_first + r), p.g_magic); };        // of the tile's row r, from t_first on
+    // (the pages of 32 of this warp's blocks are looked up together)
+    auto look_up = [&](int i) {
+        ids_from = i;
+        page_ids = i + lane < kend ? page_at(p.q, g.n_pages, u.s.b, (key0 + (i + lane) * BLOCK) >> g.log_p) : -1;
+    };
+    auto enter = [&](int x) {
+        u = sh->u;
+        t_first = p.token_of(u.tile * ROWS, G);
+        m_first = u.tile * ROWS - t_first * G;
+        rows_here = min(ROWS, u.s.n * G - u.tile * ROWS);
+        k0 = x - u.at;
+        k1 = min(u.cost, x1 - u.at);
+        kend = min(k1, u.sp.count);
+        key0 = u.sp.lo + warp * 16;                    // keys of block i: key0 + BLOCK i ..
+        bad_pages = 0;
+        look_up(k0);
+    };
+    auto fetch = [&](int i) {
+        if (i >= kend || dead) return;
+        if (i - ids_from >= 32) look_up(i);
+        const int key = key0 + i * BLOCK, page = __shfl_sync(0xffffffffu, page_ids, i - ids_from);
+        if (page < 0) bad_pages |= 1u << (i - k0 & 31);
+        else bad_pages &= ~(1u << (i - k0 & 31));
+        const size_t row = page_row(g, max(page, 0), u.h) + (size_t)(key & (g.P - 1));
+        const uint32_t dst = keys_at + put * C::STAGE, bar = bars + put * 8;
+        mbar_expect_tx_elect(bar, C::STAGE + (C::BYTES ? 32 : 0));
+        tma_load_3d_elect(dst, &tm_k, bar, 0, (int)row, 0);
+        if constexpr (C::BYTES) {
+            bulk_load_elect(exps_at + put * 32, g.ke + row, bar, 16);
+            bulk_load_elect(exps_at + put * 32 + 16, g.ve + row, bar, 16);
+        }
+        tma_load_3d_elect(dst + C::K_BYTES, &tm_v, bar, 0, (int)row, 0);
+        put = put + 1 == C::STAGES ? 0 : put + 1;
+        ++pending;
+    };
+    auto fetch_first = [&] {
+#pragma unroll
+        for (int i = 0; i < C::STAGES - 1; ++i) fetch(k0 + i);
+    };
+    auto stage_q = [&] {                               // Q of the unit's rows, in the order of K's pieces
         for (int i = threadIdx.x; i < C::STEPS * NT * 32; i += 32 * WARPS) {
             const int ln = i & 31, nt = (i >> 5) % NT, step = (i >> 5) / NT;
             const int r = nt * 8 + (ln >> 2), t = token_of(r);
             const int j = C::BYTES ? step >> 2 : step >> 1;
             const int d0 = (C::ROW < 128 ? 16 * (ln & 3) : (j >> 1) * (C::BYTES ? 128 : 64) + (2 * (ln & 3) + (j & 1)) * C::KEPP) + 4 * (C::BYTES ? step & 3 : step & 1);
             uint2 v = make_uint2(0u, 0u);
-            if (r < rows_here) v = *reinterpret_cast<const uint2 *>((const __nv_bfloat16 *)p.qry + ((size_t)(s.row0 + t_first + t) * g.Hq + h * G + m_first + r - t * G) * HD + d0);
+            if (r < rows_here) v = *reinterpret_cast<const uint2 *>((const __nv_bfloat16 *)p.qry + ((size_t)(u.s.row0 + t_first + t) * g.Hq + u.h * G + m_first + r - t * G) * HD + d0);
             q_s[i] = v;
         }
-        __syncthreads();
+    };
+    enter(x0);
+    fetch_first();
+    stage_q();
+    __syncthreads();
 
+    for (;;) {
+        const PageSeq s = u.s;
+        const TokSpan span = u.sp;
+        const int x = u.at + k1;                       // the next unit begins there
+        if (x < x1 && warp == WARPS - 1 && lane == 0) {
+            typename Line::Place next = u;
+            line.next(next);
+            sh->u = next;
+        }
         // ---- this thread's query rows: 2t, 2t + 1 of every group of 8 ----
         int lo_r[2 * NT], hi_r[2 * NT], lo_min, lo_max, hi_min, hi_max;      // (the limits of all the tile's rows)
 #pragma unroll
@@ -214,24 +252,6 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         for (int i = 0; i < 2 * NT; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
         bool bad = false;
 
-        uint32_t bad_pages = 0;                       // of the blocks on their way, the first in bit 0
-        auto fetch = [&](int i) {
-            if (i >= kend || dead) return;
-            const int key = key0 + i * BLOCK, page = page_of_block(i);
-            if (page < 0) bad_pages |= 1u << (i - k0 & 31);
-            else bad_pages &= ~(1u << (i - k0 & 31));
-            const size_t row = page_row(g, max(page, 0), h) + (size_t)(key & (g.P - 1));
-            const uint32_t dst = keys_at + put * C::STAGE, bar = bars + put * 8;
-            mbar_expect_tx_elect(bar, C::STAGE + (C::BYTES ? 32 : 0));
-            tma_load_3d_elect(dst, &tm_k, bar, 0, (int)row, 0);
-            if constexpr (C::BYTES) {
-                bulk_load_elect(exps_at + put * 32, g.ke + row, bar, 16);
-                bulk_load_elect(exps_at + put * 32 + 16, g.ve + row, bar, 16);
-            }
-            tma_load_3d_elect(dst + C::K_BYTES, &tm_v, bar, 0, (int)row, 0);
-            put = put + 1 == C::STAGES ? 0 : put + 1;
-            ++pending;
-        };
         // O^T += V^T P^T of the loaded block; keep: which of this thread's four keys are live (the others count as zeros)
         auto value_word = [&](const uint8_t *stage, int e, int i) -> uint32_t {       // word i of this thread's part of the e-th of its keys
             return reinterpret_cast<const uint32_t *>(stage + value_at(e, i / (C::VPB / 4)))[i % (C::VPB / 4)];
@@ -279,8 +299,6 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             }
         };
 
-#pragma unroll
-        for (int i = 0; i < C::STAGES - 1; ++i) fetch(k0 + i);
 #pragma unroll 1
         for (int i = k0; i < kend; ++i) {
             const int key = key0 + i * BLOCK;
@@ -431,8 +449,9 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         }
         __syncwarp();                                 // (the stages may be written over)
         // ---- the warps' shares meet ----
+        const uint32_t o_at = C::EARLY ? (put == 0 ? C::STAGES - 1 : put - 1) * C::STAGE : 0;      // (the same for all warps)
         const bool any_bad = __any_sync(0xffffffffu, bad);
-        if (any_bad && lane == 0) report_bad_page(g.status, b);
+        if (any_bad && lane == 0) report_bad_page(g.status, s.b);
 #pragma unroll
         for (int r = 0; r < 2 * NT; ++r) {
 #pragma unroll
@@ -449,24 +468,35 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 #pragma unroll
             for (int q = 0; q < WARPS; ++q) all = fmaxf(all, ml_s[q * ROWS + rr].x);
             f[r] = m[r] == -INFINITY ? 0.f : ex2(m[r] - all);
-            // column c of piece j: 8 VCOLS j + VCOLS g + c; register (tile, 0 / 2) holds an even / odd column of an even row's pair
-            float *dst = reinterpret_cast<float *>(keys) + rr * C::OSTRIDE + gq * C::VCOLS;
+            // column c of piece j: 8 VCOLS j + VCOLS g + c; register (tile, 0 / 2) holds an even / odd column of an even row's pair. Four columns lie
+            // where 16-byte pieces of a row are swapped by its bits 1 and 2: neither these writes nor the reads below meet in a bank more often than they must.
+            float *dst = reinterpret_cast<float *>(keys + o_at) + rr * HD;
 #pragma unroll
             for (int j = 0; j < C::VPIECES; ++j)
 #pragma unroll
                 for (int x2 = 0; x2 < C::VCOLS; x2 += 4) {
-                    const int tile = (j * C::VCOLS + x2) / 2;
-                    *reinterpret_cast<float4 *>(dst + j * 8 * C::VCOLS + x2) = make_float4(o[tile][r >> 1][r & 1] * f[r], o[tile][r >> 1][2 + (r & 1)] * f[r],
-                                                                                         o[tile + 1][r >> 1][r & 1] * f[r], o[tile + 1][r >> 1][2 + (r & 1)] * f[r]);
+                    const int tile = (j * C::VCOLS + x2) / 2, piece = (j * 8 + gq) * (C::VCOLS / 4) + x2 / 4;
+                    *reinterpret_cast<float4 *>(dst + 4 * (piece ^ t4)) = make_float4(o[tile][r >> 1][r & 1] * f[r], o[tile][r >> 1][2 + (r & 1)] * f[r],
+                                                                                      o[tile + 1][r >> 1][r & 1] * f[r], o[tile + 1][r >> 1][2 + (r & 1)] * f[r]);
                 }
         }
-        __syncthreads();
+        // ---- the next unit is on its way while this one's results are written ----
         const bool starts = k0 == 0, ends = k1 == u.cost;
-        const int slot = 2 * cta + (starts ? 1 : 0);
+        const int slot = 2 * cta + (starts ? 1 : 0), h = u.h, rows_done = rows_here, t_done = t_first, m_done = m_first, first_row = u.tile * ROWS;
+        if (starts && !ends && threadIdx.x == 0) {
+            PageSplit m2 = {s.b, s.row0, first_row, rows_done, h, shares.owner(u.at + u.cost - 1), ROWS, 0};
+            part.meta[cta] = m2;
+        }
+        if (x < x1) {
+            enter(x);
+            if (C::EARLY) fetch_first();
+            stage_q();
+        }
+        __syncthreads();
         for (int i = threadIdx.x; i < ROWS * (HD / 8); i += 32 * WARPS) {
             const int r = i / (HD / 8), c0 = i % (HD / 8) * 8;
-            if (r >= rows_here) continue;
-            const int t = token_of(r);
+            if (r >= rows_done) continue;
+            const int t = G == 1 ? r : (int)__umulhi((uint32_t)(m_done + r), p.g_magic);
             float all = -INFINITY, sum = 0.f, acc[8];
 #pragma unroll
             for (int q = 0; q < WARPS; ++q) all = fmaxf(all, ml_s[q * ROWS + r].x);
@@ -477,8 +507,8 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 const float2 v = ml_s[q * ROWS + r];
                 // (a maximum of -inf carries no weight, a sum that is NaN is kept)
                 sum += v.x == -INFINITY ? v.y * 0.f : v.y * ex2(v.x - all);
-                const float4 *src = reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(smem + q * C::WARP) + r * C::OSTRIDE + c0);
-                const float4 y0 = src[0], y1 = src[1];
+                const float *src = reinterpret_cast<const float *>(smem + q * C::WARP + o_at) + r * HD;
+                const float4 y0 = *reinterpret_cast<const float4 *>(src + 4 * ((c0 >> 2) ^ ((r >> 1) & 3))), y1 = *reinterpret_cast<const float4 *>(src + 4 * ((c0 >> 2) + 1 ^ ((r >> 1) & 3)));
                 acc[0] += y0.x; acc[1] += y0.y; acc[2] += y0.z; acc[3] += y0.w;
                 acc[4] += y1.x; acc[5] += y1.y; acc[6] += y1.z; acc[7] += y1.w;
             }
@@ -486,27 +516,16 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[e] *= inv;
-                store8((__nv_bfloat16 *)p.out + ((size_t)(s.row0 + t_first + t) * g.Hq + h * G + m_first + r - t * G) * HD + c0, acc);
+                store8((__nv_bfloat16 *)p.out + ((size_t)(s.row0 + t_done + t) * g.Hq + h * G + m_done + r - t * G) * HD + c0, acc);
             } else {
                 store8(partial8(part, slot, HD, r, c0), acc);
                 if (c0 == 0) part.ml[(size_t)slot * part.rows + r] = make_float2(all, sum);
             }
         }
-        if (starts && !ends && threadIdx.x == 0) {
-            PageSplit m2 = {b, s.row0, rt * ROWS, min(ROWS, s.n * G - rt * ROWS), h, shares.owner(u.at + u.cost - 1), ROWS, 0};
-            part.meta[cta] = m2;
-        }
-        x = u.at + k1;
-        fence_proxy_async_smem();    // (the next blocks come over what the warps put down)
-        __syncthreads();             // (this unit's results and Q have been read)
-        if (ends && x < x1) {
-            if (threadIdx.x == 0) {
-                typename Line::Place next = u;
-                line.next(next);
-                sh->u = next;
-            }
-            __syncthreads();
-        }
+        if (x >= x1) return;
+        fence_proxy_async_smem();    // (blocks come over what the warps put down)
+        __syncthreads();             // (this unit's results have been read, the next one's Q is there)
+        if (!C::EARLY) fetch_first();
     }
 }
 
