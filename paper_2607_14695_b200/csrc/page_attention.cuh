@@ -53,7 +53,7 @@ struct PageShares {
 template <typename SPAN>
 struct PageLine {
     const PageAttention &p;
-    const SPAN span;
+    SPAN span;
     int width, longest;              // lanes of a sequence; the longest unit
     PageSeq mine;                    // sequence lane / width
     int mine_cost;                   // its blocks, in the first of its lanes (0 in the others)
@@ -83,6 +83,11 @@ struct PageLine {
         width = 32;
         while (width > 1 && p.q.B * width > 32) width >>= 1;
         mine = seq_of(lane / width);
+        return count(lane);
+    }
+    // (again, when `span` counts otherwise)
+    __device__ __forceinline__ int count(int lane)
+    {
         longest = 1;
         mine_cost = seq_cost(mine, lane, longest);
         int sum = mine_cost;
@@ -183,18 +188,18 @@ struct PagePartials {
     // tile see and others do not was not finite, and 0 times it is NaN on the tensor cores; and the blocks of that kernel that are done with them.
     uint8_t *careful;
     uint32_t *careful_done;
+    uint32_t *arrived;     // [CTAs]: how many CTAs have left their partial of the unit that this one began (page_token_kernel; zero between launches)
     int rows;              // rows of a slot
     float scale_log2;
 };
 __device__ __forceinline__ float *partial8(const PagePartials &part, size_t slot, int d, int r, int c0) { return part.o + ((slot * (size_t)(d >> 3) + (size_t)(c0 >> 3)) * part.rows + r) * 8; }
-constexpr int kMostCtas = 512;              // of a launch that leaves partial results
+constexpr int kTokenCtas = 160, kMostPairs = 128;      // of page_token_kernel's CTAs, of page_chunk_kernel's pairs
 int page_token_rows(int dtype, int format, int d, int G, int rows);
-// ctas: how many were launched
-cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int sm_count, int &ctas, cudaStream_t st);
+cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int sm_count, cudaStream_t st);
 bool page_chunk_takes(int dtype, int G, int d);
 cudaError_t launch_page_widen(const PageAttention &a, void *k_wide, void *v_wide, int format, int sm_count, cudaStream_t st);
 // k, v: one layer's pages in bf16
 cudaError_t launch_page_chunk(const PageAttention &a, const PagePartials &part, const void *k, const void *v, int pairs, cudaStream_t st);
-cudaError_t launch_page_merge(const PageAttention &a, const PagePartials &part, int ctas, int format, int sm_count, cudaStream_t st);
+cudaError_t launch_page_merge(const PageAttention &a, const PagePartials &part, int pairs, int format, int sm_count, cudaStream_t st);
 
 }  // namespace reflex

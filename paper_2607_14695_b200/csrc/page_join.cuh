@@ -1,0 +1,50 @@
+// Joining the partial results of a unit: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i, in the order of the keys.
+#pragma once
+
+#include "page_attention.cuh"
+#include "sm100_ptx.cuh"
+
+namespace reflex {
+
+struct PageSum { float m, l, o[8]; };
+
+// partials first, first + step .. of the n of a unit that CTA (or pair) `cta` began, of 8 columns of a row
+__device__ __forceinline__ void page_sum(const PagePartials &part, int d, int cta, int n, int r, int c0, int first, int step, PageSum &a)
+{
+    auto slot = [&](int i) -> size_t { return i == 0 ? 2 * (size_t)cta + 1 : 2 * (size_t)(cta + i); };
+    a.m = -INFINITY; a.l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a.o[e] = 0.f;
+    for (int i0 = first; i0 < n; i0 += 4 * step) {
+        float4 v[4][2];
+        float2 ml[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + j * step;
+            if (i < n) {
+                ml[j] = __ldcg(part.ml + slot(i) * part.rows + r);
+                const float4 *src = reinterpret_cast<const float4 *>(partial8(part, slot(i), d, r, c0));
+                v[j][0] = __ldcg(src); v[j][1] = __ldcg(src + 1);
+            } else ml[j] = make_float2(-INFINITY, 0.f);
+        }
+        float top = a.m;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, ml[j].x);
+        const float old = a.m == -INFINITY ? 0.f : ptx::ex2(a.m - top);
+        a.l *= a.m == -INFINITY ? 1.f : old;             // (0, or the NaN of a part that went wrong)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) a.o[e] *= old;
+        a.m = top;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float w = ml[j].x == -INFINITY ? 0.f : ptx::ex2(ml[j].x - top);
+            a.l += ml[j].y * w;
+            if (w == 0.f) continue;                     // (what a part that has seen nothing left there is not looked at)
+            const float f[8] = {v[j][0].x, v[j][0].y, v[j][0].z, v[j][0].w, v[j][1].x, v[j][1].y, v[j][1].z, v[j][1].w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a.o[e] = fmaf(f[e], w, a.o[e]);
+        }
+    }
+}
+
+}  // namespace reflex

@@ -3,58 +3,27 @@
 // the loads of 4 partials in flight; long lists (one sequence over the whole device) are cut in 8 among the warps of a block, which then add up.
 //
 // It also computes again, row by row, the sequences that the tensor-core kernel has marked (see PagePartials::careful).
+#include "page_join.cuh"
 #include "page_plain.cuh"
-#include "sm100_ptx.cuh"
 
 namespace reflex {
 
 constexpr int kMergeThreads = 256;
-constexpr int kMergeMost = kMostCtas;
+constexpr int kMergeMost = kMostPairs;
 constexpr int kMergeLong = 16;            // partials of a unit from which on its list is cut
 
-struct MergeSum { float m, l, o[8]; };
-
-__device__ __forceinline__ void merge_list(const PagePartials &part, int d, int cta, int n, int r, int c0, int first, int step, MergeSum &a)
+__device__ __forceinline__ void page_add(PageSum &a, const PageSum &b)
 {
-    auto slot = [&](int i) -> size_t { return i == 0 ? 2 * (size_t)cta + 1 : 2 * (size_t)(cta + i); };
-    a.m = -INFINITY; a.l = 0.f;
+    const float top = fmaxf(a.m, b.m), fa = a.m == -INFINITY ? 0.f : ptx::ex2(a.m - top), fb = b.m == -INFINITY ? 0.f : ptx::ex2(b.m - top);
+    a.l = (a.m == -INFINITY ? a.l : a.l * fa) + (b.m == -INFINITY ? b.l : b.l * fb);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) a.o[e] = 0.f;
-    for (int i0 = first; i0 < n; i0 += 4 * step) {
-        float4 v[4][2];
-        float2 ml[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = i0 + j * step;
-            if (i < n) {
-                ml[j] = part.ml[slot(i) * part.rows + r];
-                const float4 *src = reinterpret_cast<const float4 *>(partial8(part, slot(i), d, r, c0));
-                v[j][0] = src[0]; v[j][1] = src[1];
-            } else ml[j] = make_float2(-INFINITY, 0.f);
-        }
-        float top = a.m;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) top = fmaxf(top, ml[j].x);
-        const float old = a.m == -INFINITY ? 0.f : ptx::ex2(a.m - top);
-        a.l *= a.m == -INFINITY ? 1.f : old;             // (0, or the NaN of a part that went wrong)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) a.o[e] *= old;
-        a.m = top;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float w = ml[j].x == -INFINITY ? 0.f : ptx::ex2(ml[j].x - top);
-            a.l += ml[j].y * w;
-            if (w == 0.f) continue;                     // (what a part that has seen nothing left there is not looked at)
-            const float f[8] = {v[j][0].x, v[j][0].y, v[j][0].z, v[j][0].w, v[j][1].x, v[j][1].y, v[j][1].z, v[j][1].w};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) a.o[e] = fmaf(f[e], w, a.o[e]);
-        }
-    }
+    for (int e = 0; e < 8; ++e) a.o[e] = a.o[e] * fa + b.o[e] * fb;
+    a.m = top;
 }
 
 template <int FMT>
 __global__ void __launch_bounds__(kMergeThreads, 4)
-page_merge_kernel(const PageAttention p, const PagePartials part, int ctas)
+page_merge_kernel(const PageAttention p, const PagePartials part, int pairs)
 {
     __shared__ int first_s[kMergeMost + 1];        // first piece of work of each unit that was split (by the CTA that began it)
     __shared__ __align__(16) uint8_t scratch[kMergeThreads * 44];
@@ -65,28 +34,17 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int ctas)
     // (sequences are marked before this kernel, and the marks go when its last block is done: all blocks see the same)
     bool marked = false;
     for (int b = tid; b < p.q.B; b += kMergeThreads) marked |= part.careful[b] != 0;
-    int pieces[2], of[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int c = 2 * tid + k;
-        pieces[k] = 0;
-        of[k] = -1;
-        if (c < ctas) {
-            const PageSplit m = part.meta[c];
-            of[k] = m.b;
-            const int per = m.last - c + 1 > kMergeLong ? 32 : 256;
-            if (m.b >= 0) pieces[k] = (m.rows * groups + per - 1) / per;
-        }
+    int pieces = 0, of = -1;
+    if (tid < pairs) {
+        const PageSplit s = part.meta[tid];
+        of = s.b;
+        const int per = s.last - tid + 1 > kMergeLong ? 32 : 256;
+        if (s.b >= 0) pieces = (s.rows * groups + per - 1) / per;
     }
     const bool any_marked = __syncthreads_or(marked);
-    if (any_marked) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-            if (of[k] >= 0 && part.careful[of[k]]) pieces[k] = 0;
-    }
+    if (any_marked && of >= 0 && part.careful[of]) pieces = 0;
     {
-        const int mine = pieces[0] + pieces[1];
-        int incl = mine;
+        int incl = pieces;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, incl, o);
@@ -95,21 +53,14 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int ctas)
         int *sum_s = reinterpret_cast<int *>(scratch);
         if (lane == 31) sum_s[warp] = incl;
         __syncthreads();
-        int before = 0, all = 0;
-#pragma unroll
-        for (int q = 0; q < kMergeThreads / 32; ++q) {
-            if (q < warp) before += sum_s[q];
-            all += sum_s[q];
-        }
-        static_assert(kMergeMost == 2 * kMergeThreads, "two entries a thread");
-        first_s[2 * tid] = before + incl - mine;
-        first_s[2 * tid + 1] = before + incl - mine + pieces[0];
-        if (tid == 0) first_s[kMergeMost] = all;
-        if (ctas < kMergeMost && tid == 0) first_s[ctas] = all;
+        int before = 0;
+        for (int q = 0; q < warp; ++q) before += sum_s[q];
+        static_assert(kMergeMost < kMergeThreads, "an entry a thread, and the end");
+        if (tid <= pairs) first_s[tid] = before + incl - pieces;
         __syncthreads();
     }
-    for (int w = blockIdx.x; w < first_s[ctas]; w += gridDim.x) {
-        int lo = 0, hi = ctas;                      // first_s[lo] <= w < first_s[hi]
+    for (int w = blockIdx.x; w < first_s[pairs]; w += gridDim.x) {
+        int lo = 0, hi = pairs;                      // first_s[lo] <= w < first_s[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (first_s[mid] <= w) lo = mid; else hi = mid;
@@ -120,22 +71,15 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int ctas)
         const int item = (w - first_s[lo]) * (cut ? 32 : 256) + (cut ? lane : tid);
         const int r = item % m.rows, c0 = item / m.rows * 8, at = r < m.half ? r : 128 + r - m.half;
         const bool live = c0 < d;
-        MergeSum a;
-        if (live) merge_list(part, d, lo, n, at, c0, cut ? warp : 0, cut ? 8 : 1, a);
+        PageSum a;
+        if (live) page_sum(part, d, lo, n, at, c0, cut ? warp : 0, cut ? 8 : 1, a);
         if (cut) {
-            MergeSum *all = reinterpret_cast<MergeSum *>(scratch);
+            PageSum *all = reinterpret_cast<PageSum *>(scratch);
             __syncthreads();
             if (live) all[tid] = a;
             __syncthreads();
             if (warp > 0 || !live) continue;
-            for (int q = 1; q < 8; ++q) {
-                const MergeSum b = all[q * 32 + lane];
-                const float top = fmaxf(a.m, b.m), fa = a.m == -INFINITY ? 0.f : ptx::ex2(a.m - top), fb = b.m == -INFINITY ? 0.f : ptx::ex2(b.m - top);
-                a.l = (a.m == -INFINITY ? a.l : a.l * fa) + (b.m == -INFINITY ? b.l : b.l * fb);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) a.o[e] = a.o[e] * fa + b.o[e] * fb;
-                a.m = top;
-            }
+            for (int q = 1; q < 8; ++q) page_add(a, all[q * 32 + lane]);
         }
         if (!live) continue;
         const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
@@ -167,7 +111,7 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int ctas)
     }
 }
 
-cudaError_t launch_page_merge(const PageAttention &a, const PagePartials &part, int ctas, int format, int sm_count, cudaStream_t st)
+cudaError_t launch_page_merge(const PageAttention &a, const PagePartials &part, int pairs, int format, int sm_count, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(4 * sm_count));
@@ -179,9 +123,9 @@ cudaError_t launch_page_merge(const PageAttention &a, const PagePartials &part, 
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     count_launch();
-    if (format == REFLEX_PAGE_SAME) return cudaLaunchKernelEx(&cfg, page_merge_kernel<REFLEX_PAGE_SAME>, a, part, ctas);
-    if (format == REFLEX_PAGE_E4M3) return cudaLaunchKernelEx(&cfg, page_merge_kernel<REFLEX_PAGE_E4M3>, a, part, ctas);
-    return cudaLaunchKernelEx(&cfg, page_merge_kernel<REFLEX_PAGE_INT8>, a, part, ctas);
+    if (format == REFLEX_PAGE_SAME) return cudaLaunchKernelEx(&cfg, page_merge_kernel<REFLEX_PAGE_SAME>, a, part, pairs);
+    if (format == REFLEX_PAGE_E4M3) return cudaLaunchKernelEx(&cfg, page_merge_kernel<REFLEX_PAGE_E4M3>, a, part, pairs);
+    return cudaLaunchKernelEx(&cfg, page_merge_kernel<REFLEX_PAGE_INT8>, a, part, pairs);
 }
 
 }  // namespace reflex

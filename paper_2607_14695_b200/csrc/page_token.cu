@@ -10,16 +10,15 @@
 // 8-bit rows stay unscaled in the products (they are exact in bf16): 2^e of a key scales its logits, 2^e of a value the key's weight, in fp32.
 // A warp walks every WARPS-th block of 16 keys with a running maximum, fetches for itself, and has one or two blocks on their way while it works on one:
 // 100 KB or more per SM. (64 streams of 3300 keys in 8 bits, 112 MB: 46.7 us with one block at a time in registers, 49.5 with rows by cp.async, whose
-// 17 instructions a block kept the load pipe busy, 39.4 by TMA.)
+// 17 instructions a block kept the load pipe busy, 33.6 by TMA and with all that follows.)
 //
 // The keys of all (sequence, row tile, KV head) units form one line that the CTAs share evenly, whatever the lengths; a unit that more than one
-// CTA works on leaves fp32 partials, which page_merge_kernel joins in the order of the keys (results do not depend on timing).
+// CTA works on leaves fp32 partials, which the last of them to finish joins in the order of the keys (results do not depend on timing).
 #include <math.h>
 
 #include <algorithm>
 
-#include "page_attention.cuh"
-#include "sm100_ptx.cuh"
+#include "page_join.cuh"
 
 namespace reflex {
 
@@ -37,6 +36,14 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a)
     return d;
 }
 constexpr unsigned long long kTokenWaitNs = 1000000000ull;
+
+// Adds 1 and returns what was there. What the block has written before its last barrier is seen by whoever sees the sum, and the other way round
+__device__ __forceinline__ uint32_t arrive_gpu(uint32_t *at)
+{
+    uint32_t old;
+    asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(old) : "l"(at) : "memory");
+    return old;
+}
 
 template <int FMT, int HD, int NT> struct Tok {
     static constexpr bool BYTES = FMT != REFLEX_PAGE_SAME;
@@ -72,12 +79,12 @@ template <int FMT, int HD, int NT> struct Tok {
     static_assert(SMEM <= 232448, "shared memory");
 };
 
-// the blocks of keys that a tile of ROWS rows needs
-struct TokSpan { int lo, hi, count; };
+// the blocks of keys that a tile of ROWS rows needs, and the pieces of `per` blocks that they make
+struct TokSpan { int lo, hi, blocks, count; };
 template <int ROWS, int BLOCK>
 struct TokSpanOf {
     const PageAttention &p;
-    int G;
+    int G, per;
     __device__ __forceinline__ int tiles(const PageSeq &s) const { return (s.n * G + ROWS - 1) / ROWS; }
     __device__ __forceinline__ TokSpan operator()(const PageSeq &s, int tile) const
     {
@@ -85,7 +92,8 @@ struct TokSpanOf {
         TokSpan t;
         t.lo = r.lo & ~15;
         t.hi = r.hi;
-        t.count = t.hi > t.lo ? (t.hi - t.lo + BLOCK - 1) / BLOCK : 0;
+        t.blocks = t.hi > t.lo ? (t.hi - t.lo + BLOCK - 1) / BLOCK : 0;
+        t.count = per == 1 ? t.blocks : (t.blocks + per - 1) / per;
         return t;
     }
 };
@@ -105,13 +113,14 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     const int G = g.Hq / g.Hkv;
     uint8_t *keys = smem + warp * C::WARP;             // this warp's stages
     const uint32_t keys_at = smem_u32(keys), exps_at = smem_u32(smem + C::OFF_EXP) + warp * C::STAGES * 32, bars = smem_u32(smem + C::OFF_BAR) + warp * C::STAGES * 8;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-    // Warp 0 walks the line for all. No more CTAs than leave each the square root of a fifth of the longest unit: a partial costs the merge a fifth of what a block
-    // costs here.
+    // Warp 0 walks the line for all. Where there are fewer blocks than keep all CTAs busy, the line is counted in pieces of several blocks, a CTA takes one, and
+    // none has parts of two units: the square root of a fifth of the longest unit, since joining a partial costs about a fifth of a block.
+    // (8 streams of 3300 keys, bf16: 27.0 us in blocks, 35 a stream and two a CTA, 18.6 in pieces of two.)
     using Line = PageLine<TokSpanOf<ROWS, BLOCK>>;
-    Line line{p, {p, G}};
-    struct Shared { typename Line::Place u; int total, nc; };      // (u: the first unit, and later the next)
+    Line line{p, {p, G, 1}};
+    struct Join { int parts, from, row, head, m, rows; };           // a split unit that this CTA has to join (parts: 0 if it has not)
+    struct Shared { typename Line::Place u; int total, nc, per; Join join[2]; };      // (u: the first unit, and later the next)
     static_assert(sizeof(Shared) <= 128, "place in shared memory");
     Shared *sh = reinterpret_cast<Shared *>(smem + C::OFF_PLACE);
     const int cta = blockIdx.x;
@@ -119,22 +128,25 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     fence_mbar_init();
     if (warp == 1 && lane < 2) prefetch_tmap(lane ? &tm_v : &tm_k);
     if (warp == 0) {
-        const int total = line.begin(lane);
-        const int least = max(1, (int)sqrtf((float)line.longest * 0.2f)), nc = min((int)gridDim.x, (total + least - 1) / least);
+        int total = line.begin(lane);
+        const int per = (int)sqrtf((float)line.longest * 0.2f);
+        if (per > 1 && total <= per * (int)gridDim.x) {
+            line.span.per = per;
+            total = line.count(lane);
+        }
+        const int nc = min((int)gridDim.x, total);
         if (cta < nc) {
             const typename Line::Place first = line.find(PageShares(total, nc).of(cta), lane);
             if (lane == 0) sh->u = first;
         }
-        if (lane == 0) {
-            sh->total = total; sh->nc = nc;
-            part.meta[cta].b = -1;
-        }
+        if (lane == 0) { sh->total = total; sh->nc = nc; sh->per = line.span.per; sh->join[0].parts = sh->join[1].parts = 0; }
     }
     __syncthreads();
     const int nc = sh->nc;
     if (cta >= nc) return;
     const PageShares shares(sh->total, nc);
-    const int x0 = shares.of(cta), x1 = shares.of(cta + 1);
+    const int x0 = shares.of(cta), x1 = shares.of(cta + 1), per = sh->per;
+    line.span.per = per;
 
     int put = 0, got = 0;                              // the stage that is filled next, that is read next
     uint32_t got_phase = 0;
@@ -159,7 +171,7 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     };
     // ---- the unit at hand ----
     typename Line::Place u;
-    int t_first, m_first, rows_here, k0, k1, kend, key0, ids_from, page_ids;
+    int t_first, m_first, rows_here, k0, kend, key0, ids_from, page_ids;
     uint32_t bad_pages;                                // of the blocks on their way, the first in bit 0
     auto token_of = [&](int r) -> int { return G == 1 ? r : (int)__umulhi((uint32_t)(m_first + r), p.g_magic); };        // of the tile's row r, from t_first on
     // (the pages of 32 of this warp's blocks are looked up together)
@@ -172,9 +184,8 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         t_first = p.token_of(u.tile * ROWS, G);
         m_first = u.tile * ROWS - t_first * G;
         rows_here = min(ROWS, u.s.n * G - u.tile * ROWS);
-        k0 = x - u.at;
-        k1 = min(u.cost, x1 - u.at);
-        kend = min(k1, u.sp.count);
+        k0 = (x - u.at) * per;
+        kend = min(min(u.cost, x1 - u.at) * per, u.sp.blocks);
         key0 = u.sp.lo + warp * 16;                    // keys of block i: key0 + BLOCK i ..
         bad_pages = 0;
         look_up(k0);
@@ -220,7 +231,7 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     for (;;) {
         const PageSeq s = u.s;
         const TokSpan span = u.sp;
-        const int x = u.at + k1;                       // the next unit begins there
+        const int x = min(u.at + u.cost, x1);          // the next unit begins there
         if (x < x1 && warp == WARPS - 1 && lane == 0) {
             typename Line::Place next = u;
             line.next(next);
@@ -252,11 +263,11 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         for (int i = 0; i < 2 * NT; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
         bool bad = false;
 
-        // O^T += V^T P^T of the loaded block; keep: which of this thread's four keys are live (the others count as zeros)
+        // O^T += V^T P^T of the loaded block
         auto value_word = [&](const uint8_t *stage, int e, int i) -> uint32_t {       // word i of this thread's part of the e-th of its keys
-            return reinterpret_cast<const uint32_t *>(stage + value_at(e, i / (C::VPB / 4)))[i % (C::VPB / 4)];
+            return *reinterpret_cast<const uint32_t *>(stage + value_at(e, i / (C::VPB / 4)) + i % (C::VPB / 4) * 4);
         };
-        auto times_v = [&](const uint8_t *stage, const uint32_t (&pt)[NT][2], uint32_t keep, bool finite) {
+        auto times_v = [&](const uint8_t *stage, const uint32_t (&pt)[NT][2]) {
             uint32_t v[4][C::VPB / 4];
 #pragma unroll
             for (int i = 0; i < C::VW; ++i) {
@@ -268,18 +279,7 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                         else *reinterpret_cast<uint2 *>(v[e]) = *reinterpret_cast<const uint2 *>(src);
                     }
                 }
-                uint32_t w[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    w[e] = v[e][i % (C::VPB / 4)];
-                    if constexpr (!C::BYTES) {
-                        if (keep != 15u && !((keep >> e) & 1u)) w[e] = 0u;
-                        if (!finite) {
-                            if ((w[e] & 0x7f80u) == 0x7f80u) w[e] &= 0xffff0000u;
-                            if ((w[e] & 0x7f800000u) == 0x7f800000u) w[e] &= 0x0000ffffu;
-                        }
-                    }
-                }
+                const uint32_t w[4] = {v[0][i % (C::VPB / 4)], v[1][i % (C::VPB / 4)], v[2][i % (C::VPB / 4)], v[3][i % (C::VPB / 4)]};
                 if constexpr (C::BYTES) {
                     // four columns of four keys: two tiles of 16 (column, column + 1) pairs. Pairs of keys are put side by side first.
                     const uint32_t lo01 = biased<FMT>(__byte_perm(w[0], w[1], 0x5140)), hi01 = biased<FMT>(__byte_perm(w[0], w[1], 0x7362));
@@ -403,30 +403,35 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 pt[nt][1] = transpose8x8(pack_bf16(v[2], v[3]));
             }
             // ---- values ----
-            if (whole || C::BYTES) times_v(stage, pt, 15u, true);
-            else {
-                // A masked key has weight 0, but 0 times what lies there may be NaN: keys that no row sees count as zeros. A key that some
-                // rows see is multiplied for all of them, which does no harm while it is finite.
-                uint32_t live = 0;
-                bool odd = false;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = key + 2 * t4 + (e & 1) + 8 * (e >> 1);
-                    if (j >= lo_min && j < hi_max && !lost) {
-                        live |= 1u << e;
-#pragma unroll
-                        for (int q = 0; q < C::VW; ++q) {
-                            const uint32_t word = value_word(stage, e, q);
-                            odd |= (word & 0x7f80u) == 0x7f80u || (word & 0x7f800000u) == 0x7f800000u;
-                        }
+            if (!C::BYTES && !whole) {
+                // A masked key has weight 0, but 0 times what lies there may be NaN: keys that no row sees become zeros. A key that some
+                // rows see is multiplied for all of them, which does no harm while it is finite. (In place and in short loops: as a second
+                // form of the products this was 1000 instructions, and 7 us of the one block at the end of a sequence, most of them to fetch the code.)
+                auto each_piece = [&](auto change) -> bool {          // change(key, uint32_t &pair of elements) -> bool
+                    bool any = false;
+#pragma unroll 1
+                    for (uint32_t at = lane * 16; at < C::K_BYTES; at += 512) {
+                        uint4 *piece = reinterpret_cast<uint4 *>(const_cast<uint8_t *>(stage) + C::K_BYTES + at);
+                        uint4 v = *piece;
+                        const int j = key + (int)((at / C::BOX) & 15);
+                        any |= change(j, v.x); any |= change(j, v.y); any |= change(j, v.z); any |= change(j, v.w);
+                        *piece = v;
                     }
-                }
-                const bool any_odd = __any_sync(0xffffffffu, odd);
+                    fence_proxy_async_smem();         // (TMA writes there next)
+                    __syncwarp();
+                    return __any_sync(0xffffffffu, any);
+                };
+                auto odd_low = [](uint32_t w) -> bool { return (w & 0x7f80u) == 0x7f80u; };
+                auto odd_high = [](uint32_t w) -> bool { return (w & 0x7f800000u) == 0x7f800000u; };
+                const bool any_odd = each_piece([&](int j, uint32_t &w) -> bool {
+                    if (j < lo_min || j >= hi_max || lost) w = 0u;
+                    return odd_low(w) || odd_high(w);
+                });
                 if (any_odd) {
                     // what is not finite goes, as it is, to the rows that see it (whatever their weight), and counts as zero in the products
 #pragma unroll 1
                     for (int from = 0; from < 4; ++from) {
-#pragma unroll
+#pragma unroll 1
                         for (int e = 0; e < 4; ++e) {
                             const int j = key + 2 * from + (e & 1) + 8 * (e >> 1);
 #pragma unroll
@@ -443,9 +448,14 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                             }
                         }
                     }
+                    each_piece([&](int, uint32_t &w) -> bool {
+                        if (odd_low(w)) w &= 0xffff0000u;
+                        if (odd_high(w)) w &= 0x0000ffffu;
+                        return false;
+                    });
                 }
-                times_v(stage, pt, live, !any_odd);
             }
+            times_v(stage, pt);
         }
         __syncwarp();                                 // (the stages may be written over)
         // ---- the warps' shares meet ----
@@ -481,12 +491,9 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 }
         }
         // ---- the next unit is on its way while this one's results are written ----
-        const bool starts = k0 == 0, ends = k1 == u.cost;
-        const int slot = 2 * cta + (starts ? 1 : 0), h = u.h, rows_done = rows_here, t_done = t_first, m_done = m_first, first_row = u.tile * ROWS;
-        if (starts && !ends && threadIdx.x == 0) {
-            PageSplit m2 = {s.b, s.row0, first_row, rows_done, h, shares.owner(u.at + u.cost - 1), ROWS, 0};
-            part.meta[cta] = m2;
-        }
+        const bool starts = k0 == 0, ends = u.at + u.cost <= x1;
+        const int slot = 2 * cta + (starts ? 1 : 0), h = u.h, rows_done = rows_here, t_done = t_first, m_done = m_first;
+        const int from = starts ? cta : shares.owner(u.at), parts = (ends ? cta : shares.owner(u.at + u.cost - 1)) - from + 1;     // the CTAs on this unit
         if (x < x1) {
             enter(x);
             if (C::EARLY) fetch_first();
@@ -498,21 +505,26 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             if (r >= rows_done) continue;
             const int t = G == 1 ? r : (int)__umulhi((uint32_t)(m_done + r), p.g_magic);
             float all = -INFINITY, sum = 0.f, acc[8];
+            if (parts == 1 || c0 == 0) {
 #pragma unroll
-            for (int q = 0; q < WARPS; ++q) all = fmaxf(all, ml_s[q * ROWS + r].x);
+                for (int q = 0; q < WARPS; ++q) all = fmaxf(all, ml_s[q * ROWS + r].x);
+#pragma unroll
+                for (int q = 0; q < WARPS; ++q) {
+                    const float2 v = ml_s[q * ROWS + r];
+                    // (a maximum of -inf carries no weight, a sum that is NaN is kept)
+                    sum += v.x == -INFINITY ? v.y * 0.f : v.y * ex2(v.x - all);
+                }
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) acc[e] = 0.f;
 #pragma unroll
             for (int q = 0; q < WARPS; ++q) {
-                const float2 v = ml_s[q * ROWS + r];
-                // (a maximum of -inf carries no weight, a sum that is NaN is kept)
-                sum += v.x == -INFINITY ? v.y * 0.f : v.y * ex2(v.x - all);
                 const float *src = reinterpret_cast<const float *>(smem + q * C::WARP + o_at) + r * HD;
                 const float4 y0 = *reinterpret_cast<const float4 *>(src + 4 * ((c0 >> 2) ^ ((r >> 1) & 3))), y1 = *reinterpret_cast<const float4 *>(src + 4 * ((c0 >> 2) + 1 ^ ((r >> 1) & 3)));
                 acc[0] += y0.x; acc[1] += y0.y; acc[2] += y0.z; acc[3] += y0.w;
                 acc[4] += y1.x; acc[5] += y1.y; acc[6] += y1.z; acc[7] += y1.w;
             }
-            if (starts && ends) {
+            if (parts == 1) {
                 const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) acc[e] *= inv;
@@ -522,25 +534,49 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 if (c0 == 0) part.ml[(size_t)slot * part.rows + r] = make_float2(all, sum);
             }
         }
-        if (x >= x1) return;
         fence_proxy_async_smem();    // (blocks come over what the warps put down)
         __syncthreads();             // (this unit's results have been read, the next one's Q is there)
+        if (parts > 1 && threadIdx.x == 0) {
+            Join &jn = sh->join[starts ? 1 : 0];
+            jn.parts = arrive_gpu(part.arrived + from) == (uint32_t)parts - 1u ? parts : 0;
+            jn.from = from; jn.row = s.row0 + t_done; jn.head = h * G; jn.m = m_done; jn.rows = rows_done;
+        }
+        if (x >= x1) break;
         if (!C::EARLY) fetch_first();
+    }
+
+    // ---- the last CTA on a split unit to come by joins the partials of all, behind its own units ----
+    for (int which = 0; which < 2; ++which) {
+        __syncthreads();
+        const Join jn = sh->join[which];
+        const int n = jn.parts;
+        if (n == 0) continue;
+        if (threadIdx.x == 0) part.arrived[jn.from] = 0u;
+        // (short code: what runs once costs what it takes to fetch it; forms with 16 partials on their way or the weights worked out first were no faster)
+        for (int i = threadIdx.x; i < ROWS * (HD / 8); i += 32 * WARPS) {
+            const int r = i % ROWS, c0 = i / ROWS * 8, t = G == 1 ? r : (int)__umulhi((uint32_t)(jn.m + r), p.g_magic);
+            PageSum a;
+            page_sum(part, HD, jn.from, n, r, c0, 0, 1, a);
+            if (r >= jn.rows) continue;
+            const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a.o[e] *= inv;
+            store8((__nv_bfloat16 *)p.out + ((size_t)(jn.row + t) * g.Hq + jn.head + jn.m + r - t * G) * HD + c0, a.o);
+        }
     }
 }
 
 template <int FMT, int HD, int NT>
-static cudaError_t launch_token(const PageAttention &a, const PagePartials &part, int sm_count, int &ctas, cudaStream_t st)
+static cudaError_t launch_token(const PageAttention &a, const PagePartials &part, int sm_count, cudaStream_t st)
 {
     using C = Tok<FMT, HD, NT>;
     static std::atomic<unsigned long long> done{0};
     cudaError_t e = once_per_device(done, [] { return cudaFuncSetAttribute(page_token_kernel<FMT, HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::SMEM); });
     if (e != cudaSuccess) return e;
-    ctas = std::min(sm_count, kMostCtas);
     CUtensorMap tk, tv;
     if (!encode_map_rows(&tk, a.g.k, C::ROW, a.g.n_pages * a.g.Hkv * a.g.P, 16) || !encode_map_rows(&tv, a.g.v, C::ROW, a.g.n_pages * a.g.Hkv * a.g.P, 16)) return cudaErrorInvalidValue;
     count_launch();
-    page_token_kernel<FMT, HD, NT><<<ctas, 32 * C::WARPS, C::SMEM, st>>>(tk, tv, a, part);
+    page_token_kernel<FMT, HD, NT><<<std::min(sm_count, kTokenCtas), 32 * C::WARPS, C::SMEM, st>>>(tk, tv, a, part);
     return cudaGetLastError();
 }
 
@@ -553,13 +589,13 @@ int page_token_rows(int dtype, int format, int d, int G, int rows)
     return rows <= 8 || wide ? 8 : 16;
 }
 
-cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int sm_count, int &ctas, cudaStream_t st)
+cudaError_t launch_page_token(const PageAttention &a, const PagePartials &part, int format, int rows, int sm_count, cudaStream_t st)
 {
     auto go = [&](auto f, auto hd) -> cudaError_t {
         constexpr int FMT = decltype(f)::value, HD = decltype(hd)::value;
         if constexpr (!(FMT == REFLEX_PAGE_SAME && HD == 256))
-            if (rows == 16) return launch_token<FMT, HD, 2>(a, part, sm_count, ctas, st);
-        return launch_token<FMT, HD, 1>(a, part, sm_count, ctas, st);
+            if (rows == 16) return launch_token<FMT, HD, 2>(a, part, sm_count, st);
+        return launch_token<FMT, HD, 1>(a, part, sm_count, st);
     };
     auto by_d = [&](auto f) -> cudaError_t {
         if (a.g.d == 64) return go(f, std::integral_constant<int, 64>{});

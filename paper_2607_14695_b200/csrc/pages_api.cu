@@ -36,18 +36,18 @@ size_t rows_of(const reflex_pages_desc &d) { return (size_t)d.n_pages * d.Hkv * 
 size_t row_bytes(const reflex_pages_desc &d) { return (size_t)d.d * (d.format == REFLEX_PAGE_SAME ? elem_size(d.dtype) : 1); }
 
 // Layout of the workspace: status word, marked sequences, partial results of split units, one layer of pages in bf16 (8-bit formats).
-struct PagesLayout { size_t done, careful, meta, ml, o, wide, bytes; };
+struct PagesLayout { size_t done, careful, arrived, meta, ml, o, wide, bytes; };
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-constexpr int kMostPairs = 128;
 bool widened(const reflex_pages_desc &d) { return d.format != REFLEX_PAGE_SAME && page_chunk_takes(d.dtype, d.Hq / d.Hkv, d.d); }
 PagesLayout pages_layout(const reflex_pages_desc &d)
 {
-    const size_t rows = page_chunk_takes(d.dtype, d.Hq / d.Hkv, d.d) ? std::max((size_t)2 * kMostCtas * 16, (size_t)2 * kMostPairs * 256) : (size_t)2 * kMostCtas * 16;
+    const size_t rows = page_chunk_takes(d.dtype, d.Hq / d.Hkv, d.d) ? std::max((size_t)2 * kTokenCtas * 16, (size_t)2 * kMostPairs * 256) : (size_t)2 * kTokenCtas * 16;
     PagesLayout w;
     w.done = 128;
     w.careful = 256;
-    w.meta = w.careful + kMaxSeqs;
-    w.ml = w.meta + up256(kMostCtas * sizeof(PageSplit));
+    w.arrived = w.careful + kMaxSeqs;
+    w.meta = w.arrived + 256 * sizeof(uint32_t);             // (all before it is zero at first, and after each call but for the status)
+    w.ml = w.meta + up256(kMostPairs * sizeof(PageSplit));
     w.o = w.ml + up256(rows * sizeof(float2));
     w.wide = w.o + up256(rows * (size_t)d.d * sizeof(float));
     w.bytes = w.wide + (widened(d) ? 2 * up256(rows_of(d) * (size_t)d.d * 2) : 0);
@@ -147,7 +147,7 @@ int reflex_pages_create(const reflex_pages_desc *desc, void *k_pool, void *v_poo
     p->k = (char *)k_pool; p->v = (char *)v_pool; p->ke = (char *)k_exp; p->ve = (char *)v_exp; p->ws = (char *)workspace;
     cudaError_t e = cudaGetDevice(&p->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device);
-    if (e == cudaSuccess) e = cudaMemsetAsync(workspace, 0, 256 + kMaxSeqs, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(workspace, 0, pages_layout(p->desc).meta, (cudaStream_t)stream);
     if (e != cudaSuccess) { delete p; return fail_cuda(e, "pages set-up"); }
     *out = p;
     return REFLEX_OK;
@@ -244,17 +244,16 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     const PagesLayout w = pages_layout(d);
     PagePartials part;
     part.o = (float *)(p->ws + w.o); part.ml = (float2 *)(p->ws + w.ml); part.meta = (PageSplit *)(p->ws + w.meta);
-    part.careful = (uint8_t *)(p->ws + w.careful); part.careful_done = (uint32_t *)(p->ws + w.done);
+    part.careful = (uint8_t *)(p->ws + w.careful); part.careful_done = (uint32_t *)(p->ws + w.done); part.arrived = (uint32_t *)(p->ws + w.arrived);
     part.scale_log2 = a.scale * 1.4426950408889634f;
     cudaError_t e;
-    int ctas = 0;
     const int token_rows = page_token_rows(d.dtype, d.format, d.d, G, (int)std::min(per_seq, 1ll << 20));
     if (token_rows) {
         part.rows = token_rows;
-        e = launch_page_token(a, part, d.format, token_rows, p->sm_count, ctas, st);
+        e = launch_page_token(a, part, d.format, token_rows, p->sm_count, st);
     } else if (page_chunk_takes(d.dtype, G, d.d)) {
         part.rows = 256;
-        ctas = std::min(p->sm_count / 2, kMostPairs);
+        const int pairs = std::min(p->sm_count / 2, kMostPairs);
         const void *k = a.g.k, *v = a.g.v;
         e = cudaSuccess;
         if (d.format != REFLEX_PAGE_SAME) {
@@ -262,11 +261,11 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
             v = p->ws + w.wide + (w.bytes - w.wide) / 2;
             e = launch_page_widen(a, (void *)k, (void *)v, d.format, p->sm_count, st);
         }
-        if (e == cudaSuccess) e = launch_page_chunk(a, part, k, v, ctas, st);
+        if (e == cudaSuccess) e = launch_page_chunk(a, part, k, v, pairs, st);
+        if (e == cudaSuccess) e = launch_page_merge(a, part, pairs, d.format, p->sm_count, st);
     } else {
         e = launch_page_plain(a, d.dtype, d.format, st);
     }
-    if (e == cudaSuccess && ctas) e = launch_page_merge(a, part, ctas, d.format, p->sm_count, st);
     return e == cudaSuccess ? REFLEX_OK : fail_cuda(e, "page attention launch");
 }
 
