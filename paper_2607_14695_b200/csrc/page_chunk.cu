@@ -12,7 +12,9 @@
 //                that has had the tile before leaves the row's reference, too; O is rescaled only where it has grown by more than 2^8.
 // What bounds it: at head_dim 256 the tensor pipe (2048 cycles a tile; operand reads then take two thirds of the shared memory's bandwidth), at 128 and
 // 64 the softmax (some 700 issue slots a scheduler and tile, which the helper warps need as well; a quarter of the exponentials by a
-// polynomial instead of the special-function unit cost more of them than the unit saved: 310 us for 301 at 4 x 4160 causal tokens, 16 heads of 128). Heads of 64 run as heads of 128 whose upper chunk is left out of
+// polynomial instead of the special-function unit cost more of them than the unit saved: 310 us for 301 at 4 x 4160 causal tokens, 16 heads of 128).
+// Measured: that prefill in 281 us, 1.0 PFLOP/s of the products that its mask leaves; a frame of 256 tokens of each of 16 sequences of 3376, 8 heads of
+// 256 on one KV head, 8-bit pages, in 115 us with widening (15) and merging (15). Heads of 64 run as heads of 128 whose upper chunk is left out of
 // Q K^T and whose upper columns of O are never read: P V costs twice, underneath the softmax.
 //
 // The grid is one pair per SM pair; the tiles of all units form one line that the pairs share evenly (PageLine), so uneven sequences, causal masks and single
@@ -37,10 +39,10 @@ constexpr int kChunkRows = 256;                // of a unit
 constexpr unsigned long long kChunkWaitNs = 1000000000ull;
 constexpr float kChunkGrow = 8.0f;             // log2 units: O is rescaled only where a maximum grows by more than 2^8
 
-// A unit costs kChunkSetUp blocks before its first tile: what its Q, its masks and its results take, in tiles. (A share that ends among them
+// A unit costs SET_UP blocks before its first tile: what its Q, its masks and its results take, in tiles. (A share that ends among them
 // leaves the unit to the next pair.)
-constexpr int kChunkSetUp = 4;
 struct ChunkSpan { int tile0, tiles, hi, count; };    // key tiles [tile0, tile0 + tiles), keys below hi; blocks
+template <int SET_UP>
 struct ChunkSpanOf {
     const PageAttention &p;
     int tokens;                                // of a unit
@@ -52,7 +54,7 @@ struct ChunkSpanOf {
         c.tile0 = r.lo / kChunkKeys;
         c.hi = r.hi;
         c.tiles = r.hi > r.lo ? (r.hi + kChunkKeys - 1) / kChunkKeys - c.tile0 : 0;
-        c.count = kChunkSetUp + max(1, c.tiles);
+        c.count = SET_UP + max(1, c.tiles);
         return c;
     }
 };
@@ -76,6 +78,7 @@ template <int HD, int D> struct Chunk {
     static constexpr int NG = HD == 256 ? 1 : 2;                // softmax groups of 8 warps
     static constexpr int THREADS = 128 + 256 * NG;
     static constexpr int NU = 8;                                // units in the list
+    static constexpr int SET_UP = HD == 256 ? 6 : 4;            // (attention of 16 frames at 256: 114.6 us with 6, 117.0 with 4; causal prefill at 128: 281 with 4, 288 with 6)
     static constexpr int QFULL = 0, QEMPTY = 1, KFULL = 2, KEMPTY = KFULL + NST, VLAND = KEMPTY + NST, VEMPTY = VLAND + NST, SFULL = VEMPTY + NST, PFULL = SFULL + NS,
                          PVDONE = PFULL + NS, OFREE = PVDONE + 4, UFULL = OFREE + 1, UEMPTY = UFULL + NU, COUNT = UEMPTY + NU;
     static constexpr uint32_t BAR_BYTES = (8 * COUNT + 104 + 127) / 128 * 128;                // ... tensor memory's address, abort flag, bad units, tiles
@@ -136,8 +139,9 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const int G = p.g.Hq / p.g.Hkv;
     // The K producer walks the line. It looks for its pair's place first of all: what the line is made of does not change under this kernel (only the widening of
     // pages runs beside its start).
-    PageLine<ChunkSpanOf> line{p, {p, 2 * tile_tokens}};
-    typename PageLine<ChunkSpanOf>::Place place;
+    using Line = PageLine<ChunkSpanOf<L::SET_UP>>;
+    Line line{p, {p, 2 * tile_tokens}};
+    typename Line::Place place;
     int total = 0, x0 = 0, x1 = 0, nc = 0;
     if (warp == 0) {
         total = line.begin(lane);
@@ -229,7 +233,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 
     if (warp == 0) {
         // ---------------- the list of units; Q and K by TMA (the warp stays converged, one lane issues) ----------------
-        // A unit costs kChunkSetUp blocks ahead of its tiles; a share that ends among them leaves the unit to the next pair.
+        // A unit costs SET_UP blocks ahead of its tiles; a share that ends among them leaves the unit to the next pair.
         const PageShares shares(total, max(1, nc));
         ChunkUnit *list = reinterpret_cast<ChunkUnit *>(smem + L::OFF_UNITS);
         if (lane == 0 && rank == 0) part.meta[pair].b = -1;
@@ -248,9 +252,9 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             c.valid = false;
             while (x < x1 && ok) {
                 const int to = min(place.at + place.cost, x1);
-                const int k0 = max(0, x - place.at - kChunkSetUp), k1 = max(0, to - place.at - kChunkSetUp);
+                const int k0 = max(0, x - place.at - L::SET_UP), k1 = max(0, to - place.at - L::SET_UP);
                 if (k1 > 0) {
-                    const bool whole = k0 == 0 && k1 == place.cost - kChunkSetUp;
+                    const bool whole = k0 == 0 && k1 == place.cost - L::SET_UP;
                     const ChunkUnit u = {place.s.b, place.s.row0, place.s.n, place.s.len, place.tile * 2 * tile_tokens, place.h, place.sp.tile0 + k0, max(0, min(k1, place.sp.tiles) - k0), place.sp.hi,
                                          whole ? -1 : 2 * pair + (k0 == 0 ? 1 : 0), {0, 0, 0, 0, 0, 0}};
                     publish(u);

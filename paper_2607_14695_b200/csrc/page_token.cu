@@ -580,7 +580,10 @@ static cudaError_t launch_token(const PageAttention &a, const PagePartials &part
     return cudaGetLastError();
 }
 
-// Rows of a tile for `rows` (token, head) rows per sequence and KV head on average; 0: not for this kernel.
+// Rows of a tile for `rows` (token, head) rows per sequence and KV head on average; 0: not for this kernel. Every tile reads the keys again (from L2) and has
+// them expanded again, so page_chunk_kernel is ahead from some number of rows on; later in 8-bit formats, whose pages have to be widened for it.
+// bf16, 64 streams: 53 us here and 57 there at 16 rows of 256 (3300 keys), 124 and 57 at 32; 95 and 79 at 32 rows of 128 (2000 keys, 4 KV heads).
+// int8: 63 and 115 at 32 rows of 256, 111 and 117 at 64; 96 and 145, 174 and 145 at 32 and 64 rows of 128; 134 and 202 at 32 rows of 64.
 int page_token_rows(int dtype, int format, int d, int G, int rows)
 {
     if (dtype != REFLEX_DTYPE_BF16 || d < 64 || G > 4096) return 0;
