@@ -30,14 +30,15 @@ __device__ __forceinline__ void page_sum(const PagePartials &part, int d, int ct
         float top = a.m;
 #pragma unroll
         for (int j = 0; j < 4; ++j) top = fmaxf(top, ml[j].x);
-        const float old = a.m == -INFINITY ? 0.f : ptx::ex2(a.m - top);
+        // (weights are never 0 where something was seen: an infinity among the values stays one)
+        const float old = a.m == -INFINITY ? 0.f : fmaxf(ptx::ex2(a.m - top), 1.2e-38f);
         a.l *= a.m == -INFINITY ? 1.f : old;             // (0, or the NaN of a part that went wrong)
 #pragma unroll
         for (int e = 0; e < 8; ++e) a.o[e] *= old;
         a.m = top;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float w = ml[j].x == -INFINITY ? 0.f : ptx::ex2(ml[j].x - top);
+            const float w = ml[j].x == -INFINITY ? 0.f : fmaxf(ptx::ex2(ml[j].x - top), 1.2e-38f);
             a.l += ml[j].y * w;
             if (w == 0.f) continue;                     // (what a part that has seen nothing left there is not looked at)
             const float f[8] = {v[j][0].x, v[j][0].y, v[j][0].z, v[j][0].w, v[j][1].x, v[j][1].y, v[j][1].z, v[j][1].w};

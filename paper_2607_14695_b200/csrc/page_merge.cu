@@ -91,14 +91,13 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int pairs)
     if (!any_marked) return;
     // ---- marked sequences ----
     __syncthreads();
-    float *q_s = reinterpret_cast<float *>(scratch) + warp * 256;
     for (int b = 0; b < p.q.B; ++b) {
         if (!part.careful[b]) continue;
         const PageSeq s = page_seq(p, b);
         const long long items = (long long)s.n * p.g.Hq, warps = (long long)gridDim.x * (kMergeThreads / 32);
         for (long long i = (long long)blockIdx.x * (kMergeThreads / 32) + warp; i < items; i += warps) {
             const int t = (int)(i / p.g.Hq);
-            page_plain_row<__nv_bfloat16, FMT>(p, b, s.row0 + t, (int64_t)s.len - s.n + t, s.len, (int)(i % p.g.Hq), q_s);
+            page_plain_row<__nv_bfloat16, FMT>(p, b, s.row0 + t, (int64_t)s.len - s.n + t, s.len, (int)(i % p.g.Hq));
         }
     }
     __syncthreads();

@@ -225,6 +225,6 @@ struct PageAttention {
     __device__ __forceinline__ int token_of(int row, int G) const { return g_shift >= 0 ? row >> g_shift : row / G; }      // of a (token, head) row
     uint32_t g_magic;         // x / (Hq / Hkv) = __umulhi(x, g_magic) for x < 2^16 (and more than one head in a group)
 };
-cudaError_t launch_page_plain(const PageAttention &a, int dtype, int format, cudaStream_t st);
+cudaError_t launch_page_plain(const PageAttention &a, int dtype, int format, int sm_count, cudaStream_t st);
 
 }  // namespace reflex

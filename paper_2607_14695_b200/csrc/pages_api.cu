@@ -264,7 +264,7 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
         if (e == cudaSuccess) e = launch_page_chunk(a, part, k, v, pairs, st);
         if (e == cudaSuccess) e = launch_page_merge(a, part, pairs, d.format, p->sm_count, st);
     } else {
-        e = launch_page_plain(a, d.dtype, d.format, st);
+        e = launch_page_plain(a, d.dtype, d.format, p->sm_count, st);
     }
     return e == cudaSuccess ? REFLEX_OK : fail_cuda(e, "page attention launch");
 }
