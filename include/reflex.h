@@ -366,7 +366,8 @@ typedef struct {
  * parts of both.
  * The kernels check what they follow: a table entry outside [0, n_pages) or a position outside [0, max_pages * page) is never
  * dereferenced. What such a token would have written is left out, what would have been read through it (the row read back; every row of
- * the sequence's attention that sees it) is NaN, and reflex_pages_check_status names the sequence. */
+ * the sequence's attention that sees it, and maybe rows of the sequence beside them) is NaN, and reflex_pages_check_status names the sequence.
+ * A table spans at most 2^30 positions. */
 typedef struct {
     const int32_t *table; /* device [B][max_pages]                          */
     const int32_t *cu;    /* device [B + 1] (reflex_pages_read: may be NULL) */

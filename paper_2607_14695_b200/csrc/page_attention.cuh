@@ -29,6 +29,10 @@ __device__ __forceinline__ PageRange page_range(const PageSeq &s, const PageAtte
     PageRange r;
     r.hi = p.causal ? max(0, min(s.len, p1 + 1)) : s.len;
     r.lo = p.window > 0 ? max(0, p0 - p.window + 1) : 0;      // (p0 >= -n: no underflow)
+    // (of positions past the table the first one is looked at, and reported, however far a length goes)
+    const int cap = p.q.max_pages << p.g.log_p;
+    r.hi = min(r.hi, cap + 1);
+    r.lo = min(r.lo, cap);
     return r;
 }
 

@@ -55,8 +55,9 @@ __device__ __forceinline__ void page_plain_sum(const PageAttention &p, int b, in
 {
     const PageGeom &g = p.g;
     const int lane = threadIdx.x & 31, h = hq / (g.Hq / g.Hkv);
-    const int64_t hi = p.causal ? min((int64_t)len, pos + 1) : len;
-    const int64_t lo = p.window > 0 ? max((int64_t)0, pos - p.window + 1) : 0;
+    const int64_t cap = (int64_t)p.q.max_pages << g.log_p;          // (of positions past the table the first one is looked at)
+    const int64_t hi = min(p.causal ? min((int64_t)len, pos + 1) : (int64_t)len, cap + 1);
+    const int64_t lo = min(p.window > 0 ? max((int64_t)0, pos - p.window + 1) : (int64_t)0, cap);
     float q[8];
     load_columns<T, REFLEX_PAGE_SAME, COLS>(p.qry, (((size_t)row * g.Hq + hq) * 32 + lane) * COLS, q);
     a.m = -INFINITY; a.l = 0.f;

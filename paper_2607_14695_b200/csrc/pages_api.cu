@@ -77,8 +77,8 @@ int check_call(const reflex_pages_t *p, int layer, int n_layers, const reflex_pa
         return api_fail(REFLEX_ERR_INVALID_ARG, "layers [%d, %lld) outside [0, L=%d)", layer, (long long)layer + n_layers, p->desc.L);
     if (!q) return api_fail(REFLEX_ERR_INVALID_ARG, "batch is NULL");
     if (q->B < 1 || q->B > p->desc.max_seqs) return api_fail(REFLEX_ERR_SHAPE, "B=%d outside [1, max_seqs=%d]", q->B, p->desc.max_seqs);
-    if (q->max_pages < 1 || (long long)q->max_pages * p->desc.page > 0x7fffffffll)
-        return api_fail(REFLEX_ERR_SHAPE, "max_pages=%d: positions must fit 31 bits, and there is one page at least", q->max_pages);
+    if (q->max_pages < 1 || (long long)q->max_pages * p->desc.page > 1ll << 30)
+        return api_fail(REFLEX_ERR_SHAPE, "max_pages=%d: a table spans at most 2^30 positions, and one page at least", q->max_pages);
     if (!q->table || !q->len || (needs_cu && !q->cu)) return api_fail(REFLEX_ERR_INVALID_ARG, "table, cu or len of the batch is NULL");
     if (!aligned(q->table, 4) || !aligned(q->len, 4) || !aligned(q->cu, 4)) return api_fail(REFLEX_ERR_ALIGN, "table, cu or len of the batch not aligned to its elements");
     int dev = -1;

@@ -1,5 +1,6 @@
 """The paged prefix against its definitions in 64 bits: rotary positions with several axes, rows into 8-bit pages and back, attention of new
 tokens over pages."""
+import ctypes
 import math
 
 import numpy as np
@@ -420,6 +421,68 @@ def test_two_handles_at_once_share_pools():
             rb.reflex_pages_attention(pages, 0, c.batch, x, o, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, outs))
+
+
+@pytest.mark.parametrize("lens,Hkv,d", [([5000], 1, 256), ([700, 2000, 33, 1500, 900, 1, 0, 1200], 1, 256), ([1300, 16, 999, 2500], 4, 128), ([3000, 1111], 2, 64)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_one_token_of_long_sequences(fmt, lens, Hkv, d):
+    """Sequences whose keys many blocks of threads share, and blocks that have parts of two sequences; the same bits from every call."""
+    c = Paged(lens, [min(n, 1) for n in lens], 64, 8, Hkv, d, BF16, fmt, seed=d)
+    c.poison()
+    c.write_all()
+    q = c.normal(c.rows, 8, d)
+    first = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.zeros_like(q, device=DEV)).clone()
+    c.check(first, c.attend(q), str(lens))
+    for _ in range(4):
+        assert torch.equal(first, rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.zeros_like(q, device=DEV)))
+    rb.reflex_pages_check_status(c.pages)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("at", [5, 1990])
+def test_infinities_whose_weight_underflows(dtype, at):
+    """An infinite value of a key that the others outweigh by 2^300 does not come out finite, wherever in the sequence it is and whoever joins the parts."""
+    n, d = 2000, 128
+    c = Paged([n], [1], 64, 4, 1, d, dtype, rb.PAGE_SAME)
+    k, v = torch.zeros(n, 1, d, dtype=dtype), c.normal(n, 1, d)
+    k[:, 0, 0] = 1.0
+    k[at, 0, 0] = -1.0
+    v[at, 0, 3] = float("inf")
+    c.write_all(k=k, v=v)
+    q = torch.zeros(1, 4, d, dtype=dtype)
+    q[..., 0] = 104.0 * d ** 0.5                     # logits 104 and -104: e^208 = 2^300
+    out = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.zeros_like(q, device=DEV)).cpu()
+    rest = [i for i in range(d) if i != 3]
+    assert not torch.isfinite(out[..., 3]).any() and torch.isfinite(out[..., rest]).all()
+    mean = (v.double().sum(0) - v[at].double())[:, rest] / (n - 1)
+    assert ((out[0][:, rest].double() - mean).abs() <= 2.0 ** -7 * v.double()[:, 0, rest].abs().mean(0) + 1e-6).all()
+
+
+@pytest.mark.parametrize("dtype,fmt", [(BF16, rb.PAGE_SAME), (BF16, rb.PAGE_INT8), (F32, rb.PAGE_E4M3)])
+@pytest.mark.parametrize("news,window", [([1, 1], 0), ([40, 45], 0), ([40, 45], 50)])
+def test_lengths_far_past_the_table(dtype, fmt, news, window):
+    """The largest length there is: nothing is followed, the sequence reads NaN and is named, and the call ends; the other sequence is right."""
+    c = Paged([100, 90], news, 32, 8, 1, 128, dtype, fmt, seed=5)
+    c.write_all()
+    batch = rb.PageBatch(c.batch.table, c.batch.cu, torch.tensor([100, 2 ** 31 - 1], dtype=torch.int32, device=DEV))
+    q = c.normal(c.rows, 8, 128)
+    out = torch.zeros((c.rows, 8, 128), dtype=dtype, device=DEV)
+    rb.reflex_pages_attention(c.pages, 0, batch, q.to(DEV), out, causal=True, window=window)
+    assert torch.isnan(out[news[0]:]).all()
+    want = c.attend(q, causal=True, window=window)
+    out[news[0]:] = want[0][news[0]:].to(DEV).to(dtype)
+    c.check(out, want)
+    with pytest.raises(rb.ReflexError) as e:
+        rb.reflex_pages_check_status(c.pages)
+    assert e.value.code == rb.ERR_STATE and "sequence 1" in str(e.value)
+
+
+def test_a_table_of_too_many_positions_is_refused():
+    c = Paged([100], [1], 32, 8, 1, 128, BF16, rb.PAGE_SAME)
+    q = torch.zeros(1, 8, 128, dtype=BF16, device=DEV)
+    b = c.batch
+    desc = rb.PageBatchDesc(b.table.data_ptr(), b.cu.data_ptr(), b.length.data_ptr(), 1, (1 << 30) // 32 + 1)
+    assert rb.load().reflex_pages_attention(c.pages.handle, 0, ctypes.byref(desc), q.data_ptr(), torch.empty_like(q).data_ptr(), 1, 0.0, 0, 0, None) == rb.ERR_SHAPE
 
 
 def test_rows_far_into_a_pool():
