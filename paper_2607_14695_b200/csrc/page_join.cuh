@@ -16,15 +16,14 @@ __device__ __forceinline__ void page_sum(const PagePartials &part, int d, int ct
 #pragma unroll
     for (int e = 0; e < 8; ++e) a.o[e] = 0.f;
     for (int i0 = first; i0 < n; i0 += 4 * step) {
-        float4 v[4][2];
+        float v[4][8];
         float2 ml[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int i = i0 + j * step;
             if (i < n) {
-                ml[j] = __ldcg(part.ml + slot(i) * part.rows + r);
-                const float4 *src = reinterpret_cast<const float4 *>(partial8(part, slot(i), d, r, c0));
-                v[j][0] = __ldcg(src); v[j][1] = __ldcg(src + 1);
+                ml[j] = part.ml[slot(i) * part.rows + r];
+                ptx::ld_global_v8(partial8(part, slot(i), d, r, c0), v[j]);
             } else ml[j] = make_float2(-INFINITY, 0.f);
         }
         float top = a.m;
@@ -41,9 +40,8 @@ __device__ __forceinline__ void page_sum(const PagePartials &part, int d, int ct
             const float w = ml[j].x == -INFINITY ? 0.f : fmaxf(ptx::ex2(ml[j].x - top), 1.2e-38f);
             a.l += ml[j].y * w;
             if (w == 0.f) continue;                     // (what a part that has seen nothing left there is not looked at)
-            const float f[8] = {v[j][0].x, v[j][0].y, v[j][0].z, v[j][0].w, v[j][1].x, v[j][1].y, v[j][1].z, v[j][1].w};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a.o[e] = fmaf(f[e], w, a.o[e]);
+            for (int e = 0; e < 8; ++e) a.o[e] = fmaf(v[j][e], w, a.o[e]);
         }
     }
 }

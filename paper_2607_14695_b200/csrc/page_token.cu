@@ -530,7 +530,9 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 for (int e = 0; e < 8; ++e) acc[e] *= inv;
                 store8((__nv_bfloat16 *)p.out + ((size_t)(s.row0 + t_done + t) * g.Hq + h * G + m_done + r - t * G) * HD + c0, acc);
             } else {
-                store8(partial8(part, slot, HD, r, c0), acc);
+                const uint32_t bits[8] = {__float_as_uint(acc[0]), __float_as_uint(acc[1]), __float_as_uint(acc[2]), __float_as_uint(acc[3]),
+                                          __float_as_uint(acc[4]), __float_as_uint(acc[5]), __float_as_uint(acc[6]), __float_as_uint(acc[7])};
+                st_global_v8(partial8(part, slot, HD, r, c0), bits);
                 if (c0 == 0) part.ml[(size_t)slot * part.rows + r] = make_float2(all, sum);
             }
         }
