@@ -15,11 +15,11 @@ __device__ __forceinline__ void page_sum(const PagePartials &part, int d, int ct
     a.m = -INFINITY; a.l = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) a.o[e] = 0.f;
-    for (int i0 = first; i0 < n; i0 += 4 * step) {
-        float v[4][8];
-        float2 ml[4];
+    for (int i0 = first; i0 < n; i0 += 8 * step) {
+        float v[8][8];
+        float2 ml[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 8; ++j) {
             const int i = i0 + j * step;
             if (i < n) {
                 ml[j] = part.ml[slot(i) * part.rows + r];
@@ -28,7 +28,7 @@ __device__ __forceinline__ void page_sum(const PagePartials &part, int d, int ct
         }
         float top = a.m;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top = fmaxf(top, ml[j].x);
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, ml[j].x);
         // (weights are never 0 where something was seen: an infinity among the values stays one)
         const float old = a.m == -INFINITY ? 0.f : fmaxf(ptx::ex2(a.m - top), 1.2e-38f);
         a.l *= a.m == -INFINITY ? 1.f : old;             // (0, or the NaN of a part that went wrong)
@@ -36,7 +36,7 @@ __device__ __forceinline__ void page_sum(const PagePartials &part, int d, int ct
         for (int e = 0; e < 8; ++e) a.o[e] *= old;
         a.m = top;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 8; ++j) {
             const float w = ml[j].x == -INFINITY ? 0.f : fmaxf(ptx::ex2(ml[j].x - top), 1.2e-38f);
             a.l += ml[j].y * w;
             if (w == 0.f) continue;                     // (what a part that has seen nothing left there is not looked at)

@@ -554,7 +554,7 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const int n = jn.parts;
         if (n == 0) continue;
         if (threadIdx.x == 0) part.arrived[jn.from] = 0u;
-        // (short code: what runs once costs what it takes to fetch it; forms with 16 partials on their way or the weights worked out first were no faster)
+        // (short code: what runs once costs what it takes to fetch it; with the partials in shared memory, or the weights worked out first, it was no faster)
         for (int i = threadIdx.x; i < ROWS * (HD / 8); i += 32 * WARPS) {
             const int r = i % ROWS, c0 = i / ROWS * 8, t = G == 1 ? r : (int)__umulhi((uint32_t)(jn.m + r), p.g_magic);
             PageSum a;
