@@ -78,7 +78,7 @@ template <int HD, int D> struct Chunk {
     static constexpr int NG = HD == 256 ? 1 : 2;                // softmax groups of 8 warps
     static constexpr int THREADS = 128 + 256 * NG;
     static constexpr int NU = 8;                                // units in the list
-    static constexpr int SET_UP = HD == 256 ? 6 : 4;            // (attention of 16 frames at 256: 114.6 us with 6, 117.0 with 4; causal prefill at 128: 281 with 4, 288 with 6)
+    static constexpr int SET_UP = HD == 256 ? 6 : 4;            // (attention of 16 frames at 256: 2 % faster with 6 than with 4; causal prefill at 128: 281 with 4, 288 with 6)
     static constexpr int QFULL = 0, QEMPTY = 1, KFULL = 2, KEMPTY = KFULL + NST, VLAND = KEMPTY + NST, VEMPTY = VLAND + NST, SFULL = VEMPTY + NST, PFULL = SFULL + NS,
                          PVDONE = PFULL + NS, OFREE = PVDONE + 4, UFULL = OFREE + 1, UEMPTY = UFULL + NU, COUNT = UEMPTY + NU;
     static constexpr uint32_t BAR_BYTES = (8 * COUNT + 104 + 127) / 128 * 128;                // ... tensor memory's address, abort flag, bad units, tiles
@@ -468,15 +468,15 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 all_hi = page_range(s, p, 0, u.token).hi;
             }
             float m_ref = -INFINITY, l = 0.f;
-            // (One instance of this code for whole and for masked tiles: three, with 64 keys unrolled in each, were 40 KB that the instruction caches had to
-            // fetch again at every change, 3000 cycles of a unit.)
-#pragma unroll 1
-            for (int jj = NG == 1 || (gt & 1) == group ? 0 : 1; jj < n; jj += NG) {          // (groups take the tiles of the whole share in turn)
+            // (With two groups one instance of this code for whole and for masked tiles: three, with 64 keys unrolled in each, were 40 KB that the instruction caches had to
+            // fetch again at every change, 3000 cycles of a unit. With one group, where the tile's chain is what the tensor pipe waits for, two: 16 frames in 113.5 us, not 119.)
+            auto tile = [&](auto mode, const int jj) {          // 0: whole, 1: masked, 2: either
+                constexpr int MODE = decltype(mode)::value;
                 const int gi = gt + jj, buf = gi % NS, st = gi % NST;
                 const uint32_t vph = (uint32_t)(gi / NST) & 1u;
                 const int key0 = (t0 + jj) * kChunkKeys + half * 64;
                 const uint32_t s_addr = tmem_base + lane_addr + kColS + buf * kChunkKeys + half * 64;
-                const bool masked = key0 < all_lo || key0 + 64 > all_hi;
+                const bool masked = MODE == 1 || (MODE == 2 && (key0 < all_lo || key0 + 64 > all_hi));
                 const uint64_t mask = masked ? bits64(mine.lo - key0, mine.hi - key0) : ~0ull;       // keys that this row sees
                 float mx = -INFINITY;
                 // One group keeps its logits in registers (168 of them a thread); two groups (96) read them from tensor memory a second time.
@@ -605,6 +605,15 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(leader_pfull + 8u * (uint32_t)buf);
+            };
+#pragma unroll 1
+            for (int jj = NG == 1 || (gt & 1) == group ? 0 : 1; jj < n; jj += NG) {          // (groups take the tiles of the whole share in turn)
+                if constexpr (NG == 2) tile(std::integral_constant<int, 2>{}, jj);
+                else {
+                    const int key0 = (t0 + jj) * kChunkKeys + half * 64;
+                    if (key0 < all_lo || key0 + 64 > all_hi) tile(std::integral_constant<int, 1>{}, jj);
+                    else tile(std::integral_constant<int, 0>{}, jj);
+                }
             }
             gt += n;
             // The group that has had the last tile finishes the unit; the other one leaves it its references and sums and goes on to the next unit, whose first tile

@@ -1,6 +1,6 @@
 // Joins the partial results of units that several CTAs have worked on: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i, in an order that the
 // units alone decide. A thread takes 8 columns of a row (partials lie as [column group][row][8], so a warp reads a contiguous kilobyte) and has
-// the loads of 8 partials in flight (which is why there are two blocks per SM and not four: a frame of 256 tokens over 3376 keys in 23.9 us, not 27.0); long lists (one sequence over the whole device) are cut in 8 among the warps of a block, which then add up.
+// the loads of 8 partials in flight (which is why there are two blocks per SM and not four: a frame of 256 tokens over 3376 keys in 23.9 us, not 27.0); long lists (one sequence over the whole device) are cut among the warps of a block, which then add up.
 //
 // It also computes again, row by row, the sequences that the tensor-core kernel has marked (see PagePartials::careful).
 #include "page_join.cuh"
@@ -11,6 +11,7 @@ namespace reflex {
 constexpr int kMergeThreads = 256;
 constexpr int kMergeMost = kMostPairs;
 constexpr int kMergeLong = 16;            // partials of a unit from which on its list is cut
+constexpr int kMergeCut = 4;              // ... in so many
 
 __device__ __forceinline__ void page_add(PageSum &a, const PageSum &b)
 {
@@ -30,7 +31,8 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int pairs)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int d = p.g.d, groups = d >> 3, G = p.g.Hq / p.g.Hkv;
-    // pieces: 256 (row, column group) items of a unit; 32 where its list of partials is cut
+    // pieces: 256 (row, column group) items of a unit; fewer where its list of partials is cut
+    constexpr int kItems = kMergeThreads / kMergeCut;
     // (sequences are marked before this kernel, and the marks go when its last block is done: all blocks see the same)
     bool marked = false;
     for (int b = tid; b < p.q.B; b += kMergeThreads) marked |= part.careful[b] != 0;
@@ -38,7 +40,7 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int pairs)
     if (tid < pairs) {
         const PageSplit s = part.meta[tid];
         of = s.b;
-        const int per = s.last - tid + 1 > kMergeLong ? 32 : 256;
+        const int per = s.last - tid + 1 > kMergeLong ? kItems : kMergeThreads;
         if (s.b >= 0) pieces = (s.rows * groups + per - 1) / per;
     }
     const bool any_marked = __syncthreads_or(marked);
@@ -68,18 +70,18 @@ page_merge_kernel(const PageAttention p, const PagePartials part, int pairs)
         const PageSplit m = part.meta[lo];
         const int n = m.last - lo + 1;
         const bool cut = n > kMergeLong;
-        const int item = (w - first_s[lo]) * (cut ? 32 : 256) + (cut ? lane : tid);
+        const int item = (w - first_s[lo]) * (cut ? kItems : kMergeThreads) + (cut ? tid % kItems : tid);
         const int r = item % m.rows, c0 = item / m.rows * 8, at = r < m.half ? r : 128 + r - m.half;
         const bool live = c0 < d;
         PageSum a;
-        if (live) page_sum(part, d, lo, n, at, c0, cut ? warp : 0, cut ? 8 : 1, a);
+        if (live) page_sum(part, d, lo, n, at, c0, cut ? tid / kItems : 0, cut ? kMergeCut : 1, a);
         if (cut) {
             PageSum *all = reinterpret_cast<PageSum *>(scratch);
             __syncthreads();
             if (live) all[tid] = a;
             __syncthreads();
-            if (warp > 0 || !live) continue;
-            for (int q = 1; q < 8; ++q) page_add(a, all[q * 32 + lane]);
+            if (tid >= kItems || !live) continue;
+            for (int q = 1; q < kMergeCut; ++q) page_add(a, all[q * kItems + tid]);
         }
         if (!live) continue;
         const float inv = a.l == 0.f ? 0.f : 1.f / a.l;
