@@ -438,6 +438,21 @@ def test_one_token_of_long_sequences(fmt, lens, Hkv, d):
     rb.reflex_pages_check_status(c.pages)
 
 
+@pytest.mark.parametrize("lens,news,Hkv,d,window", [([5000], [40], 1, 256, 0), ([9000, 70], [20, 33], 2, 128, 0), ([4100], [70], 1, 64, 3000)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_chunk_of_a_long_sequence(fmt, lens, news, Hkv, d, window):
+    """Few rows over many keys: dozens of parts of one result."""
+    c = Paged(lens, news, 64, 8, Hkv, d, BF16, fmt, seed=d)
+    c.poison()
+    c.write_all()
+    q = c.normal(c.rows, 8, d)
+    first = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.zeros_like(q, device=DEV), causal=True, window=window).clone()
+    c.check(first, c.attend(q, causal=True, window=window), str(lens))
+    for _ in range(3):
+        assert torch.equal(first, rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.zeros_like(q, device=DEV), causal=True, window=window))
+    rb.reflex_pages_check_status(c.pages)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("at", [5, 1990])
 def test_infinities_whose_weight_underflows(dtype, at):
