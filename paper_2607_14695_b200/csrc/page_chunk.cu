@@ -13,8 +13,8 @@
 // What bounds it: at head_dim 256 the tensor pipe (2048 cycles a tile; operand reads then take two thirds of the shared memory's bandwidth), at 128 and
 // 64 the softmax (some 700 issue slots a scheduler and tile, which the helper warps need as well; a quarter of the exponentials by a
 // polynomial instead of the special-function unit cost more of them than the unit saved: 310 us for 301 at 4 x 4160 causal tokens, 16 heads of 128).
-// Measured: that prefill in 281 us, 1.0 PFLOP/s of the products that its mask leaves; a frame of 256 tokens of each of 16 sequences of 3376, 8 heads of
-// 256 on one KV head, 8-bit pages, in 115 us with widening (15) and merging (15). Heads of 64 run as heads of 128 whose upper chunk is left out of
+// Measured: that prefill in 283 us, 1.0 PFLOP/s of the products that its mask leaves; a frame of 256 tokens of each of 16 sequences of 3376, 8 heads of
+// 256 on one KV head, 8-bit pages, in 111 us with widening (15) and merging (12). Heads of 64 run as heads of 128 whose upper chunk is left out of
 // Q K^T and whose upper columns of O are never read: P V costs twice, underneath the softmax.
 //
 // The grid is one pair per SM pair; the tiles of all units form one line that the pairs share evenly (PageLine), so uneven sequences, causal masks and single

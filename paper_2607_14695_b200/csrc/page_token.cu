@@ -52,14 +52,13 @@ template <int FMT, int HD, int NT> struct Tok {
     static constexpr int KP = ROW / 64;                            // 16-byte pieces of a key per thread
     static constexpr int KEPP = BYTES ? 16 : 8;                    // elements of a piece of K
     static constexpr int VB = ROW / 8;                             // bytes of a value row per thread: 8, 16, 32, 64
-    static constexpr int VP = VB < 16 ? 1 : VB / 16;               // ... in pieces, of 8 bytes or 16
-    static constexpr int VPB = VB < 16 ? 8 : 16;
+    static constexpr int VPB = VB < 16 ? 8 : 16;                   // ... in pieces of so many
     static constexpr int VW = VB / 4;                              // ... in words
     static constexpr int VCOLS = VB < 16 ? 8 : BYTES ? 16 : 8;     // consecutive columns of a thread
     static constexpr int VPIECES = HD / 8 / VCOLS;
     static constexpr int ROWS = 8 * NT;
     // a warp's blocks of keys: 16 rows of K, 16 of V, in boxes of 128 bytes (or 64) as TMA swizzles them; the exponents lie behind all stages
-    static constexpr int BOX = ROW < 128 ? ROW : 128, BOXES = ROW / BOX;
+    static constexpr int BOX = ROW < 128 ? ROW : 128;
     static constexpr uint32_t K_BYTES = 16 * ROW, STAGE = 2 * K_BYTES;
     static constexpr int STAGES = STAGE > 4 * 1024 ? 2 : 3;
     // One CTA per SM, with as many warps as registers (some 64 of O per 8 rows of head_dim 256, and 100 others) and stages leave room for: what a

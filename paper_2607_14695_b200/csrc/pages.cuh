@@ -88,13 +88,6 @@ __device__ __forceinline__ uint32_t bf16x2_mul(uint32_t a, uint32_t b)
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-__device__ __forceinline__ uint32_t bf16x2_sub(uint32_t a, uint32_t b)
-{
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-    return r;
-}
-
 __device__ __forceinline__ uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t c)
 {
     uint32_t r;
@@ -173,21 +166,6 @@ __device__ __forceinline__ void widen8(const Raw8<T> &r, float *f)
             if constexpr (sizeof(T) == 2) { f[2 * j] = __uint_as_float(w[j] << 16); f[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
             else f[4 * i + j] = __uint_as_float(w[j]);
         }
-    }
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16 *p, float *f)
-{
-    const uint4 u = *reinterpret_cast<const uint4 *>(p);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { f[2 * i] = __uint_as_float(w[i] << 16); f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
-}
-__device__ __forceinline__ void load8(const float *p, float *f)
-{
-#pragma unroll
-    for (int i = 0; i < 8; i += 4) {
-        const float4 v = *reinterpret_cast<const float4 *>(p + i);
-        f[i] = v.x; f[i + 1] = v.y; f[i + 2] = v.z; f[i + 3] = v.w;
     }
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
