@@ -169,7 +169,7 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         return C::ROW < 128 ? v_piece + (e & 1) * 64 + (e >> 1) * 512 : (v_piece ^ ((e & 1) << 4)) + (e & 1) * 128 + (e >> 1) * 1024 + j * 2048;
     };
     // ---- the unit at hand ----
-    typename Line::Place u;
+    typename Line::Place u = sh->u;
     int t_first, m_first, rows_here, k0, kend, key0, ids_from, page_ids;
     uint32_t bad_pages;                                // of the blocks on their way, the first in bit 0
     auto token_of = [&](int r) -> int { return G == 1 ? r : (int)__umulhi((uint32_t)(m_first + r), p.g_magic); };        // of the tile's row r, from t_first on
