@@ -92,8 +92,8 @@ template <int HD, int D> struct Chunk {
     static constexpr uint32_t OFF_BAR = OFF_STAGE + NG * 128 * 128;
     static constexpr uint32_t OFF_UNITS = OFF_BAR + BAR_BYTES;       // [NU] ChunkUnit
     static constexpr uint32_t OFF_MAX = OFF_UNITS + NU * 64;          // [2 tiles][128 rows][2 halves] maxima of the logits
-    static constexpr uint32_t OFF_REF = OFF_MAX + 2 * 128 * 2 * 4;    // [128] reference maxima, from group to group
-    static constexpr uint32_t OFF_SUM = OFF_REF + 128 * 4;            // [2 units][2 NG][128] (reference, sum) of a row's threads
+    static constexpr uint32_t OFF_REF = OFF_MAX + 2 * 128 * 2 * 4;    // [NG][128] reference maxima, as a group leaves them to the other one
+    static constexpr uint32_t OFF_SUM = OFF_REF + NG * 128 * 4;       // [2 units][2 NG][128] (reference, sum) of a row's threads
     static constexpr uint32_t OFF_ROWS = OFF_SUM + 2 * 2 * NG * 128 * 8;
     static constexpr uint32_t NEED = OFF_ROWS + 128 * 4;
     static constexpr uint32_t TOTAL = NEED + 1024 > 232448 ? 232448 : NEED + 1024;
@@ -522,11 +522,13 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 asm volatile("bar.sync %0, %1;" ::"r"(1 + quarter + 4 * group), "n"(64 * NG) : "memory");
                 const float2 of_row = *reinterpret_cast<const float2 *>(maxima + ((gi & 1) * 128 + row) * 2);
                 const float top = fmaxf(of_row.x, of_row.y);
-                const float was = NG == 1 || jj == 0 ? m_ref : ref[row];          // the row's reference so far
+                // The row's reference so far, as the other group has left it with the tile before. (A place for each group: both threads of a row read, one
+                // writes. The other group writes its place again behind its next barrier here, where both have arrived after they read it.)
+                const float was = NG == 1 || jj == 0 ? m_ref : ref[(group ^ 1) * 128 + row];
                 const bool grow = jj == 0 || (top - was) * sc > kChunkGrow;
                 const float to = grow ? top : was;
                 if (NG == 2) {
-                    if (half == 0) ref[row] = to;
+                    if (half == 0) ref[group * 128 + row] = to;
                     asm volatile("bar.arrive %0, 128;" ::"r"(1 + quarter + 4 * (group ^ 1)) : "memory");
                 }
                 if (m_ref != to) { l *= m_ref == -INFINITY ? (l == l ? 0.f : 1.f) : ex2((m_ref - to) * sc); m_ref = to; }

@@ -552,3 +552,40 @@ def test_refusals_of_the_binding():
         assert e.value.code == code
     with pytest.raises(ValueError):
         rb.Pages(1, 4, 16, 8, 2, 64, rb.DTYPE_BF16, rb.PAGE_INT8, k_pool=torch.zeros(1, 4, 2, 16, 64, dtype=torch.int8, device=DEV)[..., :32])
+
+
+def _attend64(q, k, v, scale, causal, window=0, length=None, allowed=2.0 ** -8 + 2e-4):
+    """One sequence in 64 bits on the GPU: q [n][Hq][d], k, v [len][Hkv][d] (length: the sequence's, where it is not the rows that k has). (result, bound of the
+    error as in Paged.check)."""
+    (n, Hq, d), (have, Hkv) = q.shape, k.shape[:2]
+    length = have if length is None else length
+    p, j = torch.arange(length - n, length, device=DEV)[:, None], torch.arange(have, device=DEV)[None]
+    seen = (j < length) & (j <= p if causal else True) & (j > p - window if window else True)
+    out, lim = [torch.zeros((n, Hq, d), dtype=torch.float64, device=DEV) for _ in range(2)]
+    for h in range(Hq):
+        x, kh, vh = q[:, h].double(), k[:, h * Hkv // Hq].double(), v[:, h * Hkv // Hq].double()
+        logits = (x @ kh.T * scale).masked_fill(~seen, -math.inf)
+        w = torch.softmax(logits, -1).nan_to_num(0.0)              # (rows that see nothing are 0)
+        slip = ((x.abs() @ kh.abs().T).masked_fill(~seen, 0.0).amax(-1, keepdim=True)) * scale * d * 2.0 ** -24
+        out[:, h] = w @ vh
+        lim[:, h] = HALF[BF16] * out[:, h].abs() + (allowed + have * 2.0 ** -24 + 2 * slip) * (1 + HALF[BF16]) * (w @ vh.abs()) + 1e-30
+    return out, lim
+
+
+@pytest.mark.parametrize("d,Hq,Hkv", [(64, 4, 2), (128, 4, 2), (256, 2, 1)])
+@pytest.mark.parametrize("every", [128, 256])
+def test_logits_that_grow_from_tile_to_tile(d, Hq, Hkv, every):
+    """Causal attention over 4160 keys whose logits grow by 2^9 every tile or two: the accumulator is rescaled all the way, and every call gives the same bits."""
+    n = 4160
+    c = Paged([n], [n], 64, Hq, Hkv, d, BF16, rb.PAGE_SAME, seed=d)
+    k, v, q = c.normal(n, Hkv, d, std=0.2), c.normal(n, Hkv, d), c.normal(n, Hq, d, std=0.2)
+    k[:, :, 0] = (torch.arange(n) // every)[:, None].to(BF16)
+    q[:, :, 0] = 6.25                           # of 9.02 log2 units a step
+    k, v, q = k.to(DEV), v.to(DEV), q.to(DEV)
+    rb.reflex_pages_write(c.pages, 0, c.batch, k, v)
+    first = rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.empty_like(q), scale=1.0, causal=True).clone()
+    want, lim = _attend64(q, k, v, 1.0, True)
+    assert ((first.double() - want).abs() <= lim).all()
+    for _ in range(30):
+        assert torch.equal(first, rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.empty_like(q), scale=1.0, causal=True))
+    rb.reflex_pages_check_status(c.pages)

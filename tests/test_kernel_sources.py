@@ -89,3 +89,18 @@ def test_a_reported_wait_names_its_kernel():
     bases = sorted(sites[b] for b in used) + [sites["kSiteEnd"]]
     for base, (name, last) in used.items():
         assert sites[base] + last < min(b for b in bases if b > sites[base]), name
+
+
+# ---- the exchange of a row's threads in page_chunk_kernel ----
+
+def _body(name):
+    return next(body for n, _, body in KERNELS if n.endswith(": " + name))
+
+
+def test_a_reference_is_not_written_where_the_row_s_other_thread_reads_it():
+    """Behind the barrier of a tile both threads of a row read the reference that the other softmax group has left, and one of them writes the group's own: nothing orders
+    the two, so they may not be one place."""
+    body = _body("page_chunk_kernel")
+    written = re.findall(r"\bref\[([^;=]+?)\] = ", body)
+    read = re.findall(r"[:(,=] ref\[([^;=]+?)\][;,)]", body)
+    assert written == ["group * 128 + row"] and read == ["(group ^ 1) * 128 + row"], (written, read)
