@@ -91,8 +91,8 @@ template <int HD, int D> struct Chunk {
     static constexpr uint32_t OFF_STAGE = OFF_V + NST * V_STAGE;      // of each group: 128 rows x 64 columns of the result
     static constexpr uint32_t OFF_BAR = OFF_STAGE + NG * 128 * 128;
     static constexpr uint32_t OFF_UNITS = OFF_BAR + BAR_BYTES;       // [NU] ChunkUnit
-    static constexpr uint32_t OFF_MAX = OFF_UNITS + NU * 64;          // [2 tiles][128 rows][2 halves] maxima of the logits
-    static constexpr uint32_t OFF_REF = OFF_MAX + 2 * 128 * 2 * 4;    // [NG][128] reference maxima, as a group leaves them to the other one
+    static constexpr uint32_t OFF_MAX = OFF_UNITS + NU * 64;          // [2 tiles of each group][128 rows][2 halves] maxima of the logits
+    static constexpr uint32_t OFF_REF = OFF_MAX + 2 * NG * 128 * 2 * 4;    // [NG][128] reference maxima, as a group leaves them to the other one
     static constexpr uint32_t OFF_SUM = OFF_REF + NG * 128 * 4;       // [2 units][2 NG][128] (reference, sum) of a row's threads
     static constexpr uint32_t OFF_ROWS = OFF_SUM + 2 * 2 * NG * 128 * 8;
     static constexpr uint32_t NEED = OFF_ROWS + 128 * 4;
@@ -518,9 +518,11 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     }
                 }
                 if (!(mx < INFINITY)) l = __int_as_float(0x7fc00000);      // (a logit that is NaN or +inf)
-                maxima[((gi & 1) * 128 + row) * 2 + half] = mx;
+                // (two places for a group's tiles in turn: what a thread has not read yet is not written before the group's next barrier)
+                const int meet = ((gi & (2 * NG - 1)) * 128 + row) * 2;
+                maxima[meet + half] = mx;
                 asm volatile("bar.sync %0, %1;" ::"r"(1 + quarter + 4 * group), "n"(64 * NG) : "memory");
-                const float2 of_row = *reinterpret_cast<const float2 *>(maxima + ((gi & 1) * 128 + row) * 2);
+                const float2 of_row = *reinterpret_cast<const float2 *>(maxima + meet);
                 const float top = fmaxf(of_row.x, of_row.y);
                 // The row's reference so far, as the other group has left it with the tile before. (A place for each group: both threads of a row read, one
                 // writes. The other group writes its place again behind its next barrier here, where both have arrived after they read it.)

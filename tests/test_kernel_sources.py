@@ -104,3 +104,15 @@ def test_a_reference_is_not_written_where_the_row_s_other_thread_reads_it():
     written = re.findall(r"\bref\[([^;=]+?)\] = ", body)
     read = re.findall(r"[:(,=] ref\[([^;=]+?)\][;,)]", body)
     assert written == ["group * 128 + row"] and read == ["(group ^ 1) * 128 + row"], (written, read)
+
+
+def test_maxima_of_a_group_s_next_tile_go_to_another_place():
+    """The maxima of a tile are read behind its barrier, and the next tile's are written with no barrier between. Tiles of a group are two apart where there are two groups."""
+    body = _body("page_chunk_kernel")
+    place = re.search(r"const int meet = \(\((.*?)\) \* 128 \+ row\) \* 2;", body)
+    assert place and not re.search(r"maxima\[(?!meet \+ half\])|maxima \+ (?!meet\))", body), place
+    for groups in (1, 2):
+        at = [eval(place.group(1).replace("NG", str(groups)), {"gi": gi}) for gi in range(16)]
+        assert all(a != b for a, b in zip(at, at[groups:])) and max(at) < 2 * groups          # a group's tile and its next one
+        for gi in range(14):                                                                   # and no group writes where the other one reads
+            assert groups == 1 or at[gi] not in (at[gi + 1], at[gi + 2])
