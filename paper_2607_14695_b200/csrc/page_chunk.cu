@@ -621,11 +621,12 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
             gt += n;
             // The group that has had the last tile finishes the unit; the other one leaves it its references and sums and goes on to the next unit, whose first tile
-            // is its own. (It cannot come by with those of the unit after that before they are read: its tiles follow this group's.)
+            // is its own. (It cannot come by with those of the unit after that before they are read: it meets this group at the barrier of the unit between. A unit without
+            // tiles, whose rows see nothing, has no barrier: it leaves no sums.)
             const int g_last = gt - 1, parity = NG == 2 ? ui & 1 : 0;
             const bool finishes = NG == 1 || ((n > 0 ? g_last : gt) & 1) == group;
             if (n > 0 && !ok) l = __int_as_float(0x7fc00000);
-            sums[((parity * NG + group) * 2 + half) * 128 + row] = make_float2(m_ref, l);
+            if (n > 0) sums[((parity * NG + group) * 2 + half) * 128 + row] = make_float2(m_ref, l);
             if (!finishes) {
                 if (n > 0) {
                     asm volatile("bar.arrive %0, 512;" ::"r"(9 + parity) : "memory");
@@ -636,16 +637,13 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
             if (n > 0) {
                 ok = ok && wait(L::PVDONE + (g_last & 3), (uint32_t)(g_last >> 2) & 1u, 12);
-                if (NG == 2) asm volatile("bar.sync %0, 512;" ::"r"(9 + parity) : "memory");
-            }
-            if (NG == 1 || n == 0) group_sync();
-            // the row's sum: references may differ, the latest one is the largest
-            {
+                if (NG == 2) asm volatile("bar.sync %0, 512;" ::"r"(9 + parity) : "memory"); else group_sync();
+                // the row's sum: references may differ, the latest one is the largest
                 float2 part_of[2 * NG];
                 m_ref = -INFINITY;
 #pragma unroll
                 for (int q = 0; q < 2 * NG; ++q) {
-                    part_of[q] = q / 2 == group || n > 0 ? sums[(parity * 2 * NG + q) * 128 + row] : make_float2(-INFINITY, 0.f);
+                    part_of[q] = sums[(parity * 2 * NG + q) * 128 + row];
                     m_ref = fmaxf(m_ref, part_of[q].x);
                 }
                 l = 0.f;

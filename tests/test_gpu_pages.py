@@ -589,3 +589,23 @@ def test_logits_that_grow_from_tile_to_tile(d, Hq, Hkv, every):
     for _ in range(30):
         assert torch.equal(first, rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.empty_like(q), scale=1.0, causal=True))
     rb.reflex_pages_check_status(c.pages)
+
+
+@pytest.mark.parametrize("d,Hkv", [(64, 2), (128, 2), (256, 1)])
+def test_units_without_a_key_between_others(d, Hkv):
+    """Hundreds of sequences, of which every second or third has new tokens and no token that they see: every pair of blocks takes a dozen units, with and without keys in
+    turn (lists of units begin anew). The rows that see nothing are 0, the others are right, and every call gives the same bits."""
+    shapes = [(64, 256), (20, 0), (33, 390), (64, 250), (25, 0), (17, 129)]
+    news, lens = [[shapes[b % 6][i] for b in range(300)] for i in range(2)]
+    c = Paged(lens, news, 64, Hkv, Hkv, d, BF16, rb.PAGE_SAME, seed=d)
+    k, v, q = c.normal(sum(lens), Hkv, d, std=1.5).to(DEV), c.normal(sum(lens), Hkv, d).to(DEV), c.normal(c.rows, Hkv, d).to(DEV)
+    at = torch.tensor([0] + lens).cumsum(0).tolist()
+    rb.reflex_pages_write(c.pages, 0, rb.PageBatch(c.batch.table, torch.tensor(at, dtype=torch.int32, device=DEV), c.batch.length), k, v)
+    first = rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.full_like(q, 7.0)).clone()
+    for b, (n, length) in enumerate(zip(news, lens)):
+        r = slice(int(c.cu[b]), int(c.cu[b + 1]))
+        want, lim = _attend64(q[r], k[at[b]:at[b + 1]], v[at[b]:at[b + 1]], d ** -0.5, False) if length else (torch.zeros_like(q[r]).double(), 0.0)
+        assert ((first[r].double() - want).abs() <= lim).all(), b
+    for _ in range(10):
+        assert torch.equal(first, rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.full_like(q, 7.0)))
+    rb.reflex_pages_check_status(c.pages)

@@ -116,3 +116,9 @@ def test_maxima_of_a_group_s_next_tile_go_to_another_place():
         assert all(a != b for a, b in zip(at, at[groups:])) and max(at) < 2 * groups          # a group's tile and its next one
         for gi in range(14):                                                                   # and no group writes where the other one reads
             assert groups == 1 or at[gi] not in (at[gi + 1], at[gi + 2])
+
+
+def test_a_unit_without_tiles_leaves_no_sums():
+    """A softmax group that is ahead does not meet the other one at a unit without tiles. What it wrote there would be in the place of a unit that the other group may
+    not have finished."""
+    assert re.findall(r"([^;{}]*)\bsums\[[^;=]*\] = ", _body("page_chunk_kernel"))[0].strip() == "if (n > 0)"
