@@ -424,7 +424,7 @@ int reflex_pages_write(reflex_pages_t *pages, int layer, const reflex_page_batch
                        int n_rows, const reflex_rotary *rot, const int32_t *pos, void *stream);
 
 /* Tokens [start[b], len[b]) of every sequence (start NULL: 0; a negative start counts as 0) and of layers [layer, layer + n_layers) back as dense rows.
- *   k_out, v_out   device [B][n_layers][S_out][Hkv][d] dtype: token p to row p - start[b]; rows past a sequence's last token are left
+ *   k_out, v_out   device [B][n_layers][S_out][Hkv][d] dtype, 16-byte aligned: token p to row p - start[b]; rows past a sequence's last token are left
  *                  as they were, tokens past S_out rows are left out */
 int reflex_pages_read(reflex_pages_t *pages, int layer, int n_layers, const reflex_page_batch *batch, const int32_t *start, void *k_out, void *v_out,
                       int S_out, void *stream);

@@ -155,8 +155,9 @@ __device__ __forceinline__ Piece<T, FMT> take16(const void *pool, const uint8_t 
     p.e = FMT == REFLEX_PAGE_SAME ? 0 : exps[row];
     return p;
 }
+// (sectors: dst is a multiple of 32 bytes; outputs are promised 16)
 template <typename T, int FMT>
-__device__ __forceinline__ void give16(const Piece<T, FMT> &p, bool ok, T *dst)
+__device__ __forceinline__ void give16(const Piece<T, FMT> &p, bool ok, T *dst, bool sectors)
 {
     if constexpr (FMT == REFLEX_PAGE_SAME) {
         const uint32_t nan = sizeof(T) == 2 ? 0x7fc07fc0u : 0x7fc00000u;
@@ -172,7 +173,11 @@ __device__ __forceinline__ void give16(const Piece<T, FMT> &p, bool ok, T *dst)
             o[2 * i + 1] = bf16x2_mul(expand2<FMT, 2, 3>(biased<FMT>(in[i])), sc);
         }
         if constexpr (sizeof(T) == 2) {
-            ptx::st_global_v8(dst, o);
+            if (sectors) ptx::st_global_v8(dst, o);
+            else {
+                reinterpret_cast<uint4 *>(dst)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+                reinterpret_cast<uint4 *>(dst)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+            }
         } else {
             float f[16];
 #pragma unroll
@@ -197,6 +202,7 @@ page_read_kernel(const PageGeom g, const reflex_page_batch q, const int32_t *sta
     const size_t out0 = ((size_t)b * n_layers + l) * S_out;
     const int per_head = g.log_p + log_pieces;                                  // (page, head) blocks of 2^per_head pieces
     const int64_t i0 = (int64_t)blockIdx.x * (DEPTH * kRowThreads) + threadIdx.x;
+    const bool sectors = ((reinterpret_cast<uintptr_t>(k_out) | reinterpret_cast<uintptr_t>(v_out)) & 31u) == 0;
     Piece<T, FMT> pk[DEPTH], pv[DEPTH];
     int64_t out[DEPTH];                  // -1: none
     bool ok[DEPTH];
@@ -220,8 +226,8 @@ page_read_kernel(const PageGeom g, const reflex_page_batch q, const int32_t *sta
 #pragma unroll
     for (int j = 0; j < DEPTH; ++j) {
         if (out[j] < 0) continue;
-        give16<T, FMT>(pk[j], ok[j], k_out + out[j]);
-        give16<T, FMT>(pv[j], ok[j], v_out + out[j]);
+        give16<T, FMT>(pk[j], ok[j], k_out + out[j], sectors);
+        give16<T, FMT>(pv[j], ok[j], v_out + out[j], sectors);
     }
 }
 

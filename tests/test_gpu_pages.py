@@ -609,3 +609,39 @@ def test_units_without_a_key_between_others(d, Hkv):
     for _ in range(10):
         assert torch.equal(first, rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.full_like(q, 7.0)))
     rb.reflex_pages_check_status(c.pages)
+
+
+def _at_16(t):
+    """The same rows 16 bytes behind a multiple of 32."""
+    step = 16 // t.element_size()
+    room = torch.zeros(t.numel() + 2 * step, dtype=t.dtype, device=t.device)
+    assert room.data_ptr() % 32 == 0
+    y = room[step:step + t.numel()].view(t.shape)
+    y.copy_(t)
+    return y
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("news", [[1, 1], [40, 70]])
+def test_rows_at_16_bytes(fmt, dtype, news):
+    """Every tensor of rows 16 bytes behind a multiple of 32, which is all that is asked of it: the same bits."""
+    d, Hq, Hkv = 128, 4, 2
+    c = Paged([90, 170], news, 32, Hq, Hkv, d, dtype, fmt)
+    c.write_all()
+    rot = _rot(d, 2)
+    pos = torch.randint(0, 400, (2, c.rows), dtype=torch.int32, device=DEV)
+    rows = c.normal(c.rows, Hq + 2 * Hkv, d).to(DEV)
+    results = []
+    for place in (lambda t: t, _at_16):
+        x = place(rows)
+        q, out = [place(torch.zeros((c.rows, Hq, d), dtype=dtype, device=DEV)) for _ in range(2)]
+        kv = [place(torch.zeros((2, 1, 170, Hkv, d), dtype=dtype, device=DEV)) for _ in range(2)]
+        rb.reflex_rotary_axes(x[:, :Hq], q, pos, rot)
+        rb.reflex_pages_write(c.pages, 0, c.batch, x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], rotary=rot, pos=pos)
+        rb.reflex_pages_attention(c.pages, 0, c.batch, q, out, causal=True)
+        rb.reflex_pages_read(c.pages, 0, c.batch, kv[0], kv[1])
+        kv_mixed = [kv[0].clone(), place(torch.zeros_like(kv[1]))]                 # (one of the two at a multiple of 32)
+        rb.reflex_pages_read(c.pages, 0, c.batch, kv_mixed[0], kv_mixed[1])
+        results.append([t.clone() for t in (q, out, *kv, *kv_mixed)])
+    assert all(torch.equal(a, b) for a, b in zip(*results))

@@ -122,3 +122,12 @@ def test_a_unit_without_tiles_leaves_no_sums():
     """A softmax group that is ahead does not meet the other one at a unit without tiles. What it wrote there would be in the place of a unit that the other group may
     not have finished."""
     assert re.findall(r"([^;{}]*)\bsums\[[^;=]*\] = ", _body("page_chunk_kernel"))[0].strip() == "if (n > 0)"
+
+
+def test_32_byte_stores_to_the_caller_s_rows_look_at_their_address():
+    """Outputs are promised 16-byte alignment. A store of 32 bytes faults on any other multiple of 16: of the paged prefix, those that do not go to the workspace come behind a
+    look at the address."""
+    text = open(os.path.join(CSRC, "page_rows.cu")).read()
+    stores = re.findall(r"([^\n;{}]*)\bptx::st_global_v8\(", text)
+    assert stores and all(s.strip() == "if (sectors)" for s in stores), stores
+    assert re.search(r"const bool sectors = \(\(reinterpret_cast<uintptr_t>\(k_out\) \| reinterpret_cast<uintptr_t>\(v_out\)\) & 31u\) == 0;", text)
