@@ -236,9 +236,10 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     a.g_shift = (G & (G - 1)) == 0 ? __builtin_ctz((unsigned)G) : -1;
     a.g_magic = G > 1 ? 0xffffffffu / (uint32_t)G + 1u : 0u;
     const long long per_seq = ((long long)n_rows * G + batch->B - 1) / batch->B;           // (token, head) rows of a sequence and KV head
-    // (the tensor-core kernels count tiles of rows times blocks of 64 keys in 32 bits)
-    if (page_chunk_takes(d.dtype, G, d.d) &&
-        ((double)n_rows * G / 8 + batch->B) * d.Hkv * ((double)batch->max_pages * d.page / 64 + 2) > 2.0e9)
+    const int token_rows = page_token_rows(d.dtype, d.format, d.d, G, (int)std::min(per_seq, 1ll << 20));
+    // (the tensor-core kernels count tiles of rows times blocks of 64 keys, and the rows of a KV head to the end of the last tile, in 32 bits)
+    if ((token_rows || page_chunk_takes(d.dtype, G, d.d)) &&
+        ((long long)n_rows * G > 0x7fffff00ll || ((double)n_rows * G / 8 + batch->B) * d.Hkv * ((double)batch->max_pages * d.page / 64 + 2) > 2.0e9))
         return api_fail(REFLEX_ERR_SHAPE, "n_rows=%d, B=%d and max_pages=%d: more tiles of rows and keys than 31 bits count", n_rows, batch->B, batch->max_pages);
     cudaStream_t st = (cudaStream_t)stream;
     const PagesLayout w = pages_layout(d);
@@ -247,7 +248,6 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     part.careful = (uint8_t *)(p->ws + w.careful); part.careful_done = (uint32_t *)(p->ws + w.done); part.arrived = (uint32_t *)(p->ws + w.arrived);
     part.scale_log2 = a.scale * 1.4426950408889634f;
     cudaError_t e;
-    const int token_rows = page_token_rows(d.dtype, d.format, d.d, G, (int)std::min(per_seq, 1ll << 20));
     if (token_rows) {
         part.rows = token_rows;
         e = launch_page_token(a, part, d.format, token_rows, p->sm_count, st);

@@ -645,3 +645,14 @@ def test_rows_at_16_bytes(fmt, dtype, news):
         rb.reflex_pages_read(c.pages, 0, c.batch, kv_mixed[0], kv_mixed[1])
         results.append([t.clone() for t in (q, out, *kv, *kv_mixed)])
     assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+@pytest.mark.parametrize("Hq,Hkv,n_rows,max_pages", [(1024, 4, 65536, 1024), (4096, 1, 600000, 1), (4096, 1, 524288, 1), (1024, 8, 65536, 1024)])
+def test_lines_of_more_work_than_31_bits_count_are_refused(Hq, Hkv, n_rows, max_pages):
+    """... whichever kernel would count it: groups of 129 to 4096 heads as well. (Nothing is launched: the rows do not exist.)"""
+    pages = rb.Pages(1, 4, 128, Hq, Hkv, 128, rb.DTYPE_BF16, rb.PAGE_INT8, max_seqs=1, max_rows=n_rows)
+    table, cu, length, rows = [torch.zeros(max(n, 64), dtype=torch.int32, device=DEV) for n in (max_pages, 2, 1, 64)]
+    desc = rb.PageBatchDesc(table.data_ptr(), cu.data_ptr(), length.data_ptr(), 1, max_pages)
+    before = rb.reflex_kernel_launch_count()
+    assert rb.load().reflex_pages_attention(pages.handle, 0, ctypes.byref(desc), rows.data_ptr(), rows.data_ptr() + 64, n_rows, 0.0, 0, 0, None) == rb.ERR_SHAPE
+    assert rb.reflex_kernel_launch_count() == before
