@@ -28,7 +28,7 @@ __device__ __forceinline__ PageRange page_range(const PageSeq &s, const PageAtte
     const int p0 = s.len - s.n + t0, p1 = s.len - s.n + t1;
     PageRange r;
     r.hi = p.causal ? max(0, min(s.len, p1 + 1)) : s.len;
-    r.lo = p.window > 0 ? max(0, p0 - p.window + 1) : 0;      // (p0 >= -n: no underflow)
+    r.lo = p.window > 0 && p0 >= p.window ? p0 - p.window + 1 : 0;      // (p0 may be negative, and the window as large as there is)
     // (of positions past the table the first one is looked at, and reported, however far a length goes)
     const int cap = p.q.max_pages << p.g.log_p;
     r.hi = min(r.hi, cap + 1);

@@ -656,3 +656,18 @@ def test_lines_of_more_work_than_31_bits_count_are_refused(Hq, Hkv, n_rows, max_
     before = rb.reflex_kernel_launch_count()
     assert rb.load().reflex_pages_attention(pages.handle, 0, ctypes.byref(desc), rows.data_ptr(), rows.data_ptr() + 64, n_rows, 0.0, 0, 0, None) == rb.ERR_SHAPE
     assert rb.reflex_kernel_launch_count() == before
+
+
+@pytest.mark.parametrize("dtype,fmt", [(BF16, rb.PAGE_SAME), (BF16, rb.PAGE_INT8), (F32, rb.PAGE_SAME)])
+@pytest.mark.parametrize("lens,news", [([5, 40], [9, 1]), ([30, 200], [70, 90])])
+@pytest.mark.parametrize("causal", [False, True])
+def test_the_largest_window(dtype, fmt, lens, news, causal):
+    """A window that limits nothing, over rows in front of the first token too (more new tokens than tokens)."""
+    c = Paged(lens, news, 16, 8, 1, 128, dtype, fmt, seed=4)
+    c.write_all()
+    q = c.normal(c.rows, 8, 128)
+    want = c.attend(q, causal=causal)
+    for window in (2 ** 31 - 1, 2 ** 31 - 2, 2 ** 30):
+        out = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.full_like(q, 7.0, device=DEV), causal=causal, window=window)
+        c.check(out, want, str(window))
+    assert causal or bool((want[0][0] != 0).all())           # the first row, far in front of the first token, sees all of them
