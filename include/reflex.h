@@ -367,6 +367,7 @@ typedef struct {
  * The kernels check what they follow: a table entry outside [0, n_pages) or a position outside [0, max_pages * page) is never
  * dereferenced. What such a token would have written is left out, what would have been read through it (the row read back; every row of
  * the sequence's attention that sees it, and maybe rows of the sequence beside them) is NaN, and reflex_pages_check_status names the sequence.
+ * Entries of pages that no new token sees (in front of their windows) may be anything.
  * A table spans at most 2^30 positions. */
 typedef struct {
     const int32_t *table; /* device [B][max_pages]                          */

@@ -41,7 +41,7 @@ constexpr float kChunkGrow = 8.0f;             // log2 units: O is rescaled only
 
 // A unit costs SET_UP blocks before its first tile: what its Q, its masks and its results take, in tiles. (A share that ends among them
 // leaves the unit to the next pair.)
-struct ChunkSpan { int tile0, tiles, hi, count; };    // key tiles [tile0, tile0 + tiles), keys below hi; blocks
+struct ChunkSpan { int tile0, tiles, lo, hi, count; };    // key tiles [tile0, tile0 + tiles), keys [lo, hi); blocks
 template <int SET_UP>
 struct ChunkSpanOf {
     const PageAttention &p;
@@ -52,7 +52,7 @@ struct ChunkSpanOf {
         const PageRange r = page_range(s, p, tile * tokens, min(s.n, (tile + 1) * tokens) - 1);
         ChunkSpan c;
         c.tile0 = r.lo / kChunkKeys;
-        c.hi = r.hi;
+        c.lo = r.lo; c.hi = r.hi;
         c.tiles = r.hi > r.lo ? (r.hi + kChunkKeys - 1) / kChunkKeys - c.tile0 : 0;
         c.count = SET_UP + max(1, c.tiles);
         return c;
@@ -63,9 +63,9 @@ struct ChunkSpanOf {
 struct ChunkUnit {
     int b, row0, n_rows, len;      // the sequence
     int token, h;                  // first token of the pair's rows, KV head
-    int t0, n, hi;                 // keys below hi
+    int t0, n, lo, hi;             // keys [lo, hi) of these tiles: no row sees others
     int slot;                      // of its partial result, -1: the whole unit is the pair's
-    int unused[6];
+    int unused[5];
 };
 static_assert(sizeof(ChunkUnit) == 64, "list of units");
 
@@ -193,7 +193,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     auto unit_ready = [&](int i) -> bool { return all(wait(L::UFULL + i % L::NU, (uint32_t)(i / L::NU) & 1u, 1)); };      // the i-th of the list may be read
 
     // the tiles of the share as one sequence: number g, tile jj of unit number i of the list, ui of those that have keys
-    struct Cursor { int b, h, t0, n, hi, q_row, jj, g, ui, i; bool valid; };
+    struct Cursor { int b, h, t0, n, lo, hi, q_row, jj, g, ui, i; bool valid; };
     auto settle = [&](Cursor &c) {          // the i-th unit, or the first one behind it with a tile
         for (;; ++c.i) {
             c.valid = unit_ready(c.i);
@@ -202,7 +202,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             c.n = u.n;
             if (c.n != 0) {
                 c.valid = c.n > 0;
-                c.b = u.b; c.h = u.h; c.t0 = u.t0; c.hi = u.hi;
+                c.b = u.b; c.h = u.h; c.t0 = u.t0; c.lo = u.lo; c.hi = u.hi;
                 c.q_row = u.row0 + u.token + (int)rank * tile_tokens;
                 c.jj = 0;
                 return;
@@ -210,7 +210,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
     };
     auto begin = [&]() -> Cursor {
-        Cursor c = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, false};
+        Cursor c = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, false};
         settle(c);
         return c;
     };
@@ -219,7 +219,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         if (++c.jj == c.n) { ++c.ui; ++c.i; settle(c); }
     };
     // Where a warp's tile of keys lies, box by box: lane i has the row of box i in the layer's pages (0 where it holds no key below the unit's
-    // last, or where the table is wrong: `bad`). It is looked up a tile ahead, since a table entry takes some 500 cycles to come.
+    // last, or where the table is wrong: `bad`, if one of its keys can be seen; pages in front of all windows may be gone). It is looked up a tile ahead, since a table entry takes some 500 cycles to come.
     const int per_half = 64 / box;               // boxes of 64 keys
     auto boxes = [&](int key0, int hi) -> int { return (min(max(hi - key0, 0), 64) + box - 1) / box; };
     auto look_up = [&](const Cursor &c, bool &bad) -> int {
@@ -227,8 +227,8 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         bad = false;
         if (!c.valid || lane >= 2 * per_half || key >= c.hi) return 0;
         const int page = page_at(p.q, p.g.n_pages, c.b, key >> p.g.log_p);
-        bad = page < 0;
-        return bad ? 0 : (int)page_row(p.g, page, c.h) + (key & (p.g.P - 1));
+        bad = page < 0 && key + box > c.lo;
+        return page < 0 ? 0 : (int)page_row(p.g, page, c.h) + (key & (p.g.P - 1));
     };
 
     if (warp == 0) {
@@ -238,7 +238,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         ChunkUnit *list = reinterpret_cast<ChunkUnit *>(smem + L::OFF_UNITS);
         if (lane == 0 && rank == 0) part.meta[pair].b = -1;
         bool bad, ok = true;
-        Cursor c = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, false};
+        Cursor c = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, false};
         int x = x0;
         auto publish = [&](const ChunkUnit &u) {
             if (c.i >= L::NU) ok = ok && all(wait(L::UEMPTY + c.i % L::NU, (uint32_t)(c.i / L::NU - 1) & 1u, 13));
@@ -255,15 +255,15 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 const int k0 = max(0, x - place.at - L::SET_UP), k1 = max(0, to - place.at - L::SET_UP);
                 if (k1 > 0) {
                     const bool whole = k0 == 0 && k1 == place.cost - L::SET_UP;
-                    const ChunkUnit u = {place.s.b, place.s.row0, place.s.n, place.s.len, place.tile * 2 * tile_tokens, place.h, place.sp.tile0 + k0, max(0, min(k1, place.sp.tiles) - k0), place.sp.hi,
-                                         whole ? -1 : 2 * pair + (k0 == 0 ? 1 : 0), {0, 0, 0, 0, 0, 0}};
+                    const ChunkUnit u = {place.s.b, place.s.row0, place.s.n, place.s.len, place.tile * 2 * tile_tokens, place.h, place.sp.tile0 + k0, max(0, min(k1, place.sp.tiles) - k0), place.sp.lo, place.sp.hi,
+                                         whole ? -1 : 2 * pair + (k0 == 0 ? 1 : 0), {0, 0, 0, 0, 0}};
                     publish(u);
                     if (k0 == 0 && !whole && rank == 0 && lane == 0) {
                         const int first = u.token * G;
                         const PageSplit m = {u.b, u.row0, first, min(2 * tile_tokens * G, u.n_rows * G - first), u.h, shares.owner(place.at + place.cost - 1), tile_tokens * G, 0};
                         part.meta[pair] = m;
                     }
-                    c.b = u.b; c.h = u.h; c.t0 = u.t0; c.n = u.n; c.hi = u.hi;
+                    c.b = u.b; c.h = u.h; c.t0 = u.t0; c.n = u.n; c.lo = u.lo; c.hi = u.hi;
                     c.q_row = u.row0 + u.token + (int)rank * tile_tokens;
                     c.jj = 0;
                     c.valid = u.n > 0 && ok;
@@ -272,7 +272,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 if (x < x1) line.next(place);
                 if (c.valid) return;
             }
-            const ChunkUnit none = {0, 0, 0, 0, 0, 0, 0, -1, 0, -1, {0, 0, 0, 0, 0, 0}};
+            const ChunkUnit none = {0, 0, 0, 0, 0, 0, 0, -1, 0, 0, -1, {0, 0, 0, 0, 0}};
             publish(none);
         };
         next_unit();
@@ -452,7 +452,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         if (NG == 2 && group == 1) asm volatile("bar.arrive %0, 128;" ::"r"(1 + quarter) : "memory");
         for (int ul = 0; unit_ready(ul); ++ul) {
             const ChunkUnit &u = units[ul % L::NU];
-            const int n = u.n, t0 = u.t0, hi = u.hi;
+            const int n = u.n, t0 = u.t0, lo = u.lo, hi = u.hi;
             if (n < 0) break;
             auto leave = [&] {                     // this warp is done with the list's entry
                 __syncwarp();
@@ -553,11 +553,11 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 }
                 if (masked) {
                     ok = ok && wait(L::VLAND + st, vph, 9);
-                    // Keys behind the last one count as zeros in V (a weight of 0 does not make a stale NaN one); a key that only some rows see must be
+                    // Keys that no row sees count as zeros in V (a weight of 0 does not make a stale NaN one); a key that only some rows see must be
                     // finite, or the sequence is done again row by row. The 128 threads of a half share its 64 keys: half of this CTA's columns each.
                     const int key = key0 + (row & 63);
                     uint4 *v0 = reinterpret_cast<uint4 *>(smem + L::OFF_V + st * L::V_STAGE + (half * 64 + (row & 63)) * 128) + (row >> 6) * 4;
-                    if (key >= hi) {
+                    if (key < lo || key >= hi) {
 #pragma unroll 1
                         for (int c = 0; c < 4 * VCH; ++c) v0[(c >> 2) * (128 * 128 / 16) + ((c + row) & 3)] = make_uint4(0, 0, 0, 0);
                     } else if ((key < all_lo || key >= all_hi) && (D == HD || rank == 0)) {

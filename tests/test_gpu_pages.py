@@ -671,3 +671,28 @@ def test_the_largest_window(dtype, fmt, lens, news, causal):
         out = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.full_like(q, 7.0, device=DEV), causal=causal, window=window)
         c.check(out, want, str(window))
     assert causal or bool((want[0][0] != 0).all())           # the first row, far in front of the first token, sees all of them
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (BF16, 256), (F32, 64)])
+@pytest.mark.parametrize("news", [[1, 1, 1], [40, 70, 33]])
+@pytest.mark.parametrize("page,gone", [(16, -1), (64, 10 ** 6)])
+def test_pages_in_front_of_the_window_may_be_gone(fmt, dtype, d, news, page, gone):
+    """A sequence keeps the pages that its window reaches. The table's entries of the others, and rows that are not finite in front of the window, change nothing."""
+    lens, window = [700, 333, 1090], 100
+    c = Paged(lens, news, page, 4, 1, d, dtype, fmt, seed=d + news[0])
+    total = sum(lens)
+    k, v = c.normal(total, 1, d, std=1.5), c.normal(total, 1, d)
+    table, at = c.table.clone(), 0
+    for b, (n, m) in enumerate(zip(lens, news)):
+        first = max(0, n - m - window + 1)                 # that the first new token sees
+        k[at + first - 1], v[at + first - 1] = math.nan, math.inf
+        table[b, :first // page] = gone
+        at += n
+    c.write_all(k=k, v=v)
+    q = c.normal(c.rows, 4, d)
+    batch = rb.PageBatch(table.to(DEV), c.batch.cu, c.batch.length)
+    for causal in (True, False):
+        out = rb.reflex_pages_attention(c.pages, 0, batch, q.to(DEV), torch.full_like(q, 7.0, device=DEV), causal=causal, window=window)
+        c.check(out, c.attend(q, causal=causal, window=window), f"causal {causal}")
+        rb.reflex_pages_check_status(c.pages)
