@@ -59,6 +59,7 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
     const int e0 = turns && !adj ? lane * 8 : lane * 16, e1 = turns && !adj ? lane * 8 + R / 2 : lane * 16 + 8;
     TurnRate rate[TURNS ? 8 : 1];
     uint32_t axes = 0;              // four bits each
+    uint32_t still = 0;             // pairs that do not turn (see rotary_axes_kernel)
     if (TURNS && turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -66,6 +67,7 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
             rate[TURNS ? i : 0] = turn_rate(r.rot.freq[lane * 8 + i]);
             if (axis >= r.rot.axes) rate[TURNS ? i : 0].lo = rate[TURNS ? i : 0].hi = 0u;
             else axes |= (uint32_t)axis << (4 * i);
+            if ((rate[TURNS ? i : 0].lo | rate[TURNS ? i : 0].hi) == 0u) still |= 1u << i;
         }
     }
     __syncthreads();
@@ -117,16 +119,26 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
                         w[i] = u0 * s[i] + w0 * c[i];
                     }
                 }
+                if (FMT != REFLEX_PAGE_SAME && still) {
+                    Raw8<float> u0, w0, u1 = narrow8<float>(u), w1 = narrow8<float>(w);
+                    float f[8];
+                    widen8(ka, f); u0 = narrow8<float>(f);
+                    widen8(kb, f); w0 = narrow8<float>(f);
+                    if (adj) keep_pairs<float, true>(still, u0, w0, u1, w1); else keep_pairs<float, false>(still, u0, w0, u1, w1);
+                    widen8(u1, u); widen8(w1, w);
+                }
             }
             if constexpr (FMT == REFLEX_PAGE_SAME) {
                 if (live) {
                     T *kd = (T *)g.k + row * g.d, *vd = (T *)g.v + row * g.d;
-                    if (TURNS) { store8(kd + e0, u); store8(kd + e1, w); }
-                    else
-#pragma unroll
-                        for (int i = 0; i < (int)sizeof(T) / 2; ++i) { reinterpret_cast<uint4 *>(kd + e0)[i] = ka.w[i]; reinterpret_cast<uint4 *>(kd + e1)[i] = kb.w[i]; }
-#pragma unroll
-                    for (int i = 0; i < (int)sizeof(T) / 2; ++i) { reinterpret_cast<uint4 *>(vd + e0)[i] = va.w[i]; reinterpret_cast<uint4 *>(vd + e1)[i] = vb.w[i]; }
+                    Raw8<T> ya = ka, yb = kb;
+                    if (TURNS && turns) {
+                        ya = narrow8<T>(u);
+                        yb = narrow8<T>(w);
+                        if (still) { if (adj) keep_pairs<T, true>(still, ka, kb, ya, yb); else keep_pairs<T, false>(still, ka, kb, ya, yb); }
+                    }
+                    put8(kd + e0, ya); put8(kd + e1, yb);
+                    put8(vd + e0, va); put8(vd + e1, vb);
                 }
             } else {
                 uint32_t top;

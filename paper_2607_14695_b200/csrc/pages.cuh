@@ -173,6 +173,46 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
+template <typename T>
+__device__ __forceinline__ Raw8<T> narrow8(const float *f)
+{
+    Raw8<T> r;
+    if constexpr (sizeof(T) == 2) r.w[0] = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    else {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+            r.w[i] = make_uint4(__float_as_uint(f[4 * i]), __float_as_uint(f[4 * i + 1]), __float_as_uint(f[4 * i + 2]), __float_as_uint(f[4 * i + 3]));
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void put8(T *p, const Raw8<T> &r)
+{
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4 *>(p)[i] = r.w[i];
+}
+// The marked ones of eight pairs, elements i of both chunks (or 2i and 2i + 1 of the two in a row), as they were: to the bit
+template <typename T, bool ADJ>
+__device__ __forceinline__ void keep_pairs(uint32_t marked, const Raw8<T> &a0, const Raw8<T> &b0, Raw8<T> &a, Raw8<T> &b)
+{
+    constexpr int PER = 4 / (int)sizeof(T);              // elements of a word
+    auto chunk = [&](const Raw8<T> &was, Raw8<T> &is, int second) {
+#pragma unroll
+        for (int i = 0; i < 8 / PER; ++i) {
+            const uint4 &w = was.w[i >> 2];
+            uint4 &y = is.w[i >> 2];
+            const uint32_t old = (i & 3) == 0 ? w.x : (i & 3) == 1 ? w.y : (i & 3) == 2 ? w.z : w.w;
+            uint32_t &now = (i & 3) == 0 ? y.x : (i & 3) == 1 ? y.y : (i & 3) == 2 ? y.z : y.w;
+            uint32_t mask = 0;
+#pragma unroll
+            for (int e = 0; e < PER; ++e)
+                if (marked & (1u << (ADJ ? 4 * second + (i * PER + e) / 2 : i * PER + e))) mask |= PER == 2 ? 0xffffu << (16 * e) : 0xffffffffu;
+            now = (now & ~mask) | (old & mask);
+        }
+    };
+    chunk(a0, a, 0);
+    chunk(b0, b, 1);
+}
 __device__ __forceinline__ void store8(__nv_bfloat16 *p, const float *f)
 {
     *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));

@@ -25,6 +25,7 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
     const int e0 = turns && !ADJ ? slot * 8 : slot * 16, e1 = turns && !ADJ ? slot * 8 + R / 2 : slot * 16 + 8;
     TurnRate rate[8];
     uint32_t axes = 0;              // four bits each
+    uint32_t still = 0;             // pairs that do not turn: 0 times an infinity of the other element is not to be added to them
     if (turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -32,6 +33,7 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
             rate[i] = turn_rate(r.rot.freq[slot * 8 + i]);
             if (axis >= r.rot.axes) rate[i].lo = rate[i].hi = 0u;
             else axes |= (uint32_t)axis << (4 * i);
+            if ((rate[i].lo | rate[i].hi) == 0u) still |= 1u << i;
         }
     }
     const int h0 = blockIdx.y * heads_per_thread, h1 = min(H, h0 + heads_per_thread);
@@ -55,10 +57,11 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
                 if (h + k >= h1) break;
-                float u[8], v[8];
-                widen8(a[k], u);
-                widen8(b[k], v);
+                Raw8<T> ya = a[k], yb = b[k];
                 if (turns) {
+                    float u[8], v[8];
+                    widen8(a[k], u);
+                    widen8(b[k], v);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         // (adjacent: pair i is elements 2i, 2i + 1 of the 16)
@@ -68,9 +71,12 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
                         p0 = u0 * c[i] - v0 * s[i];
                         p1 = u0 * s[i] + v0 * c[i];
                     }
+                    ya = narrow8<T>(u);
+                    yb = narrow8<T>(v);
+                    if (still) keep_pairs<T, ADJ>(still, a[k], b[k], ya, yb);
                 }
-                store8(yr + (size_t)(h + k) * d + e0, u);
-                store8(yr + (size_t)(h + k) * d + e1, v);
+                put8(yr + (size_t)(h + k) * d + e0, ya);
+                put8(yr + (size_t)(h + k) * d + e1, yb);
             }
         }
     }

@@ -696,3 +696,28 @@ def test_pages_in_front_of_the_window_may_be_gone(fmt, dtype, d, news, page, gon
         out = rb.reflex_pages_attention(c.pages, 0, batch, q.to(DEV), torch.full_like(q, 7.0, device=DEV), causal=causal, window=window)
         c.check(out, c.attend(q, causal=causal, window=window), f"causal {causal}")
         rb.reflex_pages_check_status(c.pages)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_pairs_that_do_not_turn_stay_as_they_are(dtype, adjacent):
+    """Frequency 0, or an axis without positions: to the bit, whatever lies in the pair's other element (infinities, NaN, -0)."""
+    n, H, d, R = 6, 3, 64, 48
+    g = torch.Generator().manual_seed(1)
+    x = torch.randn(n, H, d, generator=g).to(dtype)
+    odd = torch.tensor([math.inf, -math.inf, math.nan, -0.0, 0.0])
+    at = torch.randint(0, n * H * d, (n * H * 12,), generator=g)
+    x.view(-1)[at] = odd[torch.arange(len(at)) % 5].to(dtype)
+    rot = _rot(R, 3, adjacent)
+    rot.freq[::5] = 0.0                                                       # pairs 0, 5, 10 ...
+    pos = torch.randint(1, 3000, (2, n), generator=g, dtype=torch.int32)      # no positions of axis 2
+    still = (rot.freq == 0).cpu() | (rot.axis >= 2).cpu()
+    columns = torch.cat([still.repeat_interleave(2) if adjacent else still.repeat(2), torch.ones(d - R, dtype=torch.bool)])
+    bits = lambda t: t.contiguous().view(torch.int16 if dtype == BF16 else torch.int32)        # noqa: E731
+    y = rb.reflex_rotary_axes(x.to(DEV), torch.empty((n, H, d), dtype=dtype, device=DEV), pos.to(DEV), rot).cpu()
+    assert torch.equal(bits(y[..., columns]), bits(x[..., columns]))
+    c = Paged([n], [n], 16, H, H, d, dtype, rb.PAGE_SAME)
+    rb.reflex_pages_write(c.pages, 0, c.batch, x.to(DEV), x.to(DEV), rotary=rot, pos=pos.to(DEV))
+    k, v = _read(c)
+    assert torch.equal(bits(k[0, 0][..., columns]), bits(x[..., columns])) and torch.equal(bits(v[0, 0]), bits(x))
+    assert _same(k[0, 0], y)                                                  # both turn alike
