@@ -380,7 +380,7 @@ typedef struct {
  * pos[axis[i]][token] * freq[i] (radians; freq 0: not at all). Pairs are elements (i, i + R / 2), or (2i, 2i + 1) where adjacent;
  * elements from R on are left as they are. */
 typedef struct {
-    const float *freq;   /* device [R / 2]                                              */
+    const float *freq;   /* device [R / 2]; magnitudes below 2^40: other pairs come out NaN */
     const uint8_t *axis; /* device [R / 2]; an axis >= axes does not turn its pair       */
     int32_t R;           /* a multiple of 16, at most d                                 */
     int32_t axes;        /* 1 .. 8                                                      */

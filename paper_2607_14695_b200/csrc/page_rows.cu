@@ -59,7 +59,7 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
     const int e0 = turns && !adj ? lane * 8 : lane * 16, e1 = turns && !adj ? lane * 8 + R / 2 : lane * 16 + 8;
     TurnRate rate[TURNS ? 8 : 1];
     uint32_t axes = 0;              // four bits each
-    uint32_t still = 0;             // pairs that do not turn (see rotary_axes_kernel)
+    uint32_t still = 0, unknown = 0;          // pairs that do not turn, that have no angle (see rotary_axes_kernel)
     if (TURNS && turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -68,6 +68,7 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
             if (axis >= r.rot.axes) rate[TURNS ? i : 0].lo = rate[TURNS ? i : 0].hi = 0u;
             else axes |= (uint32_t)axis << (4 * i);
             if ((rate[TURNS ? i : 0].lo | rate[TURNS ? i : 0].hi) == 0u) still |= 1u << i;
+            else if (!turnable(r.rot.freq[lane * 8 + i])) unknown |= 1u << i;
         }
     }
     __syncthreads();
@@ -90,7 +91,10 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
             if (h == h0 && exists) {            // (while the first rows are on their way)
                 if (TURNS && turns) {
 #pragma unroll
-                    for (int i = 0; i < (TURNS ? 8 : 1); ++i) turn(rate[i], r.pos[(size_t)((axes >> (4 * i)) & 15u) * n_rows + t], s[i], c[i]);
+                    for (int i = 0; i < (TURNS ? 8 : 1); ++i) {
+                        turn(rate[i], r.pos[(size_t)((axes >> (4 * i)) & 15u) * n_rows + t], s[i], c[i]);
+                        if (unknown & (1u << i)) s[i] = c[i] = __int_as_float(0x7fc00000);
+                    }
                 }
                 const int b = find_seq(cu_s, q.B, (int)t);
                 const int64_t at = (int64_t)q.len[b] - cu_s[b + 1] + t;

@@ -125,11 +125,15 @@ template <int FMT> __device__ __forceinline__ float exponent_f32(int e) { return
 // ---- rotation angles ----
 // A pair's frequency in revolutions per position, modulo 1, as a 64-bit fraction: position times fraction, modulo 2^64, is the fraction of a
 // revolution that the position turns by, for any 32-bit position and with no rounding. Its upper 32 bits are a quarter of fp32's spacing near 1.
+// (That is as far as 1 / (2 pi) in two doubles goes: from 2^40 on an angle would lose bits, and the fraction of NaN or an infinity is none. `turnable` says so;
+// such a pair comes out NaN. What rate they have does not matter, but it is not 0.)
 struct TurnRate { uint32_t lo, hi; };
+__device__ __forceinline__ bool turnable(float freq) { return fabsf(freq) < 0x1p40f; }
 __device__ __forceinline__ TurnRate turn_rate(float freq)
 {
     // 1 / (2 pi) to twice the precision of a double
     const double c0 = 0x1.45f306dc9c883p-3, c1 = -0x1.6b01ec5417056p-57;
+    if (!turnable(freq)) return {1u, 0u};
     const double f = (double)freq, r0 = f * c0, r1 = fma(f, c0, -r0) + f * c1;
     const double whole = floor(r0), frac = r0 - whole;                     // exact
     const unsigned long long u = __double2ull_rd(frac * 0x1p64) + (unsigned long long)__double2ll_rn(r1 * 0x1p64);

@@ -26,6 +26,7 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
     TurnRate rate[8];
     uint32_t axes = 0;              // four bits each
     uint32_t still = 0;             // pairs that do not turn: 0 times an infinity of the other element is not to be added to them
+    uint32_t unknown = 0;           // pairs without an angle
     if (turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -34,6 +35,7 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
             if (axis >= r.rot.axes) rate[i].lo = rate[i].hi = 0u;
             else axes |= (uint32_t)axis << (4 * i);
             if ((rate[i].lo | rate[i].hi) == 0u) still |= 1u << i;
+            else if (!turnable(r.rot.freq[slot * 8 + i])) unknown |= 1u << i;
         }
     }
     const int h0 = blockIdx.y * heads_per_thread, h1 = min(H, h0 + heads_per_thread);
@@ -52,6 +54,7 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
                 for (int i = 0; i < 8; ++i) {
                     turn(rate[i], r.pos[(size_t)((axes >> (4 * i)) & 15u) * n + t], s[i], c[i]);
                     if (r.inverse) s[i] = -s[i];
+                    if (unknown & (1u << i)) s[i] = c[i] = __int_as_float(0x7fc00000);
                 }
             }
 #pragma unroll

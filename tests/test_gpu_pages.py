@@ -721,3 +721,29 @@ def test_pairs_that_do_not_turn_stay_as_they_are(dtype, adjacent):
     k, v = _read(c)
     assert torch.equal(bits(k[0, 0][..., columns]), bits(x[..., columns])) and torch.equal(bits(v[0, 0]), bits(x))
     assert _same(k[0, 0], y)                                                  # both turn alike
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_frequencies_without_an_angle(dtype, adjacent):
+    """NaN, infinities and what no angle is kept for make their pairs NaN, and no others (an axis without positions: not turned, whatever its frequency)."""
+    n, d, R = 5, 64, 32
+    x = torch.randn(n, 2, d).to(dtype)
+    rot = _rot(R, 3, adjacent)
+    odd = {0: math.nan, 3: math.inf, 6: -math.inf, 9: 2.0 ** 40, 12: -3e38, 2: math.nan, 5: math.inf}           # pairs 2 and 5: axis 2
+    for i, f in odd.items():
+        rot.freq[i] = f
+    rot.freq[7], rot.freq[10] = 1.5 * 2 ** 20, -(2.0 ** 24) + 1
+    pos = torch.randint(-3000, 3000, (2, n), dtype=torch.int32)
+    pos[:, 0] = 0
+    lost = torch.tensor([i in odd and i % 3 < 2 for i in range(R // 2)])
+    lost = torch.cat([lost.repeat_interleave(2) if adjacent else lost.repeat(2), torch.zeros(d - R, dtype=torch.bool)])
+    freq = torch.where(torch.isfinite(rot.freq) & (rot.freq.abs() < 2.0 ** 40), rot.freq, 0.0).cpu()
+    want = U.rotated(x, pos, freq, rot.axis.cpu(), adjacent)
+    # (angles of 2^24 * 3000 in 64 bits lose 2^-53 of themselves in the reference: 2^-17 of a radian)
+    lim = HALF[dtype] * want.abs() + x.double().abs().amax(-1, keepdim=True) * 2 * (2.0 ** -17 + 2.0 ** -20)
+    y = rb.reflex_rotary_axes(x.to(DEV), torch.empty((n, 2, d), dtype=dtype, device=DEV), pos.to(DEV), rot).cpu()
+    assert torch.isnan(y[..., lost]).all() and ((y.double() - want).abs() <= lim)[..., ~lost].all()
+    c = Paged([n], [n], 16, 2, 2, d, dtype, rb.PAGE_SAME)
+    rb.reflex_pages_write(c.pages, 0, c.batch, x.to(DEV), x.to(DEV), rotary=rot, pos=pos.to(DEV))
+    assert _same(_read(c)[0][0, 0], y)
