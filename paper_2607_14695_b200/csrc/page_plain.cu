@@ -45,11 +45,10 @@ page_plain_kernel(const PageAttention p)
         for (int i = 0; i < 8; ++i) all.acc[i] = 0.f;
 #pragma unroll 4
         for (int q = 0; q < kSplitWarps; ++q) {
-            float f = expf(m_s[q] - mr);
-            if (f == 0.f && m_s[q] > -INFINITY) f = 1.2e-38f;       // (an infinity among the values stays one)
+            const float f = expf(m_s[q] - mr);
             all.l = fmaf(l_s[q], f, all.l);
             all.bad |= bad_s[q] != 0;
-            if (f == 0.f) continue;
+            if (m_s[q] == -INFINITY) continue;       // (nothing was seen: nothing there is looked at)
 #pragma unroll
             for (int i = 0; i < 8; ++i) all.acc[i] = fmaf(acc_s[q][lane + 32 * i], f, all.acc[i]);
         }

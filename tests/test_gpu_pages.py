@@ -747,3 +747,28 @@ def test_frequencies_without_an_angle(dtype, adjacent):
     c = Paged([n], [n], 16, 2, 2, d, dtype, rb.PAGE_SAME)
     rb.reflex_pages_write(c.pages, 0, c.batch, x.to(DEV), x.to(DEV), rotary=rot, pos=pos.to(DEV))
     assert _same(_read(c)[0][0, 0], y)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("news,at", [(1, 5), (1, 4950), (40, 5), (40, 4950)])
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_large_values_whose_weight_underflows(dtype, fmt, news, at):
+    """A value of 1e38 of a key that another one outweighs by 2^300 adds nothing, wherever in the sequence it is and whoever joins the parts (40 rows: dozens of them)."""
+    n, d = 5000, 128
+    c = Paged([n], [news], 64, 4, 1, d, dtype, fmt)
+    k, v = torch.zeros(n, 1, d, dtype=dtype), c.normal(n, 1, d)
+    k[:, 0, 0] = -1.0
+    k[2500, 0, 0] = 1.0
+    v[at, 0, 3::5] = 1e38
+    c.write_all(k=k, v=v)
+    q = torch.zeros(news, 4, d, dtype=dtype)
+    q[..., 0] = 104.0 * d ** 0.5                     # logits -104, and 104 of the one key: e^208 = 2^300
+    out = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.zeros_like(q, device=DEV))
+    one = c.attend(q[:1].expand(news, -1, -1)) if news == 1 else None
+    if one is None:                                  # (all rows are alike)
+        c.news, c.cu, c.rows = [1], torch.tensor([0, 1], dtype=torch.int32), 1
+        one = c.attend(q[:1])
+        for i in range(news):
+            c.check(out[i:i + 1], one, f"row {i}")
+    else:
+        c.check(out, one)
