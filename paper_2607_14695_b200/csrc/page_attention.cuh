@@ -7,6 +7,11 @@ namespace reflex {
 
 __device__ __forceinline__ void report_page_wait(uint32_t *status, uint32_t code) { atomicCAS(status, 0u, status_word(kSitePages + code)); }
 
+// Weights are 2^-24 of what the softmax has them, in sums and in products alike, so that it goes with the division: O is a sum over the keys of weights, which reach 2^8 between
+// two changes of the reference, times values, which reach 2^127 and more, and is not to pass fp32 ahead of the division (nor a weight times a value's 2^e bf16). That holds
+// for 2^15 such keys. Down below, values of 2^-100 are still normal numbers as products.
+constexpr float kWeightShift = 24.f;
+
 struct PageSeq { int b, row0, n, len; };      // first row of its new tokens, how many, tokens in all
 
 // (whatever the device arrays hold, rows stay inside [0, n_rows))

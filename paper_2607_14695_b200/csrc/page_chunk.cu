@@ -573,7 +573,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                     }
                     fence_proxy_async_smem();
                 }
-                const float mr = m_ref == -INFINITY ? 0.f : m_ref * sc;
+                const float mr = m_ref == -INFINITY ? 0.f : m_ref * sc + kWeightShift;
                 const uint64_t sc2 = pack_f32x2(sc, sc), nm2 = pack_f32x2(-mr, -mr);
                 uint64_t sum2[2] = {0ull, 0ull};
                 auto weights = [&](uint32_t (&v)[32], int c) {

@@ -54,6 +54,8 @@ template <typename T, int FMT, int COLS>
 __device__ __forceinline__ void page_plain_sum(const PageAttention &p, int b, int row, int64_t pos, int len, int hq, int first, int step, PlainSum &a)
 {
     const PageGeom &g = p.g;
+    constexpr float kShare = 0x1p-24f;
+    static_assert(kWeightShift == 24.f, "2^-kWeightShift");
     const int lane = threadIdx.x & 31, h = hq / (g.Hq / g.Hkv);
     const int64_t cap = (int64_t)p.q.max_pages << g.log_p;          // (of positions past the table the first one is looked at)
     const int64_t hi = min(p.causal ? min((int64_t)len, pos + 1) : (int64_t)len, cap + 1);
@@ -110,7 +112,7 @@ __device__ __forceinline__ void page_plain_sum(const PageAttention &p, int b, in
         }
         const float m_new = !(top <= a.m) ? top : a.m;
         const float mr = m_new == -INFINITY ? 0.f : m_new;
-        const float alpha = expf(a.m - mr), w = page >= 0 ? expf(s - mr) : 0.f, wv = w * vs;
+        const float alpha = expf(a.m - mr), w = page >= 0 ? expf(s - mr) * kShare : 0.f, wv = w * vs;
         a.m = m_new;
         a.l = a.l * alpha + w;
 #pragma unroll

@@ -394,7 +394,7 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float x2 = w[nt][e], mr = m[2 * nt + (e & 1)];
-                    const float pe = ex2(x2 - (mr == -INFINITY ? 0.f : mr));
+                    const float pe = ex2(x2 - (mr == -INFINITY ? 0.f : mr + kWeightShift));
                     l[2 * nt + (e & 1)] += pe;
                     v[e] = !whole && x2 == -INFINITY ? 0.f : C::BYTES ? pe * (e < 2 ? vs0 : vs1) : pe;
                 }

@@ -772,3 +772,22 @@ def test_large_values_whose_weight_underflows(dtype, fmt, news, at):
             c.check(out[i:i + 1], one, f"row {i}")
     else:
         c.check(out, one)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 64), (BF16, 128), (BF16, 256), (F32, 64)])
+@pytest.mark.parametrize("news", [1, 40])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("size", [2.0 ** 127, 1e-26])
+def test_values_of_any_size(dtype, d, news, fmt, size):
+    """Values of half to all of 2^127, all of one sign, and of 1e-26, under logits that rise by almost 2^8 behind the first keys: their weighted sum is finite ahead of the division,
+    and as exact as any other."""
+    n = 1500
+    c = Paged([n, 300], [news, 1], 32, 4, 1, d, dtype, fmt, seed=d)
+    k, v = torch.zeros(n + 300, 1, d, dtype=dtype), ((0.5 + 0.5 * torch.rand(n + 300, 1, d, generator=c.g)) * size).to(dtype)
+    v[:, :, 1::2] *= -1.0
+    k[150:, :, 0] = 1.0
+    c.write_all(k=k, v=v)
+    q = c.normal(c.rows, 4, d)
+    q[..., 0] = 5.4 * d ** 0.5                       # logits 0, then 5.4 = 7.8 log2 units
+    out = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.zeros_like(q, device=DEV), causal=True)
+    c.check(out, c.attend(q, causal=True))
