@@ -263,9 +263,8 @@ cudaError_t launch_page_write(const PageGeom &g, const reflex_page_batch &q, con
                               const PageRotation &r, int dtype, int format, cudaStream_t st)
 {
     const int tpr = g.d / 16, per_block = kRowThreads / tpr;
-    const int blocks = (n_rows + per_block - 1) / per_block;
-    int hpt = (int)((long long)blocks * g.Hkv / (148 * 8));
-    hpt = hpt < 1 ? 1 : hpt > g.Hkv ? g.Hkv : hpt;
+    const long long blocks = ((long long)n_rows + per_block - 1) / per_block, share = blocks * g.Hkv / (148 * 8);
+    const int hpt = share < 1 ? 1 : share > g.Hkv ? g.Hkv : (int)share;
     const int groups = (g.Hkv + hpt - 1) / hpt;
     const int most = (148 * 16 + groups - 1) / groups;
     const dim3 grid((unsigned)(blocks > most ? most : blocks), (unsigned)groups);

@@ -89,14 +89,12 @@ cudaError_t launch_rotary_axes(const void *x, int64_t ldx, void *y, int64_t ldy,
 {
     const int per_block = kRotThreads / (d / 16);
     // heads of a token go to one thread once there are threads enough without them
-    const long long rows = (long long)((n + per_block - 1) / per_block) * H;
-    int hpt = (int)(rows / (148 * 2));
-    hpt = hpt < 1 ? 1 : hpt > H ? H : hpt;
+    const long long blocks = ((long long)n + per_block - 1) / per_block, rows = blocks * H;
+    const long long share = rows / (148 * 2);
+    const int hpt = share < 1 ? 1 : share > H ? H : (int)share;
     const int groups = (H + hpt - 1) / hpt;
-    int gx = (n + per_block - 1) / per_block;
     const int most = (148 * 8 + groups - 1) / groups;
-    if (gx > most) gx = most;
-    const dim3 grid((unsigned)gx, (unsigned)groups);
+    const dim3 grid((unsigned)(blocks > most ? most : blocks), (unsigned)groups);
     count_launch();
     auto go = [&](auto zero, auto adj) {
         using T = decltype(zero);

@@ -791,3 +791,22 @@ def test_values_of_any_size(dtype, d, news, fmt, size):
     q[..., 0] = 5.4 * d ** 0.5                       # logits 0, then 5.4 = 7.8 log2 units
     out = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.zeros_like(q, device=DEV), causal=True)
     c.check(out, c.attend(q, causal=True))
+
+
+def test_rotary_of_as_many_tokens_as_there_can_be():
+    """2^31 - 1 tokens, in place (69 GB of rows): counts of tokens do not pass 32 bits on the way to the launch."""
+    n, d = 2 ** 31 - 1, 16
+    if torch.cuda.mem_get_info()[0] < 100 << 30:
+        pytest.skip("rows and positions take 77 GB")
+    x, pos = torch.zeros((n, 1, d), dtype=BF16, device=DEV), torch.zeros((1, n), dtype=torch.int32, device=DEV)
+    at = [0, 1, 2 ** 30, n - 257, n - 1]
+    for i in at:
+        x[i, 0], pos[0, i] = 1.0, i
+    rot = _rot(d, 1)
+    rb.reflex_rotary_axes(x, x, pos, rot)
+    for i in at:
+        want = U.rotated(torch.ones(1, 1, d), torch.tensor([[i]]), rot.freq.cpu(), rot.axis.cpu())
+        # (angles of 2^31 in 64 bits: 2^-22; products and sum; half a step of the result)
+        assert ((x[i, 0].cpu().double() - want[0, 0]).abs() <= HALF[BF16] * want[0, 0].abs() + 2 * (2.0 ** -22 + 2.0 ** -20)).all(), i
+    del x, pos
+    torch.cuda.empty_cache()
