@@ -5,7 +5,7 @@
 
 namespace reflex {
 
-__device__ __forceinline__ void report_page_wait(uint32_t *status, uint32_t code) { atomicCAS(status, 0u, status_word(kSitePages + code)); }
+__device__ __forceinline__ void report_page_wait(uint32_t *status, uint32_t site) { atomicCAS(status, 0u, status_word(site)); }
 
 // Weights are 2^-24 of what the softmax has them, in sums and in products alike, so that it goes with the division: O is a sum over the keys of weights, which reach 2^8 between
 // two changes of the reference, times values, which reach 2^127 and more, and is not to pass fp32 ahead of the division (nor a weight times a value's 2^e bf16). That holds

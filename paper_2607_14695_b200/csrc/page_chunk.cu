@@ -130,7 +130,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     volatile uint32_t *tile_info = bad_unit + 8;           // [16]: (g + 1) << 4 and what the issuers have to know of tile g (written by the leader's K producer ahead of the arrival on KFULL)
     constexpr uint32_t kFirst = 1u, kLast = 2u, kSecond = 4u, kEnd = 8u;       // of its unit; has live keys in its second half; there is no such tile
     if ((base - raw_addr) + L::NEED > L::TOTAL) {          // (the same for every CTA: all of them leave)
-        if (threadIdx.x == 0) report_page_wait(p.g.status, 15u);
+        if (threadIdx.x == 0) report_page_wait(p.g.status, kSitePageChunk + 15u);
         return;
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -183,7 +183,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             }
         }
         *abort_flag = 1u;
-        report_page_wait(p.g.status, code);
+        report_page_wait(p.g.status, kSitePageChunk + code);
         return false;
     };
 
@@ -403,7 +403,7 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                             info = __reduce_or_sync(0xffffffffu, tile_info[v & 15]);
                             if ((n & 255u) == 0u && !all(*abort_flag == 0u && globaltimer_ns() - t_start < kChunkWaitNs)) break;
                         }
-                        if (info >> 4 != (uint32_t)v + 1u) { *abort_flag = 1u; report_page_wait(p.g.status, 15u); break; }
+                        if (info >> 4 != (uint32_t)v + 1u) { *abort_flag = 1u; report_page_wait(p.g.status, kSitePageChunk + 15u); break; }
                     }
                     if ((info & kEnd) || !issue_pv(info)) break;
                 }

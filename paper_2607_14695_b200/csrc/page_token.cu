@@ -308,7 +308,7 @@ page_token_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
                 --pending;
                 if (!__all_sync(0xffffffffu, wait(bars + st * 8, got_phase)) && !dead) {
                     dead = true;
-                    if (lane == 0) report_page_wait(g.status, 12u);
+                    if (lane == 0) report_page_wait(g.status, kSitePageToken + 1u);
                 }
                 got = got + 1 == C::STAGES ? 0 : got + 1;
                 got_phase ^= got == 0 ? 1u : 0u;

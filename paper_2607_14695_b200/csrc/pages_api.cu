@@ -168,7 +168,8 @@ int reflex_pages_check_status(reflex_pages_t *p, void *stream)
     if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);
     if (e != cudaSuccess) return fail_cuda(e, "status read-back");
     if (word & 0x80000000u)
-        return api_fail(REFLEX_ERR_TIMEOUT, "a device-side wait ran out (status 0x%08x: wait %u, block %u); results of that launch are invalid", word, (word >> 16) & 0x7FFFu, word & 0xFFFFu);
+        return api_fail(REFLEX_ERR_TIMEOUT, "a device-side wait ran out (status 0x%08x: wait site %u, %s, block %u); results of that launch are invalid", word, (word >> 16) & 0x7FFFu,
+                        wait_site_kernel((word >> 16) & 0x7FFFu), word & 0xFFFFu);
     if (word & kStatusBadPage)
         return api_fail(REFLEX_ERR_STATE, "sequence %u: a page outside the pool, or a position outside the page table", word & ~kStatusBadPage);
     return REFLEX_OK;

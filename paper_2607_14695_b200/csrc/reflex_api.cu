@@ -118,6 +118,19 @@ WorkspaceLayout workspace_layout(const reflex_cache_desc &d)
 
 }  // namespace reflex
 
+const char *reflex::wait_site_kernel(uint32_t site)
+{
+    static const struct { uint32_t end; const char *name; } kKernels[] = {
+        {kSiteAttnTc2, "attn_tc_kernel"}, {kSiteGate, "attn_tc2_kernel"}, {kSiteProbe, "gate_tc_kernel"}, {kSiteQkv, "wait_limit_probe_kernel"},
+        {kSiteFewRows, "norm_qkv_tc_kernel"}, {kSiteLinear, "norm_linear_small_kernel"}, {kSiteTileGemm, "linear_res_tc_kernel"},
+        {kSiteChainGemm, "tile_gemm_kernel"}, {kSiteChainAttn, "chain_gemm_kernel"}, {kSiteLinearHalf, "chain_attn_kernel"},
+        {kSiteAttnPair, "linear_half_kernel"}, {kSitePageChunk, "attn_pair_kernel"}, {kSitePageToken, "page_chunk_kernel"},
+        {kSiteEnd, "page_token_kernel"}};
+    for (const auto &k : kKernels)
+        if (site < k.end) return k.name;
+    return "unknown";
+}
+
 extern "C" {
 
 const char *reflex_last_error_string(void) { return g_err; }
@@ -225,18 +238,6 @@ int reflex_cache_slot_map(reflex_cache_t *c, int b, int32_t *slot_of_age)
         }
     }
     return REFLEX_OK;
-}
-
-static const char *wait_site_kernel(uint32_t site)
-{
-    static const struct { uint32_t end; const char *name; } kKernels[] = {
-        {kSiteAttnTc2, "attn_tc_kernel"}, {kSiteGate, "attn_tc2_kernel"}, {kSiteProbe, "gate_tc_kernel"}, {kSiteQkv, "wait_limit_probe_kernel"},
-        {kSiteFewRows, "norm_qkv_tc_kernel"}, {kSiteLinear, "norm_linear_small_kernel"}, {kSiteTileGemm, "linear_res_tc_kernel"},
-        {kSiteChainGemm, "tile_gemm_kernel"}, {kSiteChainAttn, "chain_gemm_kernel"}, {kSiteLinearHalf, "chain_attn_kernel"},
-        {kSiteAttnPair, "linear_half_kernel"}, {kSitePages, "attn_pair_kernel"}, {kSiteEnd, "page_chunk_kernel"}};
-    for (const auto &k : kKernels)
-        if (site < k.end) return k.name;
-    return "unknown";
 }
 
 int reflex_cache_check_status(reflex_cache_t *c, void *stream)

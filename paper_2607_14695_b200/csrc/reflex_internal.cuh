@@ -36,8 +36,10 @@ struct WorkspaceLayout {
 // Wait sites of the status word: a kernel's own numbers (from 1) behind a base of its own, so that a report names the kernel (wait_site_kernel)
 enum WaitSites : uint32_t {
     kSiteAttnTc = 0, kSiteAttnTc2 = 32, kSiteGate = 64, kSiteProbe = 127, kSiteQkv = 128, kSiteFewRows = 144, kSiteLinear = 160, kSiteTileGemm = 176,
-    kSiteChainGemm = 192, kSiteChainAttn = 208, kSiteLinearHalf = 224, kSiteAttnPair = 240, kSitePages = 256, kSiteEnd = 272
+    kSiteChainGemm = 192, kSiteChainAttn = 208, kSiteLinearHalf = 224, kSiteAttnPair = 240, kSitePageChunk = 256, kSitePageToken = 272,
+    kSiteEnd = 288
 };
+const char *wait_site_kernel(uint32_t site);
 // (what the first wait that runs out leaves in the status word)
 __device__ __forceinline__ uint32_t status_word(uint32_t site) { return 0x80000000u | (site << 16) | (blockIdx.x & 0xFFFFu); }
 

@@ -131,3 +131,23 @@ def test_32_byte_stores_to_the_caller_s_rows_look_at_their_address():
     stores = re.findall(r"([^\n;{}]*)\bptx::st_global_v8\(", text)
     assert stores and all(s.strip() == "if (sectors)" for s in stores), stores
     assert re.search(r"const bool sectors = \(\(reinterpret_cast<uintptr_t>\(k_out\) \| reinterpret_cast<uintptr_t>\(v_out\)\) & 31u\) == 0;", text)
+
+
+def test_a_reported_wait_of_the_pages_names_its_kernel():
+    """Their waits are reported through report_page_wait, with numbers from a base of the kernel's own; the table gives every base's kernel, in order."""
+    sites = {n: int(v) for n, v in re.findall(r"(kSite\w+) = (\d+)", open(os.path.join(CSRC, "reflex_internal.cuh")).read())}
+    used = {}
+    for name, _, body in KERNELS:
+        calls = re.findall(r"report_page_wait\([^,]*, (\w+) \+ (\w+)\)", body)
+        assert len(calls) == body.count("report_page_wait("), name
+        if calls:
+            assert len({b for b, _ in calls}) == 1, calls
+            codes = [int(c) for c in re.findall(r"\bwait\([^;]*?, (\d+)\)", body)] + [int(c[:-1]) for _, c in calls if c != "code"]
+            used[calls[0][0]] = (name.split(": ")[1], max(codes))
+    assert {n for n, _ in used.values()} == {"page_chunk_kernel", "page_token_kernel"} and len(used) == 2, used
+    table = re.findall(r'\{(kSite\w+), "(\w+)"\}', open(os.path.join(CSRC, "reflex_api.cu")).read())
+    ends = [sites[e] for e, _ in table]
+    assert ends == sorted(ends) and table[-1][0] == "kSiteEnd"
+    for base, (name, last) in used.items():
+        for site in (sites[base] + 1, sites[base] + last):
+            assert next(n for e, n in table if site < sites[e]) == name
