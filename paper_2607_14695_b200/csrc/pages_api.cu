@@ -69,6 +69,16 @@ PageGeom geometry(const reflex_pages &p, int layer)
     return g;
 }
 
+// (pools, workspace and the NULL stream are those of the handle's device)
+int check_device(const reflex_pages_t *p)
+{
+    int dev = -1;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return fail_cuda(e, "device query");
+    if (dev != p->device) return api_fail(REFLEX_ERR_STATE, "the pages belong to device %d, the current device is %d", p->device, dev);
+    return REFLEX_OK;
+}
+
 // what every call on a handle has to have
 int check_call(const reflex_pages_t *p, int layer, int n_layers, const reflex_page_batch *q, bool needs_cu)
 {
@@ -81,11 +91,7 @@ int check_call(const reflex_pages_t *p, int layer, int n_layers, const reflex_pa
         return api_fail(REFLEX_ERR_SHAPE, "max_pages=%d: a table spans at most 2^30 positions, and one page at least", q->max_pages);
     if (!q->table || !q->len || (needs_cu && !q->cu)) return api_fail(REFLEX_ERR_INVALID_ARG, "table, cu or len of the batch is NULL");
     if (!aligned(q->table, 4) || !aligned(q->len, 4) || !aligned(q->cu, 4)) return api_fail(REFLEX_ERR_ALIGN, "table, cu or len of the batch not aligned to its elements");
-    int dev = -1;
-    const cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return fail_cuda(e, "device query");
-    if (dev != p->device) return api_fail(REFLEX_ERR_STATE, "the pages belong to device %d, the current device is %d", p->device, dev);
-    return REFLEX_OK;
+    return check_device(p);
 }
 
 int check_rotation(const reflex_rotary *r, const int32_t *pos, int d)
@@ -163,6 +169,8 @@ int reflex_pages_destroy(reflex_pages_t *p)
 int reflex_pages_check_status(reflex_pages_t *p, void *stream)
 {
     if (!p) return api_fail(REFLEX_ERR_INVALID_ARG, "pages is NULL");
+    const int rc = check_device(p);
+    if (rc) return rc;
     uint32_t word = 0;
     cudaError_t e = cudaMemcpyAsync(&word, p->ws, sizeof(word), cudaMemcpyDeviceToHost, (cudaStream_t)stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize((cudaStream_t)stream);

@@ -151,3 +151,14 @@ def test_a_reported_wait_of_the_pages_names_its_kernel():
     for base, (name, last) in used.items():
         for site in (sites[base] + 1, sites[base] + last):
             assert next(n for e, n in table if site < sites[e]) == name
+
+
+def test_every_call_on_pages_looks_at_the_device():
+    """The pages' calls are refused while another device is current: with another device's NULL stream the status word would be read ahead of the kernels that
+    write it. (reflex_pages_destroy touches host memory alone.)"""
+    text = re.sub(r"//[^\n]*|/\*.*?\*/", "", open(os.path.join(CSRC, "pages_api.cu")).read(), flags=re.S)
+    calls = re.findall(r"\nint (reflex_pages_\w+)\(reflex_pages_t \*p\b[^{]*\{(.*?)\n\}\n", text, flags=re.S)
+    assert {n for n, _ in calls} == {"reflex_pages_destroy", "reflex_pages_check_status", "reflex_pages_write", "reflex_pages_read", "reflex_pages_attention"}
+    assert "return check_device(p);" in re.search(r"int check_call\(.*?\n\}\n", text, flags=re.S).group(0)
+    for name, body in calls:
+        assert name == "reflex_pages_destroy" or re.search(r"(?:const int|int) rc = check_(?:call|device)\(p", body), name
