@@ -490,8 +490,11 @@ class Pages:
         self.workspace = torch.empty((wsb,), dtype=torch.uint8, device=self.device)
         self.handle = ctypes.c_void_p()
         with torch.cuda.device(self.device):
+            raw, here = _stream(stream), torch.cuda.current_stream()
+            if raw != here.cuda_stream:         # the pools were allocated and zeroed on the current stream
+                (torch.cuda.ExternalStream(raw, device=self.device) if raw else torch.cuda.default_stream()).wait_stream(here)
             _check(lib.reflex_pages_create(ctypes.byref(self.desc), _ptr(self.k_pool), _ptr(self.v_pool), _ptr(self.k_exp), _ptr(self.v_exp), _ptr(self.workspace),
-                                           _stream(stream), ctypes.byref(self.handle)))
+                                           raw, ctypes.byref(self.handle)))
 
     def close(self):
         if getattr(self, "handle", None) is not None and self.handle:

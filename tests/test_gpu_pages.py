@@ -810,3 +810,26 @@ def test_rotary_of_as_many_tokens_as_there_can_be():
         assert ((x[i, 0].cpu().double() - want[0, 0]).abs() <= HALF[BF16] * want[0, 0].abs() + 2 * (2.0 ** -22 + 2.0 ** -20)).all(), i
     del x, pos
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_pages_made_for_another_stream(raw):
+    """Calls on the stream that the pages were made for come behind the zeroing of the pools, which the current stream does (6 GB here)."""
+    side = torch.cuda.Stream()
+    n, d, page = 64, 128, 16
+    k, v = [torch.randn(n, 1, d, device=DEV).to(BF16) for _ in range(2)]
+    n_pages = (3 << 30) // (page * d * 2)
+    table = torch.tensor([[n_pages - 1, 5, n_pages // 2, 7]], dtype=torch.int32, device=DEV)
+    batch = rb.PageBatch(table, torch.tensor([0, n], dtype=torch.int32, device=DEV), torch.tensor([n], dtype=torch.int32, device=DEV))
+    out = [torch.zeros((1, 1, n, 1, d), dtype=BF16, device=DEV) for _ in range(2)]
+    torch.cuda.synchronize()
+    on = side.cuda_stream if raw else side
+    pages = rb.Pages(1, n_pages, page, 1, 1, d, rb.DTYPE_BF16, max_seqs=1, max_rows=n, stream=on)
+    rb.reflex_pages_write(pages, 0, batch, k, v, stream=on)
+    side.synchronize()
+    torch.cuda.synchronize()
+    rb.reflex_pages_read(pages, 0, batch, out[0], out[1])
+    assert torch.equal(out[0][0, 0], k) and torch.equal(out[1][0, 0], v)
+    with torch.cuda.stream(side):                   # and the other way round: made for the NULL stream while another one is current
+        pages = rb.Pages(1, 4, page, 1, 1, d, rb.DTYPE_BF16, max_seqs=1, max_rows=n, stream=0)
+    rb.reflex_pages_check_status(pages)
