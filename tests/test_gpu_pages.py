@@ -833,3 +833,54 @@ def test_pages_made_for_another_stream(raw):
     with torch.cuda.stream(side):                   # and the other way round: made for the NULL stream while another one is current
         pages = rb.Pages(1, 4, page, 1, 1, d, rb.DTYPE_BF16, max_seqs=1, max_rows=n, stream=0)
     rb.reflex_pages_check_status(pages)
+
+
+def _check_each(c, q, out, causal, window=0):
+    """Every sequence of c (filled by write_all) against 64 bits, on the GPU."""
+    for b, n in enumerate(c.news):
+        if n == 0:
+            continue
+        r = slice(int(c.cu[b]), int(c.cu[b + 1]))
+        want, lim = _attend64(q[r], c.k[0][b].to(DEV), c.v[0][b].to(DEV), c.d ** -0.5, causal, window)
+        assert ((out[r].double() - want).abs() <= lim).all(), b
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("kind", ["tokens", "a chunk among tokens", "chunks among tokens", "idle"])
+@pytest.mark.parametrize("d,Hq,Hkv", [(64, 4, 2), (128, 16, 2), (256, 8, 1)])
+def test_more_sequences_than_a_warp_has_lanes(fmt, kind, d, Hq, Hkv):
+    """100 sequences: the walk along the line of work goes on in further blocks of 32; batches whose sequences are nothing like their average."""
+    B = 100
+    lens = [1 + (b * 97) % 130 for b in range(B)]
+    news = {"tokens": [1] * B, "a chunk among tokens": [1] * 70 + [300] + [1] * 29, "chunks among tokens": [90 if b % 9 == 4 else 1 for b in range(B)],
+            "idle": [0] * 40 + [2] + [0] * 58 + [40]}[kind]
+    lens = [max(x, n) for x, n in zip(lens, news)]
+    c = Paged(lens, news, 16, Hq, Hkv, d, BF16, fmt, seed=d, spare_rows=2)
+    c.poison()
+    k = c.normal(sum(lens), Hkv, d, std=1.5)
+    c.write_all(k=k, v=c.normal(sum(lens), Hkv, d))
+    q = c.normal(c.rows, Hq, d).to(DEV)
+    first = rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.full_like(q, 7.0), causal=True).clone()
+    _check_each(c, q, first, True)
+    assert (first[int(c.cu[-1]):] == 7.0).all()
+    for _ in range(3):
+        assert torch.equal(first, rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.full_like(q, 7.0), causal=True))
+    rb.reflex_pages_check_status(c.pages)
+
+
+@pytest.mark.parametrize("d,Hq,Hkv", [(64, 8, 1), (128, 8, 1), (256, 8, 1)])
+@pytest.mark.parametrize("news", [1, 2])
+@pytest.mark.parametrize("every", [16, 100, 1000])
+def test_logits_that_grow_under_few_tokens(d, Hq, Hkv, news, every):
+    """The kernel of few tokens: running maxima that grow by 2^9 every block of keys, or from one part of a sequence to the next."""
+    n = 4000
+    c = Paged([n, 900], [news, news], 64, Hq, Hkv, d, BF16, rb.PAGE_SAME, seed=d)
+    k, v, q = c.normal(n + 900, Hkv, d, std=0.2), c.normal(n + 900, Hkv, d), c.normal(c.rows, Hq, d, std=0.2)
+    k[:, :, 0] = (torch.arange(n + 900) % n // every)[:, None].to(BF16)
+    q[:, :, 0] = 6.25                           # of 9.02 log2 units a step
+    c.write_all(k=k, v=v)
+    out = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.empty_like(q, device=DEV), scale=1.0, causal=True)
+    for b in range(2):
+        r = slice(int(c.cu[b]), int(c.cu[b + 1]))
+        want, lim = _attend64(q[r].to(DEV), c.k[0][b].to(DEV), c.v[0][b].to(DEV), 1.0, True)
+        assert ((out[r].double() - want).abs() <= lim).all(), b

@@ -162,3 +162,12 @@ def test_every_call_on_pages_looks_at_the_device():
     assert "return check_device(p);" in re.search(r"int check_call\(.*?\n\}\n", text, flags=re.S).group(0)
     for name, body in calls:
         assert name == "reflex_pages_destroy" or re.search(r"(?:const int|int) rc = check_(?:call|device)\(p", body), name
+
+
+def test_kernels_of_the_paged_prefix_are_the_ones_a_call_can_reach():
+    assert {n for n, _, _ in KERNELS if re.match(r"(page\w*|rotary)\.cuh?: ", n)} == {
+        "rotary.cu: rotary_axes_kernel", "page_rows.cu: page_write_kernel", "page_rows.cu: page_read_kernel", "page_plain.cu: page_plain_kernel",
+        "page_token.cu: page_token_kernel", "page_chunk.cu: page_chunk_kernel", "page_chunk.cu: page_widen_kernel", "page_merge.cu: page_merge_kernel"}
+    for name, launcher in (("rotary_axes", "launch_rotary_axes"), ("page_write", "launch_page_write"), ("page_read", "launch_page_read"), ("page_plain", "launch_page_plain"),
+                           ("page_token", "launch_page_token"), ("page_chunk", "launch_page_chunk"), ("page_widen", "launch_page_widen"), ("page_merge", "launch_page_merge")):
+        assert f" = {launcher}(" in open(os.path.join(CSRC, "pages_api.cu")).read(), name
