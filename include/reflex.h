@@ -432,8 +432,8 @@ int reflex_pages_read(reflex_pages_t *pages, int layer, int n_layers, const refl
 
 /* The new tokens' attention over the pages of one layer (their own keys and values included: write them first):
  *   out = softmax(scale * q K^T + mask) V,   KV head of query head h: h / (Hq / Hkv)
- *   q, out   device [n_rows][Hq][d] dtype
- *   scale    <= 0 selects 1/sqrt(d)
+ *   q, out   device [n_rows][Hq][d] dtype; they must not overlap
+ *   scale    <= 0 selects 1/sqrt(d); at most 2e38
  *   causal   0: every new token sees all len[b] tokens; 1: the token at position p sees positions <= p
  *   window   > 0: only positions > p - window; 0: no limit
  * A row that sees nothing is 0. Softmax and sums are fp32; on the tensor cores the weights are rounded to bf16 before they meet V. Values of

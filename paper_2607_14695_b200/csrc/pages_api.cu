@@ -230,7 +230,7 @@ int reflex_pages_attention(reflex_pages_t *p, int layer, const reflex_page_batch
     if (n_rows < 0 || n_rows > d.max_rows) return api_fail(REFLEX_ERR_SHAPE, "n_rows=%d outside [0, max_rows=%d]", n_rows, d.max_rows);
     if (causal != 0 && causal != 1) return api_fail(REFLEX_ERR_INVALID_ARG, "causal must be 0 or 1");
     if (window < 0) return api_fail(REFLEX_ERR_INVALID_ARG, "window=%d is negative", window);
-    if (!(scale <= 3.0e38f)) return api_fail(REFLEX_ERR_INVALID_ARG, "scale must be a finite number");
+    if (!(scale <= 2.0e38f)) return api_fail(REFLEX_ERR_INVALID_ARG, "scale must be a number of at most 2e38");       // (times log2 e it is finite)
     if (n_rows == 0) return REFLEX_OK;
     if (!q || !out) return api_fail(REFLEX_ERR_INVALID_ARG, "q / out is NULL");
     if (q == out) return api_fail(REFLEX_ERR_INVALID_ARG, "out must not be q");

@@ -884,3 +884,21 @@ def test_logits_that_grow_under_few_tokens(d, Hq, Hkv, news, every):
         r = slice(int(c.cu[b]), int(c.cu[b + 1]))
         want, lim = _attend64(q[r].to(DEV), c.k[0][b].to(DEV), c.v[0][b].to(DEV), 1.0, True)
         assert ((out[r].double() - want).abs() <= lim).all(), b
+
+
+@pytest.mark.parametrize("dtype,fmt", [(BF16, rb.PAGE_SAME), (BF16, rb.PAGE_E4M3), (F32, rb.PAGE_SAME)])
+@pytest.mark.parametrize("news", [1, 40])
+def test_the_largest_scales(dtype, fmt, news):
+    """A scale of 2e38 is one (times log2 e still finite); above it, and NaN, are refused."""
+    c = Paged([200], [news], 32, 4, 1, 128, dtype, fmt)
+    k, v = c.normal(200, 1, 128), c.normal(200, 1, 128)
+    c.write_all(k=k * 2.0 ** -60, v=v)
+    q = c.normal(c.rows, 4, 128) * 2.0 ** -70                   # q k of about 2^-127, logits of about 1
+    out = rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.empty_like(q, device=DEV), scale=2e38 if news == 1 else 1.5e38)
+    # (products and sums down there are subnormal: steps of 2^-149 each, of which 2 * 128 and the weights' exponents are a logit's error)
+    want, mass, slip = c.attend(q, scale=2e38 if news == 1 else 1.5e38)
+    c.check(out, (want, mass, slip + 2 * 128 * 2.0 ** -149 * 2e38))
+    for scale in (3e38, math.inf, math.nan):
+        with pytest.raises(rb.ReflexError) as e:
+            rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.empty_like(q, device=DEV), scale=scale)
+        assert e.value.code == rb.ERR_INVALID_ARG
