@@ -59,7 +59,7 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
     const int e0 = turns && !adj ? lane * 8 : lane * 16, e1 = turns && !adj ? lane * 8 + R / 2 : lane * 16 + 8;
     TurnRate rate[TURNS ? 8 : 1];
     uint32_t axes = 0;              // four bits each
-    uint32_t still = 0, unknown = 0;          // pairs that do not turn, that have no angle (see rotary_axes_kernel)
+    uint32_t marks = 0;             // pairs that do not turn, and from bit 8 on those that have no angle (see rotary_axes_kernel)
     if (TURNS && turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -67,8 +67,8 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
             rate[TURNS ? i : 0] = turn_rate(r.rot.freq[lane * 8 + i]);
             if (axis >= r.rot.axes) rate[TURNS ? i : 0].lo = rate[TURNS ? i : 0].hi = 0u;
             else axes |= (uint32_t)axis << (4 * i);
-            if ((rate[TURNS ? i : 0].lo | rate[TURNS ? i : 0].hi) == 0u) still |= 1u << i;
-            else if (!turnable(r.rot.freq[lane * 8 + i])) unknown |= 1u << i;
+            if ((rate[TURNS ? i : 0].lo | rate[TURNS ? i : 0].hi) == 0u) marks |= 1u << i;
+            else if (!turnable(r.rot.freq[lane * 8 + i])) marks |= 256u << i;
         }
     }
     __syncthreads();
@@ -93,7 +93,7 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
 #pragma unroll
                     for (int i = 0; i < (TURNS ? 8 : 1); ++i) {
                         turn(rate[i], r.pos[(size_t)((axes >> (4 * i)) & 15u) * n_rows + t], s[i], c[i]);
-                        if (unknown & (1u << i)) s[i] = c[i] = __int_as_float(0x7fc00000);
+                        if (marks & (256u << i)) s[i] = c[i] = __int_as_float(0x7fc00000);
                     }
                 }
                 const int b = find_seq(cu_s, q.B, (int)t);
@@ -104,6 +104,7 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
                 else if (lane == 0 && blockIdx.y == 0) report_bad_page(g.status, b);
             }
             const size_t row = base + ((size_t)h << g.log_p);
+            const uint32_t still = marks & 255u;
             float u[8], w[8];
             if (TURNS || FMT != REFLEX_PAGE_SAME) { widen8(ka, u); widen8(kb, w); }
             if (TURNS && turns) {
@@ -123,6 +124,8 @@ page_write_kernel(const PageGeom g, const reflex_page_batch q, const T *k, int64
                         w[i] = u0 * s[i] + w0 * c[i];
                     }
                 }
+                // (asked for again, not kept: registers for it cost every row more)
+                if (still && exists) { ka = raw8(kr + (size_t)h * g.d + e0); kb = raw8(kr + (size_t)h * g.d + e1); }
                 if (FMT != REFLEX_PAGE_SAME && still) {
                     Raw8<float> u0, w0, u1 = narrow8<float>(u), w1 = narrow8<float>(w);
                     float f[8];

@@ -25,8 +25,8 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
     const int e0 = turns && !ADJ ? slot * 8 : slot * 16, e1 = turns && !ADJ ? slot * 8 + R / 2 : slot * 16 + 8;
     TurnRate rate[8];
     uint32_t axes = 0;              // four bits each
-    uint32_t still = 0;             // pairs that do not turn: 0 times an infinity of the other element is not to be added to them
-    uint32_t unknown = 0;           // pairs without an angle
+    // pairs that do not turn (0 times an infinity of the other element is not to be added to them), and from bit 8 on those that have no angle
+    uint32_t marks = 0;
     if (turns) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -34,8 +34,8 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
             rate[i] = turn_rate(r.rot.freq[slot * 8 + i]);
             if (axis >= r.rot.axes) rate[i].lo = rate[i].hi = 0u;
             else axes |= (uint32_t)axis << (4 * i);
-            if ((rate[i].lo | rate[i].hi) == 0u) still |= 1u << i;
-            else if (!turnable(r.rot.freq[slot * 8 + i])) unknown |= 1u << i;
+            if ((rate[i].lo | rate[i].hi) == 0u) marks |= 1u << i;
+            else if (!turnable(r.rot.freq[slot * 8 + i])) marks |= 256u << i;
         }
     }
     const int h0 = blockIdx.y * heads_per_thread, h1 = min(H, h0 + heads_per_thread);
@@ -54,7 +54,6 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
                 for (int i = 0; i < 8; ++i) {
                     turn(rate[i], r.pos[(size_t)((axes >> (4 * i)) & 15u) * n + t], s[i], c[i]);
                     if (r.inverse) s[i] = -s[i];
-                    if (unknown & (1u << i)) s[i] = c[i] = __int_as_float(0x7fc00000);
                 }
             }
 #pragma unroll
@@ -76,7 +75,11 @@ rotary_axes_kernel(const T *x, int64_t ldx, T *y, int64_t ldy, const PageRotatio
                     }
                     ya = narrow8<T>(u);
                     yb = narrow8<T>(v);
-                    if (still) keep_pairs<T, ADJ>(still, a[k], b[k], ya, yb);
+                    if (marks) {
+                        keep_pairs<T, ADJ>(marks, a[k], b[k], ya, yb);
+                        const float nan[8] = {NAN, NAN, NAN, NAN, NAN, NAN, NAN, NAN};
+                        keep_pairs<T, ADJ>(marks >> 8, narrow8<T>(nan), narrow8<T>(nan), ya, yb);
+                    }
                 }
                 put8(yr + (size_t)(h + k) * d + e0, ya);
                 put8(yr + (size_t)(h + k) * d + e1, yb);
