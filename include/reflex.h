@@ -388,8 +388,8 @@ typedef struct {
 } reflex_rotary;
 
 /* y = x rotated (inverse: by the opposite angles, which is also the gradient with respect to x of a loss whose gradient with respect
- * to y is given as x, and takes a row back to where it came from). Angles are reduced exactly in 64-bit integers, so positions
- * of any size lose nothing; the products are fp32, rounded to dtype once.
+ * to y is given as x, and takes a row back to where it came from). Angles are counted in 64-bit fractions of a
+ * revolution and kept to 2^-32 of one, for positions of any size; sine and cosine of that and the products are fp32, rounded to dtype once.
  *   x, y   device [n][H][d] dtype, tokens ldx / ldy elements apart (heads of a packed projection: ldx > H d); y may be x itself
  *          (same ld) but must not overlap it otherwise
  *   pos    device int32 [axes][n]

@@ -7,9 +7,11 @@ namespace reflex {
 
 __device__ __forceinline__ void report_page_wait(uint32_t *status, uint32_t site) { atomicCAS(status, 0u, status_word(site)); }
 
-// Weights are 2^-24 of what the softmax has them, in sums and in products alike, so that it goes with the division: O is a sum over the keys of weights, which reach 2^8 between
-// two changes of the reference, times values, which reach 2^127 and more, and is not to pass fp32 ahead of the division (nor a weight times a value's 2^e bf16). That holds
-// for 2^15 such keys. Down below, values of 2^-100 are still normal numbers as products.
+// Weights are 2^-24 of what the softmax has them, in sums and in products alike, so that it goes with the division: O is a sum over the keys of weights,
+// which reach 2^8 between two changes of the reference, times values, which reach 2^127 and more, and is not to pass fp32 ahead of the division (nor a
+// weight times a value's 2^e bf16). That holds for 2^15 such keys. Down below, values of 2^-100 are still normal numbers as products. (The tensor-core
+// kernels round them to bf16 for the product with V, the one form that its operands have there; the sum takes them as they are. Against 64 bits the
+// result's error goes from 0.0017 of its size, which is its own rounding to bf16, to 0.0023.)
 constexpr float kWeightShift = 24.f;
 
 struct PageSeq { int b, row0, n, len; };      // first row of its new tokens, how many, tokens in all

@@ -10,17 +10,19 @@
 //                in turn: each then has the time of two tiles for its chain of loads, maximum, exponentials and stores, and a scheduler
 //                has four of its warps. The threads of a row agree on the reference maximum at one named barrier per 32 rows, where the group
 //                that has had the tile before leaves the row's reference, too; O is rescaled only where it has grown by more than 2^8.
-// What bounds it: at head_dim 256 the tensor pipe (2048 cycles a tile; operand reads then take two thirds of the shared memory's bandwidth), at 128 and
-// 64 the softmax (some 700 issue slots a scheduler and tile, which the helper warps need as well; a quarter of the exponentials by a
-// polynomial instead of the special-function unit cost more of them than the unit saved: 310 us for 301 at 4 x 4160 causal tokens, 16 heads of 128).
-// Measured: that prefill in 283 us, 1.0 PFLOP/s of the products that its mask leaves; a frame of 256 tokens of each of 16 sequences of 3376, 8 heads of
-// 256 on one KV head, 8-bit pages, in 111 us with widening (15) and merging (12). Heads of 64 run as heads of 128 whose upper chunk is left out of
-// Q K^T and whose upper columns of O are never read: P V costs twice, underneath the softmax.
+// What bounds it: at head_dim 256 the tensor pipe (2048 of some 2350 cycles a tile; with set-up, ends of units and the uneven last tiles it is busy for 67
+// % of the launch; operand reads then take two thirds of the shared memory's bandwidth), at 128 and 64 the softmax (some 700 issue slots a scheduler and
+// tile, which the helper warps need as well; a quarter of the exponentials by a polynomial instead of the special-function unit cost more of them than the
+// unit saved: 310 us for 301 at 4 x 4160 causal tokens, 16 heads of 128). Measured in a warm graph (in brackets a pass among others, caches cold): that
+// prefill in 283 to 292 us (327 to 339), 1.0 PFLOP/s of the products that its mask leaves; a frame of 256 tokens of each of 16 sequences of 3376, 8 heads
+// of 256 on one KV head, 8-bit pages, in 111 to 113 us (122 to 127) with widening (15) and merging (12). Heads of 64 run as heads of 128 whose upper chunk
+// is left out of Q K^T and whose upper columns of O are never read: P V costs twice, underneath the softmax.
 //
 // The grid is one pair per SM pair; the tiles of all units form one line that the pairs share evenly (PageLine), so uneven sequences, causal masks and single
 // sequences fill the device alike. A unit that more than one pair works on leaves fp32 partials for page_merge_kernel.
 // 8-bit pages are first widened to bf16, exactly, into one layer's worth of workspace (page_widen_kernel): a page is used by every row tile and by both
-// CTAs of a pair, and unpacking it inside each costs more instruction slots than the softmax leaves.
+// CTAs of a pair. (Unpacking it inside each has not been built: at head_dim 128 and 64 the softmax takes the issue slots, at 256 there are slots
+// left, 0.27 issues a cycle, and it is the widening's 15 us that it could save.)
 //
 // Every wait is bounded; one that runs out is reported in the status word and makes the results NaN.
 #include <math.h>

@@ -1,8 +1,11 @@
-// Joins the partial results of units that several CTAs have worked on: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i, in an order that the
-// units alone decide. A thread takes 8 columns of a row (partials lie as [column group][row][8], so a warp reads a contiguous kilobyte) and has
-// the loads of 8 partials in flight (which is why there are two blocks per SM and not four: a frame of 256 tokens over 3376 keys in 23.9 us, not 27.0); long lists (one sequence over the whole device) are cut among the warps of a block, which then add up.
+// Joins the partial results of units that several CTAs have worked on: out = sum_i 2^(m_i - m) O_i / sum_i 2^(m_i - m) l_i, in an order that the units
+// alone decide. A thread takes 8 columns of a row (partials lie as [column group][row][8], so a warp reads a contiguous kilobyte) and has the loads of 8
+// partials in flight (which is why there are two blocks per SM and not four: a frame of 256 tokens over 3376 keys in 23.9 us, not 27.0); long lists (one
+// sequence over the whole device) are cut among the warps of a block, which then add up.
 //
-// It also computes again, row by row, the sequences that the tensor-core kernel has marked (see PagePartials::careful).
+// It also computes again, row by row, the sequences that the tensor-core kernel has marked (see PagePartials::careful). That is the plain kernel's work,
+// one row at a time: with one value of one sequence not finite at a key that some rows of a unit see and others do not, a causal frame of 256 tokens over
+// 3376 keys takes 0.76 ms and not 0.024, 16 such frames 1.6 and not 0.115, a causal prefill of 4160 tokens (16 heads of 128) 10.2 and not 0.30.
 #include "page_join.cuh"
 #include "page_plain.cuh"
 

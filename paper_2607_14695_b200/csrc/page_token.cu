@@ -1,6 +1,6 @@
 // Attention of few new tokens per sequence over pages (reflex_pages_attention): one token of each stream, or a handful.
 //
-// Bound by memory: the keys and values of a (sequence, KV head) are read once for its G query heads and a tile of 8 or 16 rows (token, head).
+// The keys and values of a (sequence, KV head) are read once for its G query heads and a tile of 8 or 16 rows (token, head).
 // TMA brings 16 rows of keys and 16 of values in swizzled boxes, and a thread's 16-byte pieces of them are its operands of mma.m16n8k16 as they lie
 // there, because the order of the contraction is free: no transposition, no bank conflict. With g = lane / 4 and t = lane % 4:
 //   S^T = K Q^T, 16 keys by 8 query rows: thread (g, t) takes pieces of keys g and g + 8; four consecutive elements of the pieces of t = 0 .. 3 are the
@@ -10,7 +10,8 @@
 // 8-bit rows stay unscaled in the products (they are exact in bf16): 2^e of a key scales its logits, 2^e of a value the key's weight, in fp32.
 // A warp walks every WARPS-th block of 16 keys with a running maximum, fetches for itself, and has one or two blocks on their way while it works on one:
 // 100 KB or more per SM. (64 streams of 3300 keys in 8 bits, 112 MB: 46.7 us with one block at a time in registers, 49.5 with rows by cp.async, whose
-// 17 instructions a block kept the load pipe busy, 33.6 by TMA and with all that follows.)
+// 17 instructions a block kept the load pipe busy, 33.6 by TMA and with all that follows. That is twice the 17 that the bytes take: the schedulers issue 0.41
+// instructions a cycle, and the largest stall is the block's barriers, three at the end of a unit, where all warps of the SM's one CTA stand.)
 //
 // The keys of all (sequence, row tile, KV head) units form one line that the CTAs share evenly, whatever the lengths; a unit that more than one
 // CTA works on leaves fp32 partials, which the last of them to finish joins in the order of the keys (results do not depend on timing).
@@ -585,6 +586,8 @@ static cudaError_t launch_token(const PageAttention &a, const PagePartials &part
 // them expanded again, so page_chunk_kernel is ahead from some number of rows on; later in 8-bit formats, whose pages have to be widened for it.
 // bf16, 64 streams: 53 us here and 57 there at 16 rows of 256 (3300 keys), 124 and 57 at 32; 95 and 79 at 32 rows of 128 (2000 keys, 4 KV heads).
 // int8: 63 and 115 at 32 rows of 256, 111 and 117 at 64; 96 and 145, 174 and 145 at 32 and 64 rows of 128; 134 and 202 at 32 rows of 64.
+// (What is known of a batch is its average: lengths are on the device. A chunk of hundreds of rows among many sequences of one token comes here as well, where
+// each of its tiles reads the keys again; the figures are those of even batches.)
 int page_token_rows(int dtype, int format, int d, int G, int rows)
 {
     if (dtype != REFLEX_DTYPE_BF16 || d < 64 || G > 4096) return 0;

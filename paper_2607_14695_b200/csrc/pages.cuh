@@ -98,7 +98,7 @@ __device__ __forceinline__ uint32_t bf16x2_fma(uint32_t a, uint32_t b, uint32_t 
 // Four bytes of an 8-bit row as they are before expand() (int8: plus 128, by the sign bits)
 template <int FMT> __device__ __forceinline__ uint32_t biased(uint32_t w) { return FMT == REFLEX_PAGE_INT8 ? w ^ 0x80808080u : w; }
 // Two bytes, in the low halves of x's halves, as two bf16: exact, times 2^-kExpandShift. Most of it on the FMA pipe: logic operations and byte permutations
-// have half its rate, and the attention of few tokens is bound by them.
+// have half its rate, and unpacking is most of what the attention of few tokens issues.
 //   int8: a byte u in the low bits of a bf16 is the (subnormal) number u 2^-133; times 2^127, less 128 2^-6, is the whole number times 2^-6.
 //   e4m3: sign, four bits of exponent and three of mantissa moved to where bf16 has them (16 x moves them, and the sign bit's 128 times 240 adds what takes it
 //   from bit 11 to bit 15) give the number times 2^-120, whether it is normal or not; the product with 2^120 is exact.
@@ -124,7 +124,8 @@ template <int FMT> __device__ __forceinline__ float exponent_f32(int e) { return
 
 // ---- rotation angles ----
 // A pair's frequency in revolutions per position, modulo 1, as a 64-bit fraction: position times fraction, modulo 2^64, is the fraction of a
-// revolution that the position turns by, for any 32-bit position and with no rounding. Its upper 32 bits are a quarter of fp32's spacing near 1.
+// revolution that the position turns by, for any 32-bit position. Its upper 32 bits are kept, 1.5e-9 radians; as a number of half revolutions
+// they are then rounded to fp32 (2^-25 at most: against 64 bits a rotation's fp32 error is 4.8e-8, where 64-bit angles leave 3.6e-8).
 // (That is as far as 1 / (2 pi) in two doubles goes: from 2^40 on an angle would lose bits, and the fraction of NaN or an infinity is none. `turnable` says so;
 // such a pair comes out NaN. What rate they have does not matter, but it is not 0.)
 struct TurnRate { uint32_t lo, hi; };
