@@ -437,7 +437,7 @@ int reflex_pages_read(reflex_pages_t *pages, int layer, int n_layers, const refl
  *   causal   0: every new token sees all len[b] tokens; 1: the token at position p sees positions <= p
  *   window   > 0: only positions > p - window; 0: no limit
  * A row that sees nothing is 0. Softmax and sums are fp32; on the tensor cores the weights are rounded to bf16 before they meet V. Values of
- * any finite size do not overflow in sums of up to 2^15 keys; below 2^-100 they lose bits.
+ * any finite size do not overflow in sums of up to 2^15 keys; below 2^-100 (rows of 8-bit pages: 2^-80) sums lose bits.
  * Requirements: n_rows <= max_rows; in bf16, (n_rows Hq / 8 + B Hkv) (max_pages page / 64 + 2) <= 2e9 and n_rows Hq / Hkv < 2^31 - 255 (REFLEX_ERR_SHAPE). */
 int reflex_pages_attention(reflex_pages_t *pages, int layer, const reflex_page_batch *batch, const void *q, void *out, int n_rows, float scale,
                            int causal, int window, void *stream);
