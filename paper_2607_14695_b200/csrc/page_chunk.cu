@@ -411,11 +411,28 @@ page_chunk_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
                 }
             } else {
                 bool ok = true, end = false;
+                // The next tile's keys are there (true), or P V of tile v is due first. (Waiting for the keys alone could be for ever: their unit may find room in the list only
+                // once the unit of tile v is done.)
+                auto keys_or_due = [&]() -> bool {
+                    const uint32_t keys = bar(L::KFULL + q_st), due = bar(L::PFULL + v_buf);
+                    if (all(mbar_try_wait(keys, q_sph))) return true;
+                    const unsigned long long t_start = globaltimer_ns();
+                    for (uint32_t n = 1;; ++n) {
+                        if (all(mbar_try_wait(keys, q_sph))) return true;
+                        if (q > v && all(mbar_test_wait(due, v_bph))) return false;
+                        if ((n & 255u) == 0u) {
+                            if (!all(*abort_flag == 0u)) break;
+                            if (!all(globaltimer_ns() - t_start < kChunkWaitNs)) { report_page_wait(p.g.status, kSitePageChunk + 4u); break; }
+                        }
+                    }
+                    *abort_flag = 1u;
+                    ok = false;
+                    return false;
+                };
                 while (ok) {
                     // Q K^T runs one tile ahead, but for a tile whose weights are there already: the end of a unit waits for nothing else.
                     while (!end && q < v + NS && (q == v || !all(mbar_test_wait(bar(L::PFULL + v_buf), v_bph)))) {
-                        ok = all(wait(L::KFULL + q_st, q_sph, 4));
-                        if (!ok) break;
+                        if (!keys_or_due()) break;
                         const uint32_t info = __reduce_or_sync(0xffffffffu, tile_info[q & 15]);
                         end = (info & kEnd) != 0u;
                         if (end) break;

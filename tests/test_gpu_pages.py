@@ -902,3 +902,25 @@ def test_the_largest_scales(dtype, fmt, news):
         with pytest.raises(rb.ReflexError) as e:
             rb.reflex_pages_attention(c.pages, 0, c.batch, q.to(DEV), torch.empty_like(q, device=DEV), scale=scale)
         assert e.value.code == rb.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("d,G", [(64, 8), (128, 8), (256, 8), (256, 1)])
+@pytest.mark.parametrize("fmt", [rb.PAGE_SAME, rb.PAGE_E4M3])
+def test_long_runs_of_units_without_a_key(d, G, fmt):
+    """New tokens that see nothing (sequences of no token; more new tokens than tokens, causal) fill the lists of units between those that see something, and behind the last one."""
+    lens = [130, 0, 300, 0, 64, 5, 700, 0, 0, 90, 2, 0]
+    news = [40, 900, 70, 2500, 64, 1200, 33, 300, 700, 90, 800, 2000]
+    c = Paged(lens, news, 32, 4 * G, 4, d, BF16, fmt, seed=d + G)
+    c.poison()
+    c.write_all()
+    q = c.normal(c.rows, 4 * G, d).to(DEV)
+    for causal in (True, False):
+        out = rb.reflex_pages_attention(c.pages, 0, c.batch, q, torch.full_like(q, 7.0), causal=causal)
+        rb.reflex_pages_check_status(c.pages)
+        for b, (n, length) in enumerate(zip(news, lens)):
+            r = slice(int(c.cu[b]), int(c.cu[b + 1]))
+            if length == 0:
+                assert (out[r] == 0).all(), b
+                continue
+            want, lim = _attend64(q[r], c.k[0][b].to(DEV), c.v[0][b].to(DEV), d ** -0.5, causal)
+            assert ((out[r].double() - want).abs() <= lim).all(), b

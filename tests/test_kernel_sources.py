@@ -171,3 +171,12 @@ def test_kernels_of_the_paged_prefix_are_the_ones_a_call_can_reach():
     for name, launcher in (("rotary_axes", "launch_rotary_axes"), ("page_write", "launch_page_write"), ("page_read", "launch_page_read"), ("page_plain", "launch_page_plain"),
                            ("page_token", "launch_page_token"), ("page_chunk", "launch_page_chunk"), ("page_widen", "launch_page_widen"), ("page_merge", "launch_page_merge")):
         assert f" = {launcher}(" in open(os.path.join(CSRC, "pages_api.cu")).read(), name
+
+
+def test_the_issuer_of_both_products_does_not_wait_for_keys_ahead_of_a_product_that_is_due():
+    """The producer of keys lists units as far as the list has room, and an entry is free once its unit's last P V is done. A warp that issues both products and waited for the next tile's
+    keys with that P V still to be issued would wait for itself, through units without tiles that fill the list."""
+    body = _body("page_chunk_kernel")
+    both = body[body.index("bool ok = true, end = false"):body.index("float *maxima")]
+    assert "wait(L::KFULL" not in both and "if (!keys_or_due()) break;" in both
+    assert "if (q > v && all(mbar_test_wait(due, v_bph))) return false;" in both
